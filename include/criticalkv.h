@@ -270,6 +270,110 @@ CKV_API int criticalkv_diagnose(criticalkv_handle h, const criticalkv_desc* d, c
                                 void* stream);
 
 /*
+ * ---- Decoding on the compressed cache ---------------------------------------------------------------------------
+ *
+ * After a prefill has been compressed, decoding reads a cache whose KV heads hold different numbers of rows (adaptive
+ * budgets).  The cache is therefore paged per (sequence, KV head): page_table[s, g, :] lists the pages of that head,
+ * row i of it is slot i % page_size of page page_table[s, g, i / page_size], and every head has its own length.
+ *
+ *   criticalkv_rope         rotary positions of new queries and keys (a new token's position is not its row number)
+ *   criticalkv_cache_store  writes rows into the pages: new tokens, or the rows a selection kept; quantises them
+ *   criticalkv_cache_load   reads rows back into a dense tensor, for another compression step
+ *   criticalkv_decode       attention of one new token per sequence over the pages
+ *
+ * Page ids outside [0, num_pages), row numbers outside the table and lengths outside [0, max_pages * page_size] never
+ * cause an access outside a buffer: such rows are skipped (store, load), treated as absent (decode), lengths are
+ * clipped; with CKV_FLAG_DEBUG_CHECKS the status word then reads CKV_EBOUNDS.
+ */
+typedef enum {
+  CKV_CACHE_PLAIN = 0, /* pages hold rows in the model's element type (dtype)                                   */
+  CKV_CACHE_E4M3 = 1,  /* 8-bit float codes (4 exponent, 3 fraction bits, largest 448), one float32 scale a row   */
+  CKV_CACHE_INT8 = 2   /* 8-bit integer codes in -127..127, one float32 scale a row                               */
+} criticalkv_cache_format;
+/* A quantised row x[0..dh): s = max(max_i |x_i| / top, 2^-100) with top = 448 or 127, r = 1 / s, code_i = x_i * r
+   rounded to nearest even; every operation a separately rounded float32 one (where top * s would overflow, s is the
+   float below).  It stands for code_i * s.  A row that holds an infinity or a NaN gets an infinite or NaN scale and
+   stands for NaN in every element. */
+
+typedef struct {
+  int32_t nseq;          /* sequences, >= 0 (0: the calls do nothing)                                           */
+  int32_t Hq, Hkv;       /* Hq % Hkv == 0, Hkv <= 64                                                            */
+  int32_t dh;            /* head dim: 64 or 128                                                                 */
+  int32_t dtype;         /* criticalkv_dtype of the rows given and returned, of q and of out                    */
+  int32_t format;        /* criticalkv_cache_format of the pages                                                */
+  int32_t page_size;     /* rows a page: 16, 32, 64, 128 or 256                                                 */
+  int32_t num_pages;     /* pages in the pool, >= 1                                                             */
+  int32_t max_pages;     /* columns of the page table, >= 1; a head holds at most max_pages * page_size rows    */
+  uint32_t flags;        /* CKV_FLAG_FORCE_SIMT (criticalkv_decode), CKV_FLAG_DEBUG_CHECKS                      */
+  float scale;           /* logit scale; <= 0 selects 1/sqrt(dh)                                                */
+  uint32_t reserved;     /* must be 0                                                                           */
+  int64_t page_stride;   /* elements of k_pages / v_pages from one page to the next, 0 = page_size * dh         */
+  void* k_pages;         /* [num_pages, page_size, dh] of dtype (plain) or 8-bit codes                          */
+  void* v_pages;
+  float* k_scale;        /* [num_pages, page_size], quantised formats only                                      */
+  float* v_scale;
+  const int32_t* page_table; /* [nseq, Hkv, max_pages]; entries behind a head's last page are never read as pages */
+} criticalkv_cache;
+
+/* Rotary positions.  The first `rot` elements of every row are rot/2 pairs, (x_i, x_{i+rot/2}) in the half layout and
+   (x_{2i}, x_{2i+1}) in the interleaved one; pair i is turned by the angle pos * freq[i] and multiplied by `factor`:
+   (a, b) -> factor * (a cos - b sin, b cos + a sin).  Elements rot..dh-1 are copied.  Angles are reduced in float64,
+   so far positions lose nothing; a negative position turns back. */
+typedef enum { CKV_ROPE_HALF = 0, CKV_ROPE_INTERLEAVED = 1 } criticalkv_rope_layout;
+typedef struct {
+  int32_t nseq, T;       /* sequences and tokens a sequence, >= 0 (0: nothing to do)                            */
+  int32_t Hq, Hk;        /* heads of q (>= 1) and of k (0: no k)                                                */
+  int32_t dh;            /* row length, a multiple of 8, at most 256                                            */
+  int32_t rot;           /* rotated elements, even, 2..dh                                                       */
+  int32_t dtype;         /* criticalkv_dtype of q, k and the outputs                                            */
+  int32_t layout;        /* criticalkv_rope_layout                                                              */
+  float factor;          /* finite; 1 except where a long-context scaling also scales the rotated part          */
+  uint32_t reserved;     /* must be 0                                                                           */
+  /* element strides for the sequence, head and token index; 0 selects the dense default [nseq, H, T, dh] */
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+} criticalkv_rope_desc;
+
+/* q_out = rotated q, k_out = rotated k; pos int32 [nseq, T], freq float64 [rot/2], radians per position.  q_out may be
+   q and k_out may be k (same strides); the buffers must not overlap otherwise. */
+CKV_API int criticalkv_rope(criticalkv_handle h, const criticalkv_rope_desc* d, const void* q, const void* k,
+                            const int32_t* pos, const double* freq, void* q_out, void* k_out, void* stream);
+
+/*
+ * Rows into the cache.  Source rows K, V [nseq, Hkv, n, dh] (element strides for sequence, head and row in `stride`,
+ * NULL or 0 entries = dense).  Which rows of head (s, g) are written, in order, behind row start[s, g]:
+ *   idx == NULL   rows 0..c-1, c = counts[s] (device int32 [nseq]) or n when counts is NULL;
+ *   idx != NULL   rows idx[s, offsets[s,g] .. offsets[s,g+1]), the result of criticalkv_select (idx [nseq, idx_rows],
+ *                 offsets [nseq, Hkv+1]); counts must be NULL.
+ * lens_out[s, g] (may be NULL, may be `start` itself) = start + rows written, at most max_pages * page_size.  Other
+ * rows of the pages keep their contents.  No page may be listed twice among the rows that one call writes.
+ */
+CKV_API int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* c, const void* K, const void* V,
+                                   int32_t n, const int64_t* stride, const int32_t* idx, const int32_t* offsets,
+                                   int64_t idx_rows, const int32_t* counts, const int32_t* start, int32_t* lens_out,
+                                   void* stream);
+
+/*
+ * Rows out of the cache.  K_out, V_out [nseq, Hkv, n, dh] (strides as above).  With align_right == 0 row i of head
+ * (s, g) goes to row i for i < min(lens[s,g], n); with align_right == 1 the last min(lens, n) rows end at row n-1,
+ * the layout that criticalkv_desc.valid_from = n - lens describes.  Other rows of the outputs keep their contents.
+ */
+CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c, const int32_t* lens, int32_t n,
+                                  const int64_t* stride, int32_t align_right, void* K_out, void* V_out, void* stream);
+
+/*
+ * Attention of one new token per sequence: for query head h of sequence s, with g = h / (Hq/Hkv) and the L = lens[s, g]
+ * rows of that KV head, out[s, h, :] = sum_i softmax_i(scale * q . k_i) v_i and lse[s, h] = log sum_i exp(scale * q .
+ * k_i) (lse may be NULL; it is what merging with attention over other keys needs).  A head without rows gives zeros and
+ * -infinity.  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
+ * bf16 queries run on tensor cores (stored 8-bit values enter exactly, sums and the softmax are float32); float32
+ * queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
+ * needs no initialisation; calls that may overlap on the GPU need workspaces of their own.
+ */
+CKV_API int criticalkv_decode_workspace_bytes(const criticalkv_cache* c, size_t* bytes);
+CKV_API int criticalkv_decode(criticalkv_handle h, const criticalkv_cache* c, const void* q, const int64_t* q_stride,
+                              const int32_t* lens, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Self-test of the bounded device-side wait every tensor-core kernel uses: launches one CTA that waits, for at most
  * limit_ns nanoseconds, on a barrier nothing will ever signal.  The kernel must give up, write 0 to *observed_device
  * (a device int; 1 would mean the wait claimed success), set the status word to CKV_ETIMEOUT and end normally.
@@ -290,7 +394,8 @@ CKV_API const char* criticalkv_last_cuda_error(criticalkv_handle h);
 /* Which kernels the last criticalkv_score on this handle launched: bit0 tensor-core window attention,
    bit1 tensor-core projection norm, bit2 CUDA-core window attention, bit3 CUDA-core projection norm,
    bit5: the last criticalkv_select (or
-   criticalkv_select_static) ran as the single kernel; bit6: its two-stage top-k ran with a cluster per head. */
+   criticalkv_select_static) ran as the single kernel; bit6: its two-stage top-k ran with a cluster per head;
+   bit7: the last criticalkv_decode ran on tensor cores, bit8: on CUDA cores. */
 CKV_API int criticalkv_last_path(criticalkv_handle h);
 /* Number of kernel launches this handle has issued since it was created. */
 CKV_API int64_t criticalkv_launch_count(criticalkv_handle h);

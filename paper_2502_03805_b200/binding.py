@@ -25,6 +25,8 @@ CKV_FLAG_SELECT_NO_CLUSTER = 256
 CKV_FLAG_DEBUG_CHECKS = 64
 CKV_FLAG_REQUIRE_TENSOR_CORES = 128
 CKV_EBOUNDS = -7
+CKV_CACHE_PLAIN, CKV_CACHE_E4M3, CKV_CACHE_INT8 = 0, 1, 2
+CKV_ROPE_HALF, CKV_ROPE_INTERLEAVED = 0, 1
 CKV_SELFTEST_MAX_WAIT_NS = 100_000_000
 CKV_STATIC_SCRATCH_BYTES = (8 << 20) + (64 << 10)
 
@@ -32,7 +34,9 @@ EXPORTS = ("criticalkv_create", "criticalkv_destroy", "criticalkv_workspace_byte
            "criticalkv_select", "criticalkv_group_scores", "criticalkv_allocate_budgets",
            "criticalkv_select_static", "criticalkv_compact", "criticalkv_gather_positions", "criticalkv_compress",
            "criticalkv_host_staging_bytes", "criticalkv_compress_host", "criticalkv_selftest_bounded_wait",
-           "criticalkv_diagnose_workspace_bytes", "criticalkv_diagnose", "criticalkv_device_status",
+           "criticalkv_diagnose_workspace_bytes", "criticalkv_diagnose", "criticalkv_rope",
+           "criticalkv_cache_store", "criticalkv_cache_load", "criticalkv_decode_workspace_bytes",
+           "criticalkv_decode", "criticalkv_device_status",
            "criticalkv_status_string", "criticalkv_last_cuda_error", "criticalkv_last_path",
            "criticalkv_launch_count")
 
@@ -45,6 +49,21 @@ class criticalkv_desc(C.Structure):
                 ("flags", C.c_uint32), ("reserved", C.c_uint32),
                 ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
                 ("adaptive_floor", C.c_float), ("reserved2", C.c_uint32), ("valid_from", C.c_void_p)]
+
+
+class criticalkv_cache(C.Structure):
+    _fields_ = [("nseq", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("dh", C.c_int32), ("dtype", C.c_int32),
+                ("format", C.c_int32), ("page_size", C.c_int32), ("num_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("flags", C.c_uint32), ("scale", C.c_float), ("reserved", C.c_uint32), ("page_stride", C.c_int64),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("page_table", C.c_void_p)]
+
+
+class criticalkv_rope_desc(C.Structure):
+    _fields_ = [("nseq", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hk", C.c_int32), ("dh", C.c_int32),
+                ("rot", C.c_int32), ("dtype", C.c_int32), ("layout", C.c_int32), ("factor", C.c_float),
+                ("reserved", C.c_uint32), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3),
+                ("q_out_stride", C.c_int64 * 3), ("k_out_stride", C.c_int64 * 3)]
 
 
 class CriticalKVError(RuntimeError):
@@ -83,6 +102,12 @@ def load():
     lib.criticalkv_compress_host.argtypes = [vp, dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.criticalkv_diagnose_workspace_bytes.argtypes = [dp, C.POINTER(sz)]
     lib.criticalkv_diagnose.argtypes = [vp, dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    cp, rp, i64p = C.POINTER(criticalkv_cache), C.POINTER(criticalkv_rope_desc), C.POINTER(C.c_int64)
+    lib.criticalkv_rope.argtypes = [vp, rp, vp, vp, vp, vp, vp, vp, vp]
+    lib.criticalkv_cache_store.argtypes = [vp, cp, vp, vp, C.c_int32, i64p, vp, vp, C.c_int64, vp, vp, vp, vp]
+    lib.criticalkv_cache_load.argtypes = [vp, cp, vp, C.c_int32, i64p, C.c_int32, vp, vp, vp]
+    lib.criticalkv_decode_workspace_bytes.argtypes = [cp, C.POINTER(sz)]
+    lib.criticalkv_decode.argtypes = [vp, cp, vp, i64p, vp, vp, vp, vp, sz, vp]
     lib.criticalkv_selftest_bounded_wait.argtypes = [vp, C.c_uint64, vp, vp]
     lib.criticalkv_device_status.argtypes = [vp, vp, C.POINTER(i32)]
     lib.criticalkv_status_string.argtypes = [i32]
@@ -261,6 +286,71 @@ def criticalkv_diagnose(handle, desc, Qw, K, V, WO, vnorm, idx, offsets, stage, 
                                     _ptr(idx), _ptr(offsets), _ptr(stage), _ptr(diag), _ptr(ws),
                                     _nbytes(ws, ws_bytes), _stream(stream))
     return _check(handle, rc, "criticalkv_diagnose", check)
+
+
+def make_cache(*, nseq, Hq, Hkv, dh, dtype, format, page_size, num_pages, max_pages, k_pages, v_pages, page_table,
+               k_scale=None, v_scale=None, page_stride=0, scale=0.0, flags=0):
+    """Cache descriptor; the caller keeps the tensors (or addresses) alive while it is in use."""
+    c = criticalkv_cache()
+    c.nseq, c.Hq, c.Hkv, c.dh = nseq, Hq, Hkv, dh
+    c.dtype = {"f32": CKV_F32, "bf16": CKV_BF16}.get(dtype, dtype)
+    c.format = {"plain": CKV_CACHE_PLAIN, "e4m3": CKV_CACHE_E4M3, "int8": CKV_CACHE_INT8}.get(format, format)
+    c.page_size, c.num_pages, c.max_pages, c.page_stride = page_size, num_pages, max_pages, page_stride
+    c.flags, c.scale, c.reserved = flags, scale, 0
+    for name, x in (("k_pages", k_pages), ("v_pages", v_pages), ("k_scale", k_scale), ("v_scale", v_scale),
+                    ("page_table", page_table)):
+        setattr(c, name, x if x is None or isinstance(x, int) else x.data_ptr())
+    return c
+
+
+def make_rope_desc(*, nseq, T, Hq, Hk, dh, rot, dtype, layout, factor=1.0, q_stride=(0, 0, 0), k_stride=(0, 0, 0),
+                   q_out_stride=(0, 0, 0), k_out_stride=(0, 0, 0)):
+    d = criticalkv_rope_desc()
+    d.nseq, d.T, d.Hq, d.Hk, d.dh, d.rot = nseq, T, Hq, Hk, dh, rot
+    d.dtype = {"f32": CKV_F32, "bf16": CKV_BF16}.get(dtype, dtype)
+    d.layout = {"half": CKV_ROPE_HALF, "interleaved": CKV_ROPE_INTERLEAVED}.get(layout, layout)
+    d.factor, d.reserved = factor, 0
+    d.q_stride[:], d.k_stride[:] = q_stride, k_stride
+    d.q_out_stride[:], d.k_out_stride[:] = q_out_stride, k_out_stride
+    return d
+
+
+def _strides(stride):
+    return None if stride is None else (C.c_int64 * len(stride))(*stride)
+
+
+def criticalkv_rope(handle, desc, q, k, pos, freq, q_out, k_out, stream=None, check=True):
+    rc = load().criticalkv_rope(handle, C.byref(desc), _ptr(q), _ptr(k), _ptr(pos), _ptr(freq), _ptr(q_out),
+                                _ptr(k_out), _stream(stream))
+    return _check(handle, rc, "criticalkv_rope", check)
+
+
+def criticalkv_cache_store(handle, cache, K, V, n, stride, idx, offsets, idx_rows, counts, start, lens_out, stream=None,
+                           check=True):
+    rc = load().criticalkv_cache_store(handle, C.byref(cache), _ptr(K), _ptr(V), n, _strides(stride), _ptr(idx),
+                                       _ptr(offsets), idx_rows, _ptr(counts), _ptr(start), _ptr(lens_out),
+                                       _stream(stream))
+    return _check(handle, rc, "criticalkv_cache_store", check)
+
+
+def criticalkv_cache_load(handle, cache, lens, n, stride, align_right, K_out, V_out, stream=None, check=True):
+    rc = load().criticalkv_cache_load(handle, C.byref(cache), _ptr(lens), n, _strides(stride), int(align_right),
+                                      _ptr(K_out), _ptr(V_out), _stream(stream))
+    return _check(handle, rc, "criticalkv_cache_load", check)
+
+
+def criticalkv_decode_workspace_bytes(cache):
+    out = C.c_size_t()
+    rc = load().criticalkv_decode_workspace_bytes(C.byref(cache), C.byref(out))
+    if rc != CKV_OK:
+        raise CriticalKVError(rc, "criticalkv_decode_workspace_bytes")
+    return out.value
+
+
+def criticalkv_decode(handle, cache, q, q_stride, lens, out, lse, ws, ws_bytes=None, stream=None, check=True):
+    rc = load().criticalkv_decode(handle, C.byref(cache), _ptr(q), _strides(q_stride), _ptr(lens), _ptr(out), _ptr(lse),
+                                  _ptr(ws), _nbytes(ws, ws_bytes), _stream(stream))
+    return _check(handle, rc, "criticalkv_decode", check)
 
 
 def criticalkv_selftest_bounded_wait(handle, limit_ns, observed, stream=None, check=True):

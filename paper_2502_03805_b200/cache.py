@@ -1,0 +1,341 @@
+"""Decoding on a compressed cache: rotary positions, the paged cache, and attention of a new token over it.
+
+Device-buffer plumbing around the C ABI, like session.py: shapes, types and devices of tensors are checked here, every
+number is computed by the kernels of libcriticalkv.  Work goes to torch's current stream of the tensors' device unless
+a stream is given.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+import math
+
+import torch
+
+from . import binding as B
+
+_TORCH_DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
+_NAME = {v: k for k, v in _TORCH_DTYPE.items()}
+_CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+class _Owner:
+    """The handle of an object: the caller's, or one of its own that is destroyed with it."""
+
+    def _take_handle(self, handle, device):
+        self._owned = handle is None
+        self.handle = B.criticalkv_create(device.index) if handle is None else handle
+
+    def close(self):
+        if getattr(self, "_owned", False) and self.handle is not None:
+            B.criticalkv_destroy(self.handle)
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _on(self, stream):
+        if stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return stream if isinstance(stream, int) else stream.cuda_stream
+
+    def _allocating(self, stream):
+        """Where outputs of a call on `stream` are allocated and cleared: on that stream, not on the current one."""
+        if stream is None:
+            return contextlib.nullcontext()
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.device)
+        return torch.cuda.stream(stream)
+
+    def _check(self, rc, where):
+        if rc != B.CKV_OK:
+            B._check(self.handle, rc, where, True)
+
+    def device_status(self, stream=None):
+        return B.criticalkv_device_status(self.handle, self._on(stream))
+
+
+def _device_of(t, what):
+    if not t.is_cuda:
+        raise ValueError(f"{what} is not on a CUDA device")
+    return t.device
+
+
+def _need(t, what, shape, dtype, device, dense=True):
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: need {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t
+
+
+def _row_strides(t, what):
+    """Element strides of all but the last dimension for the C ABI (0 = dense): rows must be contiguous, and a
+    dimension repeated with stride 0 cannot be expressed."""
+    if t.is_contiguous():
+        return None
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the elements of a row must be contiguous")
+    out, dense = [], 1
+    for size, step in zip(t.shape[::-1], t.stride()[::-1]):
+        if size > 1 and step == 0:
+            raise ValueError(f"{what}: a dimension expanded with stride 0 is not supported")
+        out.append(step if size > 1 else dense)
+        dense *= max(size, 1)
+    return tuple(out[:0:-1])
+
+
+def rope_frequencies(rot, base=10000.0, scaling=None, *, factor=1.0, original=8192, low=1.0, high=4.0, beta_fast=32.0,
+                     beta_slow=1.0):
+    """Radians per position of the rot/2 pairs, as a float64 CPU tensor: base^(-2i/rot), adjusted for long contexts.
+
+    scaling None     as it is
+    "linear"         every frequency divided by `factor` (positions interpolated)
+    "ntk"            base raised to base * factor^(rot / (rot - 2)): the slowest pair divided by `factor`, the fastest kept
+    "llama3"         wavelengths above original/low divided by `factor`, below original/high kept, blended between
+    "yarn"           pairs turning fewer than beta_slow times over `original` positions divided by `factor`, more than
+                     beta_fast times kept, a linear ramp over the pair index between (its attention factor,
+                     0.1 ln(factor) + 1, is Rotary's `factor` argument)
+    """
+    if rot < 2 or rot % 2:
+        raise ValueError("rot must be even and at least 2")
+    if not (factor >= 1.0 and base > 1.0 and original > 0):
+        raise ValueError("need factor >= 1, base > 1 and original > 0")
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    if scaling == "ntk":
+        if rot == 2:
+            raise ValueError('"ntk" needs rot > 2')
+        base = base * factor ** (rot / (rot - 2))
+    freq = torch.pow(torch.tensor(float(base), dtype=torch.float64), -2.0 * i / rot)
+    if scaling in (None, "ntk"):
+        return freq
+    if scaling == "linear":
+        return freq / factor
+    if scaling == "llama3":
+        if not high > low > 0:
+            raise ValueError("need high > low > 0")
+        turns = original * freq / (2.0 * math.pi)
+        keep = ((turns - low) / (high - low)).clamp(0.0, 1.0)
+    elif scaling == "yarn":
+        if not beta_fast > beta_slow > 0:
+            raise ValueError("need beta_fast > beta_slow > 0")
+
+        def pair(turns):   # the (real-valued) pair index that turns so often over `original` positions
+            return rot * math.log(original / (turns * 2.0 * math.pi)) / (2.0 * math.log(base))
+
+        lo = max(math.floor(pair(beta_fast)), 0)
+        hi = min(math.ceil(pair(beta_slow)), rot - 1)
+        keep = 1.0 - ((i - lo) / max(hi - lo, 0.001)).clamp(0.0, 1.0)
+    else:
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return (1.0 - keep) * freq / factor + keep * freq
+
+
+class Rotary(_Owner):
+    """Rotary positions for heads of dh elements, of which the first 2 * len(frequencies) are turned.
+
+    frequencies: radians per position of each pair (rope_frequencies, or any float64 tensor); layout "half" (pairs
+    i, i + rot/2) or "interleaved" (2i, 2i + 1); factor multiplies the turned part."""
+
+    def __init__(self, *, dh, frequencies, layout="half", factor=1.0, device=None, handle=None):
+        if layout not in ("half", "interleaved"):
+            raise ValueError(f"unknown layout {layout!r}")
+        if frequencies.dtype != torch.float64 or frequencies.dim() != 1:
+            raise ValueError("frequencies must be a float64 vector")
+        self.freq = frequencies.contiguous() if frequencies.is_cuda and device is None else frequencies.to(
+            torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)).contiguous()
+        self.device = _device_of(self.freq, "frequencies")
+        self.dh, self.rot, self.layout, self.factor = dh, 2 * self.freq.numel(), layout, float(factor)
+        self._take_handle(handle, self.device)
+
+    def rotate(self, q, k, positions, q_out=None, k_out=None, stream=None):
+        """q [nseq, Hq, T, dh] and k [nseq, Hk, T, dh] (or None), any strides with contiguous rows; positions int32
+        [nseq, T].  Returns (q_out, k_out); the outputs may be the inputs themselves."""
+        nseq, Hq, T, dh = q.shape
+        if dh != self.dh or q.dtype not in _NAME:
+            raise ValueError(f"q: need rows of {self.dh} float32 or bfloat16 elements")
+        dev = self.device
+        if q.device != dev:
+            raise ValueError(f"q is on {q.device}, not on {dev}")
+        _need(positions, "positions", (nseq, T), torch.int32, dev)
+        Hk = 0
+        if k is not None:
+            Hk = k.shape[1]
+            _need(k, "k", (nseq, Hk, T, dh), q.dtype, dev, dense=False)
+        with self._allocating(stream):
+            if q_out is None:
+                q_out = torch.empty((nseq, Hq, T, dh), dtype=q.dtype, device=dev)
+            if k is not None and k_out is None:
+                k_out = torch.empty((nseq, Hk, T, dh), dtype=q.dtype, device=dev)
+        _need(q_out, "q_out", q.shape, q.dtype, dev, dense=False)
+        if k is not None:
+            _need(k_out, "k_out", k.shape, q.dtype, dev, dense=False)
+        zero = (0, 0, 0)
+        desc = B.make_rope_desc(nseq=nseq, T=T, Hq=Hq, Hk=Hk, dh=dh, rot=self.rot, dtype=_NAME[q.dtype],
+                                layout=self.layout, factor=self.factor, q_stride=_row_strides(q, "q") or zero,
+                                k_stride=(_row_strides(k, "k") if k is not None else None) or zero,
+                                q_out_stride=_row_strides(q_out, "q_out") or zero,
+                                k_out_stride=(_row_strides(k_out, "k_out") if k is not None else None) or zero)
+        self._check(B.load().criticalkv_rope(
+            self.handle, C.byref(desc), q.data_ptr(), k.data_ptr() if k is not None else None, positions.data_ptr(),
+            self.freq.data_ptr(), q_out.data_ptr(), k_out.data_ptr() if k is not None else None, self._on(stream)),
+            "criticalkv_rope")
+        return q_out, k_out
+
+
+class PagedCache(_Owner):
+    """A paged KV cache whose heads have lengths of their own.
+
+    k_pages, v_pages [num_pages, page_size, dh] of the model's type ("plain") or of 8-bit codes ("e4m3": float8_e4m3fn,
+    "int8": int8) with k_scale, v_scale float32 [num_pages, page_size]; page_table int32 [nseq, Hkv, max_pages].  The
+    tensors stay the caller's: lengths are passed to every call, pages are handed out by whoever owns the pool
+    (PagedCache.allocate makes a pool in which every head has all its pages)."""
+
+    def __init__(self, *, Hq, dtype, k_pages, v_pages, page_table, format="plain", k_scale=None, v_scale=None, scale=0.0,
+                 flags=0, handle=None):
+        if dtype not in _TORCH_DTYPE or format not in ("plain", "e4m3", "int8"):
+            raise ValueError(f"unknown dtype {dtype!r} or format {format!r}")
+        if k_pages.dim() != 3 or page_table.dim() != 3:
+            raise ValueError("k_pages must be [num_pages, page_size, dh], page_table [nseq, Hkv, max_pages]")
+        self.dtype, self.format, self.torch_dtype = dtype, format, _TORCH_DTYPE[dtype]
+        dev = self.device = _device_of(k_pages, "k_pages")
+        num_pages, page_size, dh = k_pages.shape
+        code = _CODE.get(format, self.torch_dtype)
+        strides = []
+        for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            _need(t, what, k_pages.shape, code, dev, dense=False)
+            if not t.is_contiguous() and (t.stride(2) != 1 or t.stride(1) != dh):
+                raise ValueError(f"{what}: the rows of a page must be contiguous")
+            strides.append(page_size * dh if t.is_contiguous() else t.stride(0))
+        if strides[0] != strides[1]:
+            raise ValueError("k_pages and v_pages must have the same page stride")
+        if (k_scale is None) != (format == "plain") or (v_scale is None) != (format == "plain"):
+            raise ValueError("k_scale and v_scale go with the quantised formats")
+        if k_scale is not None:
+            _need(k_scale, "k_scale", (num_pages, page_size), torch.float32, dev)
+            _need(v_scale, "v_scale", (num_pages, page_size), torch.float32, dev)
+        nseq, Hkv, max_pages = page_table.shape
+        _need(page_table, "page_table", page_table.shape, torch.int32, dev)
+        self.nseq, self.Hq, self.Hkv, self.dh = nseq, Hq, Hkv, dh
+        self.page_size, self.num_pages, self.max_pages = page_size, num_pages, max_pages
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.page_table = page_table
+        self.desc = B.make_cache(nseq=nseq, Hq=Hq, Hkv=Hkv, dh=dh, dtype=dtype, format=format, page_size=page_size,
+                                 num_pages=num_pages, max_pages=max_pages, k_pages=k_pages, v_pages=v_pages,
+                                 page_table=page_table, k_scale=k_scale, v_scale=v_scale, page_stride=strides[0],
+                                 scale=scale, flags=flags)
+        self._ws_bytes = B.criticalkv_decode_workspace_bytes(self.desc)   # also refuses a bad description
+        self._ws = None
+        self._take_handle(handle, dev)
+
+    @classmethod
+    def allocate(cls, *, nseq, Hq, Hkv, dh, dtype, rows, format="plain", page_size=64, device=0, **kw):
+        """A cache with room for `rows` rows in every head, every page handed out."""
+        dev = torch.device("cuda", device)
+        cols = max(1, -(-rows // page_size))
+        n = max(1, nseq * Hkv * cols)
+        code = _CODE.get(format, _TORCH_DTYPE[dtype])
+        pages = [torch.zeros((n, page_size, dh), dtype=torch.uint8 if code in _CODE.values() else code,
+                             device=dev).view(code) for _ in range(2)]
+        scales = [torch.zeros((n, page_size), dtype=torch.float32, device=dev) if format != "plain" else None
+                  for _ in range(2)]
+        table = torch.arange(nseq * Hkv * cols, dtype=torch.int32, device=dev).view(nseq, Hkv, cols)
+        return cls(Hq=Hq, dtype=dtype, format=format, k_pages=pages[0], v_pages=pages[1], k_scale=scales[0],
+                   v_scale=scales[1], page_table=table, **kw)
+
+    def new_lengths(self):
+        """Lengths of an empty cache."""
+        return torch.zeros((self.nseq, self.Hkv), dtype=torch.int32, device=self.device)
+
+    def store(self, K, V, start, lens_out=None, *, idx=None, offsets=None, counts=None, stream=None):
+        """Writes rows of K, V [nseq, Hkv, n, dh] behind row start[s, g] of every head and returns lens_out, which may
+        be `start` (allocated when None).  All n rows, the first counts[s] of them, or with idx [nseq, idx_rows] and
+        offsets [nseq, Hkv+1] the rows that CompressionSession.select chose."""
+        dev, shape = self.device, (self.nseq, self.Hkv)
+        if K.dim() != 4:
+            raise ValueError("K must be [nseq, Hkv, n, dh]")
+        n = K.shape[2]
+        _need(K, "K", (*shape, n, self.dh), self.torch_dtype, dev, dense=False)
+        _need(V, "V", K.shape, self.torch_dtype, dev, dense=False)
+        strides = _row_strides(K, "K")
+        if strides != _row_strides(V, "V"):
+            raise ValueError("K and V must have the same strides")
+        _need(start, "start", shape, torch.int32, dev)
+        if lens_out is None:
+            with self._allocating(stream):
+                lens_out = torch.empty(shape, dtype=torch.int32, device=dev)
+        _need(lens_out, "lens_out", shape, torch.int32, dev)
+        idx_rows = 0
+        if (idx is None) != (offsets is None):
+            raise ValueError("idx and offsets go together")
+        if idx is not None:
+            if counts is not None:
+                raise ValueError("counts cannot be combined with idx")
+            idx_rows = idx.shape[-1]
+            _need(idx, "idx", (self.nseq, idx_rows), torch.int32, dev)
+            _need(offsets, "offsets", (self.nseq, self.Hkv + 1), torch.int32, dev)
+        if counts is not None:
+            _need(counts, "counts", (self.nseq,), torch.int32, dev)
+        if idx is not None and idx_rows == 0:      # nothing selected: an empty tensor has no address to pass
+            n, idx, offsets = 0, None, None
+        self._check(B.load().criticalkv_cache_store(
+            self.handle, C.byref(self.desc), K.data_ptr(), V.data_ptr(), n, B._strides(strides),
+            idx.data_ptr() if idx is not None else None, offsets.data_ptr() if offsets is not None else None, idx_rows,
+            counts.data_ptr() if counts is not None else None, start.data_ptr(), lens_out.data_ptr(), self._on(stream)),
+            "criticalkv_cache_store")
+        return lens_out
+
+    def load(self, lens, n=None, K_out=None, V_out=None, *, align_right=False, stream=None):
+        """Rows 0..min(lens, n)-1 of every head as K_out, V_out [nseq, Hkv, n, dh] (zeros where there is no row, when
+        allocated here; left as they were in a caller's tensor).  align_right puts the last rows of a head at the end,
+        as the compression step's valid_from = n - lens wants it."""
+        dev = self.device
+        _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, dev)
+        if K_out is None or V_out is None:
+            if n is None or K_out is not None or V_out is not None:
+                raise ValueError("give n, or both K_out and V_out")
+            with self._allocating(stream):
+                K_out = torch.zeros((self.nseq, self.Hkv, n, self.dh), dtype=self.torch_dtype, device=dev)
+                V_out = torch.zeros_like(K_out)
+        if K_out.dim() != 4 or (n is not None and n != K_out.shape[2]):
+            raise ValueError("K_out must be [nseq, Hkv, n, dh]")
+        n = K_out.shape[2]
+        _need(K_out, "K_out", (self.nseq, self.Hkv, n, self.dh), self.torch_dtype, dev, dense=False)
+        _need(V_out, "V_out", K_out.shape, self.torch_dtype, dev, dense=False)
+        strides = _row_strides(K_out, "K_out")
+        if strides != _row_strides(V_out, "V_out"):
+            raise ValueError("K_out and V_out must have the same strides")
+        self._check(B.load().criticalkv_cache_load(
+            self.handle, C.byref(self.desc), lens.data_ptr(), n, B._strides(strides), int(align_right),
+            K_out.data_ptr(), V_out.data_ptr(), self._on(stream)), "criticalkv_cache_load")
+        return K_out, V_out
+
+    def workspace(self):
+        """The decode workspace: allocated on first use and kept.  Calls of this object that may overlap on the GPU
+        (different streams, graphs replayed side by side) need `ws` arguments of their own."""
+        if self._ws is None:
+            self._ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
+        return self._ws
+
+    def attend(self, q, lens, out=None, lse=None, *, ws=None, stream=None):
+        """Attention of one new token per sequence: q [nseq, Hq, dh] over the lens[s, g] rows of every head.  Returns
+        (out [nseq, Hq, dh], lse float32 [nseq, Hq])."""
+        dev, shape = self.device, (self.nseq, self.Hq, self.dh)
+        _need(q, "q", shape, self.torch_dtype, dev, dense=False)
+        _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, dev)
+        with self._allocating(stream):
+            out = torch.empty(shape, dtype=self.torch_dtype, device=dev) if out is None else out
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=dev) if lse is None else lse
+            ws = self.workspace() if ws is None else ws
+        _need(out, "out", shape, self.torch_dtype, dev)
+        _need(lse, "lse", shape[:2], torch.float32, dev)
+        if ws.device != dev or not ws.is_contiguous():
+            raise ValueError(f"ws must be contiguous on {dev}")
+        self._check(B.load().criticalkv_decode(
+            self.handle, C.byref(self.desc), q.data_ptr(), B._strides(_row_strides(q, "q")), lens.data_ptr(),
+            out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), self._on(stream)),
+            "criticalkv_decode")
+        return out, lse

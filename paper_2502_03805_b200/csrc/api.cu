@@ -7,36 +7,15 @@
 #include <mutex>
 #include <new>
 
-#include "ckv_internal.h"
-
-struct criticalkv_handle_s {
-  int device;
-  int sm_count;
-  int cc_major, cc_minor;
-  int* status_word;  // device
-  int smem_optin;
-  int last_path;
-  int last_select_fused;
-  long long launches;
-  char cuda_error[256];
-  // host-staged path: two copy/compute streams and the events that tie them to the caller's stream
-  bool host_ready;
-  cudaStream_t host_stream[2];
-  cudaEvent_t host_event[3];
-};
+#include "handle.h"
 
 namespace {
 
 using ckv::Dims;
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int record_cuda(criticalkv_handle h, cudaError_t e) {
-  if (e == cudaSuccess) return CKV_OK;
-  if (h) snprintf(h->cuda_error, sizeof(h->cuda_error), "%s: %s", cudaGetErrorName(e), cudaGetErrorString(e));
-  return CKV_ECUDA;
-}
+using ckv::DeviceGuard;
+using ckv::align_up;
+using ckv::aligned16;
+using ckv::record_cuda;
 
 // Validates the descriptor and resolves defaults.  Returns CKV_OK or the status to hand back.
 int resolve(const criticalkv_desc* d, Dims* o) {
@@ -148,17 +127,6 @@ SelectLayout select_layout(const Dims& d, bool with_sync = true) {
   L.total = off;
   return L;
 }
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; prev = -1; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-    if (prev == dev) prev = -1;
-  }
-  ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
-};
 
 }  // namespace
 
@@ -695,7 +663,8 @@ const char* criticalkv_status_string(int s) {
 }
 
 const char* criticalkv_last_cuda_error(criticalkv_handle h) { return h ? h->cuda_error : ""; }
-int criticalkv_last_path(criticalkv_handle h) { return h ? (h->last_path | (h->last_select_fused == 1 ? 32 : 0) | (h->last_select_fused == 2 ? 64 : 0)) : 0;
+int criticalkv_last_path(criticalkv_handle h) { return h ? (h->last_path | (h->last_select_fused == 1 ? 32 : 0) | (h->last_select_fused == 2 ? 64 : 0) |
+                      (h->last_decode == 1 ? 128 : 0) | (h->last_decode == 2 ? 256 : 0)) : 0;
 }
 int64_t criticalkv_launch_count(criticalkv_handle h) { return h ? h->launches : 0; }
 

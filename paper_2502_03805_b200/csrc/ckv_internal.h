@@ -118,4 +118,43 @@ cudaError_t launch_two_stage_cluster(const Dims& d, const float* attn, const flo
                                      uint8_t* stage, const SelectDevice& dev, cudaStream_t st, int* launches,
                                      int* status_word);
 
+
+// ---- rotary positions, paged cache, decode ----
+struct RopeDims {
+  int nseq, T, Hq, Hk, dh, rot, dtype, layout;
+  float factor;
+  long long qs[3], ks[3], qos[3], kos[3];   // element strides: sequence, head, token
+};
+struct CacheDims {
+  int nseq, Hq, Hkv, dh, dtype, format, page_shift, num_pages, max_pages;
+  long long page_stride;                    // elements
+  long long capacity;                       // rows a head can hold
+  float scale;
+  int debug_checks;
+  void* k_pages;
+  void* v_pages;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* page_table;
+};
+struct DecodeCall {
+  const void* q;
+  long long q_stride[2];                    // elements: sequence, head
+  const int32_t* lens;
+  void* out;
+  float* lse;
+  void* ws;
+};
+cudaError_t launch_rope(const RopeDims& d, const void* q, const void* k, const int32_t* pos, const double* freq,
+                        void* q_out, void* k_out, int sm_count, cudaStream_t st, int* launches);
+cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V, int n, const long long* stride,
+                               const int32_t* idx, const int32_t* offsets, long long idx_rows, const int32_t* counts,
+                               const int32_t* start, int32_t* lens_out, int* status_word, cudaStream_t st,
+                               int* launches);
+cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right,
+                              void* K_out, void* V_out, int* status_word, cudaStream_t st, int* launches);
+size_t decode_workspace_bytes(const CacheDims& d);
+cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int sm_count, int* status_word,
+                               cudaStream_t st, int* launches);
+
 }  // namespace ckv

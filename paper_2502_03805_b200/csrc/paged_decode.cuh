@@ -1,0 +1,283 @@
+// What the two decode kernels share: how the rows of all heads are spread over CTAs and how partial results are joined.
+//
+// The heads of a compressed cache have different lengths, known only on the device.  Every item (sequence, KV head,
+// chunk of its query heads) is cut into tiles of TILE rows; the tiles of all items in order are one long list, and CTA
+// i of n takes the i-th n-th of it: equal work whatever the lengths are.  A range may end in the middle of an item, so
+// a CTA has at most two incomplete items: the one its range begins inside (partial slot 0) and the one that begins in
+// the range and goes on behind it (slot 1).  Their unnormalised sums with the running maximum and sum go to the
+// workspace; decode_join_kernel adds them up in CTA order, so equal inputs give equal bits.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "paged_common.cuh"
+
+namespace ckv {
+
+constexpr int kDecodeThreads = 128;
+constexpr int kDecodeWarps = kDecodeThreads / 32;
+constexpr int kDecodeMaxCtas = 1024;
+constexpr int kJoinThreads = 256;
+
+struct DecodeArgs {
+  Pages c;
+  const char* q;
+  long long qs[2];             // byte strides: sequence, head
+  const int32_t* lens;
+  char* out;                   // [nseq, Hq, dh] dense
+  float* lse;                  // [nseq, Hq] or null
+  float* part;                 // [CTA][2][rows of an item][dh + 2]: sums, maximum (base 2), sum of weights
+  int2* join;                  // [CTA]: item that ends in this CTA and began in an earlier one (or -1), its first CTA
+  int items, Hq, G;            // G = Hq / Hkv
+  int chunks, chunk_rows;      // query heads of a KV head: chunks of at most chunk_rows
+  float scale_log2;            // scale * log2(e)
+  int* status;
+};
+
+struct ItemRows {   // the query heads of an item
+  int s, head, rows, kv;       // sequence, first query head, number of heads, sequence * Hkv + KV head
+};
+__device__ __forceinline__ ItemRows item_rows(const DecodeArgs& p, int item) {
+  ItemRows r;
+  const int chunk = item % p.chunks;
+  r.kv = item / p.chunks;
+  r.s = r.kv / p.c.Hkv;
+  r.head = (r.kv % p.c.Hkv) * p.G + chunk * p.chunk_rows;
+  r.rows = min(p.chunk_rows, p.G - chunk * p.chunk_rows);
+  return r;
+}
+__device__ __forceinline__ int item_len(const DecodeArgs& p, int kv) {
+  return (int)min(max((long long)p.lens[kv], 0LL), p.c.capacity);
+}
+
+__device__ __forceinline__ float* part_slot(const DecodeArgs& p, int dh, int cta, int slot) {
+  return p.part + ((long long)cta * 2 + slot) * p.chunk_rows * (dh + 2);
+}
+
+// weight of a partial sum with maximum m against the joint maximum (m == -inf: nothing was visible there)
+__device__ __forceinline__ float rescale(float m, float top) { return m == -INFINITY ? 0.f : exp2f(m - top); }
+
+template <typename T> __device__ __forceinline__ void put2(char* at, float a, float b);
+template <> __device__ __forceinline__ void put2<float>(char* at, float a, float b) {
+  *reinterpret_cast<float2*>(at) = make_float2(a, b);
+}
+template <> __device__ __forceinline__ void put2<__nv_bfloat16>(char* at, float a, float b) {
+  *reinterpret_cast<__nv_bfloat162*>(at) = __floats2bfloat162_rn(a, b);
+}
+
+// Elements 2*pair, 2*pair+1 of row r of an item, and its lse (written by pair 0).  An item without rows gives zeros.
+template <typename T, int DH>
+__device__ __forceinline__ void put_out(const DecodeArgs& p, const ItemRows& it, int r, int pair, float a, float b, float m,
+                                        float l, bool empty) {
+  const long long row = (long long)it.s * p.Hq + it.head + r;
+  // l == 0 with rows present (every logit -inf) is 0 / 0, as in the formula
+  if (empty) put2<T>(p.out + (row * DH + 2 * pair) * sizeof(T), 0.f, 0.f);
+  else put2<T>(p.out + (row * DH + 2 * pair) * sizeof(T), a / l, b / l);
+  if (pair == 0 && p.lse != nullptr) p.lse[row] = empty ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// A CTA's range of the tile list, and the walk over the items in it.
+struct Walk {
+  long long begin, end;        // tiles
+  int item;                    // first item
+  long long first;             // its first tile in the list
+  long long total;
+  int ctas;                    // CTAs that have work (all others return)
+};
+
+// Fills the walk (all threads get the same values).  Items without rows are written here, spread over the CTAs.
+template <typename T, int DH, int TILE>
+__device__ __forceinline__ Walk plan(const DecodeArgs& p) {
+  __shared__ int sums[kDecodeThreads];
+  __shared__ int warp_sums[kDecodeWarps];
+  const int tid = threadIdx.x;
+  const int per = (p.items + kDecodeThreads - 1) / kDecodeThreads;
+  const int lo = min(tid * per, p.items), hi = min(lo + per, p.items);
+  int mine = 0;
+  bool bad = false;
+  for (int j = lo; j < hi; ++j) {
+    const int kv = j / p.chunks;
+    const int len = item_len(p, kv);
+    bad = bad || len != p.lens[kv];
+    mine += (len + TILE - 1) / TILE;
+    if (len == 0 && j % gridDim.x == blockIdx.x) {
+      const ItemRows it = item_rows(p, j);
+      for (int r = 0; r < it.rows; ++r)
+        for (int k = 0; k < DH / 2; ++k) put_out<T, DH>(p, it, r, k, 0.f, 0.f, 0.f, 0.f, true);
+    }
+  }
+  if (bad && p.status != nullptr) atomicExch(p.status, (int)CKV_EBOUNDS);
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if ((tid & 31) >= o) incl += v;
+  }
+  if ((tid & 31) == 31) warp_sums[tid >> 5] = incl;
+  __syncthreads();
+  int before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kDecodeWarps; ++w) {
+    if (w < (tid >> 5)) before += warp_sums[w];
+    total += warp_sums[w];
+  }
+  sums[tid] = before + incl;               // tiles of all items up to this thread's last
+  __syncthreads();
+  Walk w;
+  w.total = total;
+  w.ctas = (int)min((long long)gridDim.x, w.total);
+  w.begin = w.end = 0;
+  w.item = 0;
+  w.first = 0;
+  if ((int)blockIdx.x < w.ctas) {
+    w.begin = w.total * blockIdx.x / w.ctas;
+    w.end = w.total * (blockIdx.x + 1) / w.ctas;
+    int a = 0, b = kDecodeThreads - 1;     // first thread whose items reach behind tile `begin`
+    while (a < b) {
+      const int mid = (a + b) / 2;
+      if (sums[mid] > w.begin) b = mid; else a = mid + 1;
+    }
+    w.first = a ? sums[a - 1] : 0;
+    w.item = a * per;
+  }
+  return w;
+}
+
+// CTA whose range holds a tile: the largest i with total * i / ctas <= tile.
+__device__ __forceinline__ int cta_of(const Walk& w, long long tile) { return (int)(((tile + 1) * w.ctas - 1) / w.total); }
+
+// Joins the warps' results of one group of NR rows and hands them on: to the output when the CTA did the whole item,
+// else to the partial slot.  o_s [warp][NR][DH] unnormalised sums, m_s, l_s [warp][NR].  All threads call it, and the
+// buffers may be reused behind the barrier that the caller places.
+template <typename T, int DH, int NR>
+__device__ __forceinline__ void finish(const DecodeArgs& p, const ItemRows& it, const float* o_s, const float* m_s,
+                                       const float* l_s, int row0, bool whole, int slot) {
+  constexpr int PAIRS = DH / 2;
+  for (int i = threadIdx.x; i < NR * PAIRS; i += kDecodeThreads) {
+    const int r = i / PAIRS, k = i % PAIRS;
+    if (row0 + r >= it.rows) break;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kDecodeWarps; ++w) top = fmaxf(top, m_s[w * NR + r]);
+    float a = 0.f, b = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kDecodeWarps; ++w) {
+      const float f = rescale(m_s[w * NR + r], top);
+      const float2 v = *reinterpret_cast<const float2*>(o_s + (w * NR + r) * DH + 2 * k);
+      // a warp that saw no finite logit has weight 0; its sums are 0 as well
+      a += f * v.x;
+      b += f * v.y;
+      l += f * l_s[w * NR + r];
+    }
+    if (whole) {
+      put_out<T, DH>(p, it, row0 + r, k, a, b, top, l, false);
+    } else {
+      float* part = part_slot(p, DH, blockIdx.x, slot) + (row0 + r) * (DH + 2);
+      *reinterpret_cast<float2*>(part + 2 * k) = make_float2(a, b);
+      if (k == 0) *reinterpret_cast<float2*>(part + DH) = make_float2(top, l);
+    }
+  }
+}
+
+// One CTA per (CTA of the decode kernel, row of its item): joins the item that ends in that CTA, if it began in an
+// earlier one.  Warps take the partials in turn, then meet in shared memory: a fixed order of additions.
+template <typename T, int DH>
+__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p) {
+  constexpr int WARPS = kJoinThreads / 32, E = DH / 64;   // pairs of elements a lane
+  __shared__ float o_s[WARPS][DH];
+  __shared__ float m_s[WARPS], l_s[WARPS];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int cta = blockIdx.x;
+  const int2 what = p.join[cta];
+  if (what.x < 0) return;
+  const ItemRows it = item_rows(p, what.x);
+  const int r = blockIdx.y;
+  if (r >= it.rows) return;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  float m = -INFINITY, l = 0.f;
+  float2 acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = make_float2(0.f, 0.f);
+#pragma unroll 2
+  for (int c = what.y + warp; c <= cta; c += WARPS) {
+    const float* part = part_slot(p, DH, c, c == what.y ? 1 : 0) + r * (DH + 2);
+    const float2 ml = *reinterpret_cast<const float2*>(part + DH);
+    float2 v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = *reinterpret_cast<const float2*>(part + 2 * (lane + 32 * e));
+    const float top = fmaxf(m, ml.x);
+    const float f = rescale(m, top), g = rescale(ml.x, top);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      acc[e].x = acc[e].x * f + v[e].x * g;
+      acc[e].y = acc[e].y * f + v[e].y * g;
+    }
+    l = l * f + ml.y * g;
+    m = top;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) *reinterpret_cast<float2*>(&o_s[warp][2 * (lane + 32 * e)]) = acc[e];
+  if (lane == 0) { m_s[warp] = m; l_s[warp] = l; }
+  __syncthreads();
+  if (threadIdx.x < DH / 2) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, m_s[w]);
+    float a = 0.f, b = 0.f;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float f = rescale(m_s[w], top);
+      a += f * o_s[w][2 * threadIdx.x];
+      b += f * o_s[w][2 * threadIdx.x + 1];
+      l += f * l_s[w];
+    }
+    put_out<T, DH>(p, it, r, threadIdx.x, a, b, top, l, false);
+  }
+}
+
+// ---- host side ----------------------------------------------------------------------------------------------------
+inline DecodeArgs decode_args(const CacheDims& d, const DecodeCall& call, int chunk_rows, int* status_word) {
+  const int es = d.dtype == CKV_F32 ? 4 : 2;
+  DecodeArgs p;
+  p.c = pages_of(d);
+  p.q = (const char*)call.q;
+  p.qs[0] = call.q_stride[0] * es;
+  p.qs[1] = call.q_stride[1] * es;
+  p.lens = call.lens;
+  p.out = (char*)call.out;
+  p.lse = call.lse;
+  p.join = (int2*)call.ws;
+  p.part = (float*)((char*)call.ws + kDecodeMaxCtas * sizeof(int2));
+  p.Hq = d.Hq;
+  p.G = d.Hq / d.Hkv;
+  p.chunk_rows = chunk_rows;
+  p.chunks = (p.G + chunk_rows - 1) / chunk_rows;
+  p.items = d.nseq * d.Hkv * p.chunks;
+  p.scale_log2 = d.scale * 1.4426950408889634f;
+  p.status = d.debug_checks ? status_word : nullptr;
+  return p;
+}
+
+// One CTA per resident slot, fewer when even full heads have fewer tiles than that.
+inline int decode_grid(const DecodeArgs& p, int resident, int tile) {
+  const long long tiles = (p.c.capacity + tile - 1) / tile * p.items;
+  long long grid = resident < kDecodeMaxCtas ? resident : kDecodeMaxCtas;
+  if (grid > tiles) grid = tiles;
+  return grid < 1 ? 1 : (int)grid;
+}
+
+// The join may be scheduled while the decode kernel drains; it waits for it before it reads anything.
+template <typename T, int DH> cudaError_t launch_decode_join(const DecodeArgs& p, int grid, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid, (unsigned)(p.G < p.chunk_rows ? p.G : p.chunk_rows));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, DH>, p);
+}
+
+}  // namespace ckv

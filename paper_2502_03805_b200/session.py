@@ -77,6 +77,11 @@ class CompressionSession:
         return B.criticalkv_compact(self.handle, self.desc, K, V, self.idx, self.offsets, self.K_out, self.V_out,
                                     stream=stream)
 
+    def compact_into(self, cache, K, V, start, lens_out=None, stream=None):
+        """Step 5 into a PagedCache (quantised where its format says so) instead of K_out, V_out: the selected rows of
+        K, V go behind row start[b, g] of every head; returns the new lengths."""
+        return cache.store(K, V, start, lens_out, idx=self.idx[:, :self.btot], offsets=self.offsets, stream=stream)
+
     def compress(self, Qw, K, V, WO, budgets_in=None, stream=None):
         return B.criticalkv_compress(self.handle, self.desc, Qw, K, V, WO, budgets_in, self.attn, self.vnorm,
                                      self.idx, self.offsets, self.stage, self.K_out, self.V_out, self.ws,
@@ -148,6 +153,25 @@ class ChunkedPrefillCompressor:
         self.V = s.V_out[0, : s.btot].reshape(self.Hkv, int(budget), self.dh)
         self.pos = pos_out[0, : s.btot].reshape(self.Hkv, int(budget))
         return s
+
+    def to_cache(self, cache, start=None, stream=None):
+        """Writes the retained rows into a PagedCache of one sequence (decoding starts from there) and returns the
+        lengths of its heads."""
+        if self.K is None:
+            raise ValueError("nothing has been compressed yet")
+        start = cache.new_lengths() if start is None else start
+        if self.budget_mode == "uniform":
+            return cache.store(self.K[None], self.V[None], start, stream=stream)
+        # heads of different lengths: one list of rows, head g's part from offsets[g]
+        counts = [int(k.shape[0]) for k in self.K]
+        n = max(max(counts), 1)
+        K = torch.zeros((1, self.Hkv, n, self.dh), dtype=self.K[0].dtype, device=self.device)
+        V = torch.zeros_like(K)
+        for g, c in enumerate(counts):
+            K[0, g, :c], V[0, g, :c] = self.K[g], self.V[g]
+        idx = torch.cat([torch.arange(c, dtype=torch.int32) for c in counts])[None].to(self.device)
+        offsets = torch.tensor([[sum(counts[:g]) for g in range(self.Hkv + 1)]], dtype=torch.int32, device=self.device)
+        return cache.store(K, V, start, idx=idx, offsets=offsets, stream=stream)
 
     def _step_adaptive(self, Qw, K_chunk, V_chunk, WO, budget):
         Hkv, ln = self.Hkv, K_chunk.shape[1]
