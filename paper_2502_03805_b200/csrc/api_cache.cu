@@ -187,8 +187,11 @@ int criticalkv_decode(criticalkv_handle h, const criticalkv_cache* c, const void
   DeviceGuard guard(h->device);
   if (!guard.ok) return CKV_ECUDA;
   int launches = 0;
-  const cudaError_t e = ckv::launch_decode_simt(d, call, h->sm_count, h->status_word, (cudaStream_t)stream, &launches);
-  h->last_decode = 2;
+  // tensor cores would round float32 queries; CKV_FLAG_FORCE_SIMT asks for the CUDA-core kernel
+  const bool mma = d.dtype == CKV_BF16 && !(c->flags & CKV_FLAG_FORCE_SIMT);
+  const cudaError_t e = (mma ? ckv::launch_decode_mma : ckv::launch_decode_simt)(d, call, h->sm_count, h->status_word,
+                                                                                 (cudaStream_t)stream, &launches);
+  h->last_decode = mma ? 1 : 2;
   h->launches += launches;
   return record_cuda(h, e);
 }
