@@ -16,15 +16,35 @@ from . import binding as B
 
 _TORCH_DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
 _NAME = {v: k for k, v in _TORCH_DTYPE.items()}
+_NOTHING = contextlib.nullcontext()
 _CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
 
 
+def _sig(t):
+    """What the checks of a tensor look at (None for an absent one)."""
+    return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
+
+
 class _Owner:
-    """The handle of an object: the caller's, or one of its own that is destroyed with it."""
+    """The handle of an object: the caller's, or one of its own that is destroyed with it.
+
+    A decode step is a handful of microseconds, so a call whose tensors have the types, shapes, strides and devices of
+    an earlier one does not repeat the checks: `_plans` keeps what they came to (strides and descriptors for the C ABI)."""
 
     def _take_handle(self, handle, device):
         self._owned = handle is None
         self.handle = B.criticalkv_create(device.index) if handle is None else handle
+        self._plans = {}
+        self._lib = B.load()
+
+    def _plan(self, key, make, *args):
+        plan = self._plans.get(key)
+        if plan is None:
+            plan = make(*args)
+            if len(self._plans) >= 256:      # prompts of ever new lengths
+                self._plans.clear()
+            self._plans[key] = plan
+        return plan
 
     def close(self):
         if getattr(self, "_owned", False) and self.handle is not None:
@@ -39,20 +59,19 @@ class _Owner:
 
     def _on(self, stream):
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return torch._C._cuda_getCurrentRawStream(self.device.index)
         return stream if isinstance(stream, int) else stream.cuda_stream
 
     def _allocating(self, stream):
         """Where outputs of a call on `stream` are allocated and cleared: on that stream, not on the current one."""
         if stream is None:
-            return contextlib.nullcontext()
+            return _NOTHING
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=self.device)
         return torch.cuda.stream(stream)
 
-    def _check(self, rc, where):
-        if rc != B.CKV_OK:
-            B._check(self.handle, rc, where, True)
+    def _fail(self, rc, where):
+        B._check(self.handle, rc, where, True)
 
     def device_status(self, stream=None):
         return B.criticalkv_device_status(self.handle, self._on(stream))
@@ -154,36 +173,43 @@ class Rotary(_Owner):
     def rotate(self, q, k, positions, q_out=None, k_out=None, stream=None):
         """q [nseq, Hq, T, dh] and k [nseq, Hk, T, dh] (or None), any strides with contiguous rows; positions int32
         [nseq, T].  Returns (q_out, k_out); the outputs may be the inputs themselves."""
+        if q_out is None or (k_out is None and k is not None):
+            with self._allocating(stream):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device) if q_out is None else q_out
+                if k is not None and k_out is None:
+                    k_out = torch.empty(k.shape, dtype=k.dtype, device=self.device)
+        desc = self._plan((_sig(q), _sig(k), _sig(positions), _sig(q_out), _sig(k_out)), self._describe, q, k, positions,
+                          q_out, k_out)
+        rc = self._lib.criticalkv_rope(self.handle, desc, q.data_ptr(), None if k is None else k.data_ptr(),
+                                       positions.data_ptr(), self.freq.data_ptr(), q_out.data_ptr(),
+                                       None if k is None else k_out.data_ptr(), self._on(stream))
+        if rc:
+            self._fail(rc, "criticalkv_rope")
+        return q_out, k_out
+
+    def _describe(self, q, k, positions, q_out, k_out):
+        """Checks the tensors of a call and describes them to the C ABI."""
+        if q.dim() != 4 or q.shape[3] != self.dh or q.dtype not in _NAME:
+            raise ValueError(f"q: need [nseq, Hq, T, {self.dh}] of float32 or bfloat16")
         nseq, Hq, T, dh = q.shape
-        if dh != self.dh or q.dtype not in _NAME:
-            raise ValueError(f"q: need rows of {self.dh} float32 or bfloat16 elements")
         dev = self.device
-        if q.device != dev:
-            raise ValueError(f"q is on {q.device}, not on {dev}")
+        _need(q, "q", q.shape, q.dtype, dev, dense=False)
         _need(positions, "positions", (nseq, T), torch.int32, dev)
-        Hk = 0
+        _need(q_out, "q_out", q.shape, q.dtype, dev, dense=False)
+        zero, Hk, ks, kos = (0, 0, 0), 0, None, None
         if k is not None:
+            if k.dim() != 4:
+                raise ValueError("k must be [nseq, Hk, T, dh]")
             Hk = k.shape[1]
             _need(k, "k", (nseq, Hk, T, dh), q.dtype, dev, dense=False)
-        with self._allocating(stream):
-            if q_out is None:
-                q_out = torch.empty((nseq, Hq, T, dh), dtype=q.dtype, device=dev)
-            if k is not None and k_out is None:
-                k_out = torch.empty((nseq, Hk, T, dh), dtype=q.dtype, device=dev)
-        _need(q_out, "q_out", q.shape, q.dtype, dev, dense=False)
-        if k is not None:
             _need(k_out, "k_out", k.shape, q.dtype, dev, dense=False)
-        zero = (0, 0, 0)
-        desc = B.make_rope_desc(nseq=nseq, T=T, Hq=Hq, Hk=Hk, dh=dh, rot=self.rot, dtype=_NAME[q.dtype],
+            ks, kos = _row_strides(k, "k"), _row_strides(k_out, "k_out")
+        elif k_out is not None:
+            raise ValueError("k_out without k")
+        return B.make_rope_desc(nseq=nseq, T=T, Hq=Hq, Hk=Hk, dh=dh, rot=self.rot, dtype=_NAME[q.dtype],
                                 layout=self.layout, factor=self.factor, q_stride=_row_strides(q, "q") or zero,
-                                k_stride=(_row_strides(k, "k") if k is not None else None) or zero,
-                                q_out_stride=_row_strides(q_out, "q_out") or zero,
-                                k_out_stride=(_row_strides(k_out, "k_out") if k is not None else None) or zero)
-        self._check(B.load().criticalkv_rope(
-            self.handle, C.byref(desc), q.data_ptr(), k.data_ptr() if k is not None else None, positions.data_ptr(),
-            self.freq.data_ptr(), q_out.data_ptr(), k_out.data_ptr() if k is not None else None, self._on(stream)),
-            "criticalkv_rope")
-        return q_out, k_out
+                                k_stride=ks or zero, q_out_stride=_row_strides(q_out, "q_out") or zero,
+                                k_out_stride=kos or zero)
 
 
 class PagedCache(_Owner):
@@ -229,6 +255,8 @@ class PagedCache(_Owner):
                                  scale=scale, flags=flags)
         self._ws_bytes = B.criticalkv_decode_workspace_bytes(self.desc)   # also refuses a bad description
         self._ws = None
+        self._out_shape = (nseq, Hq, dh)
+        self._ref = C.byref(self.desc)
         self._take_handle(handle, dev)
 
     @classmethod
@@ -254,6 +282,23 @@ class PagedCache(_Owner):
         """Writes rows of K, V [nseq, Hkv, n, dh] behind row start[s, g] of every head and returns lens_out, which may
         be `start` (allocated when None).  All n rows, the first counts[s] of them, or with idx [nseq, idx_rows] and
         offsets [nseq, Hkv+1] the rows that CompressionSession.select chose."""
+        if lens_out is None:
+            with self._allocating(stream):
+                lens_out = torch.empty((self.nseq, self.Hkv), dtype=torch.int32, device=self.device)
+        n, idx_rows, strides = self._plan(("store", _sig(K), _sig(V), _sig(start), _sig(lens_out), _sig(idx),
+                                           _sig(offsets), _sig(counts)), self._describe_store, K, V, start, lens_out,
+                                          idx, offsets, counts)
+        if idx_rows == 0:      # no list, or an empty one, whose address could not be passed (n is 0 then)
+            idx = offsets = None
+        rc = self._lib.criticalkv_cache_store(
+            self.handle, self._ref, K.data_ptr(), V.data_ptr(), n, strides, None if idx is None else idx.data_ptr(),
+            None if offsets is None else offsets.data_ptr(), idx_rows, None if counts is None else counts.data_ptr(),
+            start.data_ptr(), lens_out.data_ptr(), self._on(stream))
+        if rc:
+            self._fail(rc, "criticalkv_cache_store")
+        return lens_out
+
+    def _describe_store(self, K, V, start, lens_out, idx, offsets, counts):
         dev, shape = self.device, (self.nseq, self.Hkv)
         if K.dim() != 4:
             raise ValueError("K must be [nseq, Hkv, n, dh]")
@@ -264,9 +309,6 @@ class PagedCache(_Owner):
         if strides != _row_strides(V, "V"):
             raise ValueError("K and V must have the same strides")
         _need(start, "start", shape, torch.int32, dev)
-        if lens_out is None:
-            with self._allocating(stream):
-                lens_out = torch.empty(shape, dtype=torch.int32, device=dev)
         _need(lens_out, "lens_out", shape, torch.int32, dev)
         idx_rows = 0
         if (idx is None) != (offsets is None):
@@ -279,27 +321,29 @@ class PagedCache(_Owner):
             _need(offsets, "offsets", (self.nseq, self.Hkv + 1), torch.int32, dev)
         if counts is not None:
             _need(counts, "counts", (self.nseq,), torch.int32, dev)
-        if idx is not None and idx_rows == 0:      # nothing selected: an empty tensor has no address to pass
-            n, idx, offsets = 0, None, None
-        self._check(B.load().criticalkv_cache_store(
-            self.handle, C.byref(self.desc), K.data_ptr(), V.data_ptr(), n, B._strides(strides),
-            idx.data_ptr() if idx is not None else None, offsets.data_ptr() if offsets is not None else None, idx_rows,
-            counts.data_ptr() if counts is not None else None, start.data_ptr(), lens_out.data_ptr(), self._on(stream)),
-            "criticalkv_cache_store")
-        return lens_out
+        return (0 if idx is not None and idx_rows == 0 else n), idx_rows, B._strides(strides)
 
     def load(self, lens, n=None, K_out=None, V_out=None, *, align_right=False, stream=None):
         """Rows 0..min(lens, n)-1 of every head as K_out, V_out [nseq, Hkv, n, dh] (zeros where there is no row, when
         allocated here; left as they were in a caller's tensor).  align_right puts the last rows of a head at the end,
         as the compression step's valid_from = n - lens wants it."""
-        dev = self.device
-        _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, dev)
         if K_out is None or V_out is None:
             if n is None or K_out is not None or V_out is not None:
                 raise ValueError("give n, or both K_out and V_out")
             with self._allocating(stream):
-                K_out = torch.zeros((self.nseq, self.Hkv, n, self.dh), dtype=self.torch_dtype, device=dev)
+                K_out = torch.zeros((self.nseq, self.Hkv, n, self.dh), dtype=self.torch_dtype, device=self.device)
                 V_out = torch.zeros_like(K_out)
+        n, strides = self._plan(("load", n, _sig(lens), _sig(K_out), _sig(V_out)), self._describe_load, lens, n, K_out,
+                                V_out)
+        rc = self._lib.criticalkv_cache_load(self.handle, self._ref, lens.data_ptr(), n, strides, 1 if align_right else 0,
+                                             K_out.data_ptr(), V_out.data_ptr(), self._on(stream))
+        if rc:
+            self._fail(rc, "criticalkv_cache_load")
+        return K_out, V_out
+
+    def _describe_load(self, lens, n, K_out, V_out):
+        dev = self.device
+        _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, dev)
         if K_out.dim() != 4 or (n is not None and n != K_out.shape[2]):
             raise ValueError("K_out must be [nseq, Hkv, n, dh]")
         n = K_out.shape[2]
@@ -308,10 +352,7 @@ class PagedCache(_Owner):
         strides = _row_strides(K_out, "K_out")
         if strides != _row_strides(V_out, "V_out"):
             raise ValueError("K_out and V_out must have the same strides")
-        self._check(B.load().criticalkv_cache_load(
-            self.handle, C.byref(self.desc), lens.data_ptr(), n, B._strides(strides), int(align_right),
-            K_out.data_ptr(), V_out.data_ptr(), self._on(stream)), "criticalkv_cache_load")
-        return K_out, V_out
+        return n, B._strides(strides)
 
     def workspace(self):
         """The decode workspace: allocated on first use and kept.  Calls of this object that may overlap on the GPU
@@ -323,19 +364,27 @@ class PagedCache(_Owner):
     def attend(self, q, lens, out=None, lse=None, *, ws=None, stream=None):
         """Attention of one new token per sequence: q [nseq, Hq, dh] over the lens[s, g] rows of every head.  Returns
         (out [nseq, Hq, dh], lse float32 [nseq, Hq])."""
-        dev, shape = self.device, (self.nseq, self.Hq, self.dh)
+        if out is None or lse is None or (ws is None and self._ws is None):
+            with self._allocating(stream):
+                out = torch.empty(self._out_shape, dtype=self.torch_dtype, device=self.device) if out is None else out
+                lse = torch.empty(self._out_shape[:2], dtype=torch.float32, device=self.device) if lse is None else lse
+                ws = self.workspace() if ws is None else ws
+        elif ws is None:
+            ws = self._ws
+        strides, size = self._plan(("attend", _sig(q), _sig(lens), _sig(out), _sig(lse), _sig(ws)), self._describe_attend,
+                                   q, lens, out, lse, ws)
+        rc = self._lib.criticalkv_decode(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(),
+                                         lse.data_ptr(), ws.data_ptr(), size, self._on(stream))
+        if rc:
+            self._fail(rc, "criticalkv_decode")
+        return out, lse
+
+    def _describe_attend(self, q, lens, out, lse, ws):
+        dev, shape = self.device, self._out_shape
         _need(q, "q", shape, self.torch_dtype, dev, dense=False)
         _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, dev)
-        with self._allocating(stream):
-            out = torch.empty(shape, dtype=self.torch_dtype, device=dev) if out is None else out
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=dev) if lse is None else lse
-            ws = self.workspace() if ws is None else ws
         _need(out, "out", shape, self.torch_dtype, dev)
         _need(lse, "lse", shape[:2], torch.float32, dev)
         if ws.device != dev or not ws.is_contiguous():
             raise ValueError(f"ws must be contiguous on {dev}")
-        self._check(B.load().criticalkv_decode(
-            self.handle, C.byref(self.desc), q.data_ptr(), B._strides(_row_strides(q, "q")), lens.data_ptr(),
-            out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), self._on(stream)),
-            "criticalkv_decode")
-        return out, lse
+        return B._strides(_row_strides(q, "q")), ws.numel() * ws.element_size()

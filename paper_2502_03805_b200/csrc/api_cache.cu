@@ -40,6 +40,7 @@ int resolve_cache(const criticalkv_cache* c, CacheDims* o) {
   const long long dense = (long long)c->page_size * c->dh;
   o->page_stride = c->page_stride ? c->page_stride : dense;
   if (o->page_stride < dense) return CKV_EINVAL;
+  if (o->page_stride >= (1LL << 38)) return CKV_ENOTSUP;   // a tensor map holds strides below 2^40 bytes
   if (o->page_stride * es % 16) return CKV_EALIGN;
   if (!c->k_pages || !c->v_pages || (c->nseq && !c->page_table)) return CKV_EINVAL;
   if (c->format != CKV_CACHE_PLAIN && (!c->k_scale || !c->v_scale)) return CKV_EINVAL;
@@ -189,7 +190,7 @@ int criticalkv_decode(criticalkv_handle h, const criticalkv_cache* c, const void
   int launches = 0;
   // tensor cores would round float32 queries; CKV_FLAG_FORCE_SIMT asks for the CUDA-core kernel
   const bool mma = d.dtype == CKV_BF16 && !(c->flags & CKV_FLAG_FORCE_SIMT);
-  const cudaError_t e = (mma ? ckv::launch_decode_mma : ckv::launch_decode_simt)(d, call, h->sm_count, h->status_word,
+  const cudaError_t e = (mma ? ckv::launch_decode_mma : ckv::launch_decode_simt)(d, call, h->device, h->sm_count, h->status_word,
                                                                                  (cudaStream_t)stream, &launches);
   h->last_decode = mma ? 1 : 2;
   h->launches += launches;

@@ -154,9 +154,9 @@ cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V,
 cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right,
                               void* K_out, void* V_out, int* status_word, cudaStream_t st, int* launches);
 size_t decode_workspace_bytes(const CacheDims& d);
-cudaError_t launch_decode_mma(const CacheDims& d, const DecodeCall& call, int sm_count, int* status_word, cudaStream_t st,
-                              int* launches);
-cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int sm_count, int* status_word,
+cudaError_t launch_decode_mma(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word,
+                              cudaStream_t st, int* launches);
+cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word,
                                cudaStream_t st, int* launches);
 
 }  // namespace ckv

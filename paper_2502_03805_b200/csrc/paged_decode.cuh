@@ -9,6 +9,8 @@
 #pragma once
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "paged_common.cuh"
 
 namespace ckv {
@@ -30,7 +32,8 @@ struct DecodeArgs {
   int items, Hq, G;            // G = Hq / Hkv
   int chunks, chunk_rows;      // query heads of a KV head: chunks of at most chunk_rows
   float scale_log2;            // scale * log2(e)
-  int* status;
+  int* status;                 // CKV_FLAG_DEBUG_CHECKS: where a violated bound is reported; null otherwise
+  int* timeout;                // where a wait that ran out is reported
 };
 
 struct ItemRows {   // the query heads of an item
@@ -255,8 +258,25 @@ inline DecodeArgs decode_args(const CacheDims& d, const DecodeCall& call, int ch
   p.items = d.nseq * d.Hkv * p.chunks;
   p.scale_log2 = d.scale * 1.4426950408889634f;
   p.status = d.debug_checks ? status_word : nullptr;
+  p.timeout = status_word;
   return p;
 }
+
+// What a kernel needs to know once per device: CTAs an SM holds, and leave for its dynamic shared memory.
+struct LaunchSetup {
+  static constexpr int kDevices = 64;
+  std::atomic<int> per_sm[kDevices] = {};
+  template <typename K> int resident(K kernel, int device, int smem) {
+    int n = device < kDevices ? per_sm[device].load(std::memory_order_acquire) : 0;
+    if (n > 0) return n;
+    if (smem > 48 * 1024 - 2048 &&
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+      return 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kDecodeThreads, smem) != cudaSuccess) return 0;
+    if (device < kDevices) per_sm[device].store(n, std::memory_order_release);
+    return n;
+  }
+};
 
 // One CTA per resident slot, fewer when even full heads have fewer tiles than that.
 inline int decode_grid(const DecodeArgs& p, int resident, int tile) {

@@ -221,22 +221,23 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
   if (threadIdx.x == 0) p.join[blockIdx.x] = join;
 }
 
-template <typename T, int FMT, int DH> cudaError_t launch(DecodeArgs p, int sm_count, cudaStream_t st) {
-  int per_sm = 0;
-  cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, decode_simt_kernel<T, FMT, DH>, kDecodeThreads, 0);
-  if (e != cudaSuccess) return e;
+template <typename T, int FMT, int DH> cudaError_t launch(DecodeArgs p, int device, int sm_count, cudaStream_t st) {
+  static LaunchSetup setup;
+  const int per_sm = setup.resident(decode_simt_kernel<T, FMT, DH>, device, 0);
+  if (per_sm < 1) return cudaErrorInvalidDeviceFunction;
+  cudaError_t e;
   const int grid = decode_grid(p, per_sm * sm_count, kTile);
   decode_simt_kernel<T, FMT, DH><<<grid, kDecodeThreads, 0, st>>>(p);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
   return launch_decode_join<T, DH>(p, grid, st);
 }
 
-template <typename T> cudaError_t by_format(const DecodeArgs& p, int format, int dh, int sm_count, cudaStream_t st) {
+template <typename T> cudaError_t by_format(const DecodeArgs& p, int format, int dh, int device, int sm_count, cudaStream_t st) {
   if (format == CKV_CACHE_PLAIN)
-    return dh == 64 ? launch<T, CKV_CACHE_PLAIN, 64>(p, sm_count, st) : launch<T, CKV_CACHE_PLAIN, 128>(p, sm_count, st);
+    return dh == 64 ? launch<T, CKV_CACHE_PLAIN, 64>(p, device, sm_count, st) : launch<T, CKV_CACHE_PLAIN, 128>(p, device, sm_count, st);
   if (format == CKV_CACHE_E4M3)
-    return dh == 64 ? launch<T, CKV_CACHE_E4M3, 64>(p, sm_count, st) : launch<T, CKV_CACHE_E4M3, 128>(p, sm_count, st);
-  return dh == 64 ? launch<T, CKV_CACHE_INT8, 64>(p, sm_count, st) : launch<T, CKV_CACHE_INT8, 128>(p, sm_count, st);
+    return dh == 64 ? launch<T, CKV_CACHE_E4M3, 64>(p, device, sm_count, st) : launch<T, CKV_CACHE_E4M3, 128>(p, device, sm_count, st);
+  return dh == 64 ? launch<T, CKV_CACHE_INT8, 64>(p, device, sm_count, st) : launch<T, CKV_CACHE_INT8, 128>(p, device, sm_count, st);
 }
 
 }  // namespace
@@ -247,12 +248,12 @@ size_t decode_workspace_bytes(const CacheDims& d) {
   return (kDecodeMaxCtas * (sizeof(int2) + 2 * rows * (d.dh + 2) * sizeof(float)) + 255) / 256 * 256;
 }
 
-cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int sm_count, int* status_word, cudaStream_t st,
+cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word, cudaStream_t st,
                                int* launches) {
   const DecodeArgs p = decode_args(d, call, kQ, status_word);
   *launches += 2;
-  return d.dtype == CKV_F32 ? by_format<float>(p, d.format, d.dh, sm_count, st)
-                            : by_format<__nv_bfloat16>(p, d.format, d.dh, sm_count, st);
+  return d.dtype == CKV_F32 ? by_format<float>(p, d.format, d.dh, device, sm_count, st)
+                            : by_format<__nv_bfloat16>(p, d.format, d.dh, device, sm_count, st);
 }
 
 }  // namespace ckv

@@ -1,9 +1,10 @@
-// Rows into and out of the paged cache.
+// Rows into and out of the paged cache.  Both kernels read and write every row once and are bound by HBM.
 //
-// A row is handled by dh * sizeof(element) / 16 neighbouring lanes, 16 bytes of the model's element type each; the
-// largest magnitude of a row is a shuffle reduction over those lanes, so a row is read once and written once.  Both
-// kernels are bound by HBM; a thread keeps four rows of K and of V in flight (the chain row index -> page id -> row
-// is what a single row would wait for).
+// Store: a row is handled by the fewest lanes that keep its 16-byte pieces coalesced (64 bytes of the row each), because
+// the scale's division and reciprocal are paid once per lane: with 16 bytes a lane the 8-bit formats were bound by
+// arithmetic (8 x 8 heads, 6553 of 32768 rows of 128 bf16 each to e4m3: 101 us; floor 51).  A thread has 64 bytes of K
+// and of V in flight; the chain row index -> page id -> row is covered by the other CTAs of the SM.
+// Load: 16 bytes of output a lane, four rows of K and V in flight.
 #include <cuda_bf16.h>
 
 #include "paged_common.cuh"
@@ -12,7 +13,8 @@ namespace ckv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 4;          // rows of K and V in flight per thread
+constexpr int kRows = 4;          // load: rows of K and V in flight per thread
+constexpr int kPieces = 4;        // store: 16-byte pieces of a row per lane
 
 // (a, b) rounded to two e4m3 codes, a in the low byte.
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
@@ -53,11 +55,11 @@ template <> struct Piece<__nv_bfloat16> {
 
 // Scale and codes of a row piece (criticalkv.h states the rule).  The row's largest magnitude is found on the bit
 // patterns, whose order puts NaN above infinity, so a row with a NaN gets a NaN scale.
-template <int FMT, int LANES, int V>
-__device__ __forceinline__ float quantise(const float (&x)[V], uint32_t (&code)[V / 4]) {
+template <int FMT, int LANES, int N>
+__device__ __forceinline__ float quantise(const float (&x)[N], uint32_t (&code)[N / 4]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
   constexpr float kTop = FMT == CKV_CACHE_E4M3 ? 448.f : 127.f;
@@ -67,7 +69,7 @@ __device__ __forceinline__ float quantise(const float (&x)[V], uint32_t (&code)[
   if (top < 0x7f800000u && __fmul_rn(scale, kTop) == INFINITY) scale = __uint_as_float(__float_as_uint(scale) - 1);
   const float r = __frcp_rn(scale);
 #pragma unroll
-  for (int i = 0; i < V / 4; ++i) {
+  for (int i = 0; i < N / 4; ++i) {
     float y[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = __fmul_rn(x[4 * i + j], r);
@@ -119,9 +121,12 @@ __device__ __forceinline__ int32_t new_length(const StoreArgs& p, int item, int 
   return (int32_t)min(max(m, 0LL), p.c.capacity);
 }
 
+// Lanes that share a row in the store kernel.
+constexpr int store_lanes(int row_bytes) { return row_bytes / (16 * kPieces); }
+
 template <typename T, int FMT, int DH>
 __global__ void __launch_bounds__(kThreads) store_kernel(StoreArgs p) {
-  constexpr int V = Piece<T>::V, LANES = DH / V, RPP = kThreads / LANES;   // rows a pass
+  constexpr int V = Piece<T>::V, LANES = store_lanes(DH * (int)sizeof(T)), ROWS = kThreads / LANES;   // rows a pass
   const int item = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
   const int s = item / p.c.Hkv, g = item % p.c.Hkv;
   const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
@@ -134,55 +139,60 @@ __global__ void __launch_bounds__(kThreads) store_kernel(StoreArgs p) {
     if (chunk == 0 && threadIdx.x == 0) p.lens_out[item] = new_length(p, item, rows);
   }
   const int32_t* pages = p.c.table + (long long)item * p.c.max_pages;
-  const char* src[2] = {p.src[0] + s * p.ss[0] + g * p.ss[1] + lane * 16, p.src[1] + s * p.ss[0] + g * p.ss[1] + lane * 16};
-  const int step = RPP * kRows;
-  for (long long base = (long long)chunk * step; base < rows; base += (long long)p.chunks * step) {
-    long long slot[kRows];                // page * page_size + row in it, or -1
-    int from[kRows];
+  for (long long base = (long long)chunk * ROWS; base < rows; base += (long long)p.chunks * ROWS) {
+    const long long r = base + sub;
+    long long slot = -1;                  // page * page_size + row in it
+    int from = 0;
+    if (r < rows) {
+      from = p.idx != nullptr ? p.idx[(long long)s * p.idx_rows + first + r] : (int)r;
+      const long long to = start + r;
+      if (to >= 0 && to < p.c.capacity && from >= 0 && from < p.n) {
+        const int page = pages[to >> p.c.page_shift];
+        if (page >= 0 && page < p.c.num_pages)
+          slot = ((long long)page << p.c.page_shift) + (to & ((1 << p.c.page_shift) - 1));
+      }
+      bad = bad || slot < 0;
+    }
+    uint4 raw[2][kPieces];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const long long r = base + u * RPP + sub;
-      slot[u] = -1;
-      from[u] = 0;
-      if (r < rows) {
-        from[u] = p.idx != nullptr ? p.idx[(long long)s * p.idx_rows + first + r] : (int)r;
-        const long long to = start + r;
-        if (to >= 0 && to < p.c.capacity && from[u] >= 0 && from[u] < p.n) {
-          const int page = pages[to >> p.c.page_shift];
-          if (page >= 0 && page < p.c.num_pages)
-            slot[u] = ((long long)page << p.c.page_shift) + (to & ((1 << p.c.page_shift) - 1));
-        }
-        bad = bad || slot[u] < 0;
+    for (int w = 0; w < 2; ++w) {
+      const char* src = p.src[w] + s * p.ss[0] + g * p.ss[1] + from * p.ss[2] + lane * 16;
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        raw[w][j] = make_uint4(0, 0, 0, 0);
+        if (slot >= 0) raw[w][j] = *reinterpret_cast<const uint4*>(src + j * LANES * 16);
       }
     }
-    uint4 raw[kRows][2];
+    const long long page_at = (slot >> p.c.page_shift) * p.c.page_stride;
+    const int in_page = (int)(slot & ((1 << p.c.page_shift) - 1));
 #pragma unroll
-    for (int u = 0; u < kRows; ++u)
+    for (int w = 0; w < 2; ++w) {
+      if constexpr (FMT == CKV_CACHE_PLAIN) {
+        char* to = p.c.page[w] + page_at + in_page * (DH * (int)sizeof(T)) + lane * 16;
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        raw[u][w] = make_uint4(0, 0, 0, 0);
-        if (slot[u] >= 0) raw[u][w] = *reinterpret_cast<const uint4*>(src[w] + from[u] * p.ss[2]);
-      }
+        for (int j = 0; j < kPieces; ++j)
+          if (slot >= 0) *reinterpret_cast<uint4*>(to + j * LANES * 16) = raw[w][j];
+      } else {
+        float x[kPieces * V];
+        uint32_t code[kPieces * V / 4];
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) {
+        for (int j = 0; j < kPieces; ++j) {
+          float piece[V];
+          Piece<T>::get(raw[w][j], piece);
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        char* to = p.c.page[w] + (slot[u] >> p.c.page_shift) * p.c.page_stride;
-        const long long in_page = slot[u] & ((1 << p.c.page_shift) - 1);
-        if (FMT == CKV_CACHE_PLAIN) {
-          if (slot[u] >= 0) *reinterpret_cast<uint4*>(to + in_page * (DH * (int)sizeof(T)) + lane * 16) = raw[u][w];
-        } else {
-          float x[V];
-          uint32_t code[V / 4];
-          Piece<T>::get(raw[u][w], x);
-          const float scale = quantise<FMT, LANES, V>(x, code);
-          if (slot[u] >= 0) {
+          for (int i = 0; i < V; ++i) x[V * j + i] = piece[i];
+        }
+        const float scale = quantise<FMT, LANES>(x, code);
+        char* to = p.c.page[w] + page_at + in_page * DH + lane * V;
+        if (slot >= 0) {
+#pragma unroll
+          for (int j = 0; j < kPieces; ++j) {
             if constexpr (V == 8)
-              *reinterpret_cast<uint2*>(to + in_page * DH + lane * 8) = make_uint2(code[0], code[1]);
+              *reinterpret_cast<uint2*>(to + j * LANES * V) = make_uint2(code[2 * j], code[2 * j + 1]);
             else
-              *reinterpret_cast<uint32_t*>(to + in_page * DH + lane * 4) = code[0];
-            if (lane == 0) p.c.scale[w][slot[u]] = scale;
+              *reinterpret_cast<uint32_t*>(to + j * LANES * V) = code[j];
           }
+          if (lane == 0) p.c.scale[w][slot] = scale;
         }
       }
     }
@@ -334,7 +344,7 @@ cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V,
   for (int i = 0; i < 3; ++i) p.ss[i] = stride[i] * es;
   p.n = n; p.idx = idx; p.offsets = offsets; p.idx_rows = idx_rows; p.counts = counts; p.start = start;
   p.status = d.debug_checks ? status_word : nullptr;
-  const int step = kThreads / (d.dh * es / 16) * kRows;
+  const int step = kThreads / store_lanes(d.dh * es);
   p.chunks = chunks_for(idx ? (idx_rows + d.Hkv - 1) / d.Hkv : n, step, items);
   const bool later = lens_out == start && lens_out != nullptr && p.chunks > 1;
   p.lens_out = later ? nullptr : lens_out;

@@ -2,10 +2,9 @@
 // Pair i of a row is turned by pos * freq[i]: (a, b) -> factor * (a cos - b sin, b cos + a sin).
 //
 // The angle is reduced to a fraction of a turn in float64 (pos * freq loses up to pos * 2^-24 radians in float32: 0.008
-// at position 131072) and only then goes to sincospif.  All heads of a token share its rot/2 angles, so a CTA works on
-// a tile of tokens, puts their cosines and sines into shared memory once and then streams the tokens' rows of every
-// head: 16 bytes of a pair's first and second elements per thread, four such units in flight.  Bound by HBM (every
-// row is read and written once).
+// at position 131072) and only then goes to sincospif.  All heads of a token share its rot/2 angles, so a thread owns
+// one unit of one token's rows (16 bytes of a pair's first elements and 16 of its second), keeps the unit's cosines and
+// sines in registers and walks over the heads, four rows in flight.  Bound by HBM: every row is read and written once.
 #include <cuda_bf16.h>
 
 #include "ckv_internal.h"
@@ -14,7 +13,7 @@ namespace ckv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnits = 4;        // units in flight per thread
+constexpr int kRows = 4;         // rows in flight per thread
 
 struct RopeArgs {
   const char* x[2];              // q, k
@@ -23,9 +22,10 @@ struct RopeArgs {
   const int32_t* pos;
   const double* freq;
   float factor;
-  int T, Hq, H, dh, rot;         // H = Hq + Hk
-  int tile, tiles;               // tokens a CTA, CTAs along the tokens of a sequence
-  int heads;                     // heads a CTA
+  int T, heads[2], dh, rot;
+  int units, tile, tiles;        // units a row; tokens a CTA, CTAs along the tokens of a sequence
+  int groups;                    // threads that share a unit of a token and take turns at the heads
+  int splits;                    // CTAs that share a tile of tokens and take turns at the heads
 };
 
 template <typename T> __device__ __forceinline__ float to_f32(T v);
@@ -40,108 +40,85 @@ template <typename T> union Vec16 {
   T e[16 / sizeof(T)];
 };
 
-// What one unit of a row covers: VEC units move 16-byte vectors, the others single elements (row parts that do not
-// divide into vectors).
+// VEC units move 16-byte vectors, the others single elements (row parts that do not divide into vectors).
 template <typename T, bool VEC, bool HALF>
 __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
-  extern __shared__ float table[];              // cos [tile][rot/2], sin [tile][rot/2], both times factor
   constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
+  constexpr int P = (HALF || !VEC) ? V : V / 2;                // pairs a unit
   const int pairs = p.rot / 2;
-  const int s = blockIdx.x / p.tiles, t0 = (blockIdx.x % p.tiles) * p.tile;
-  const int nt = min(p.tile, p.T - t0);
-  const int h0 = blockIdx.y * p.heads, nh = min(p.heads, p.H - h0);
-  float* cosine = table;
-  float* sine = table + p.tile * pairs;
-
-  // units of a row: first the rotated ones, then the copied ones
-  const unsigned turned = (HALF || !VEC) ? pairs / V : p.rot / V;
-  const unsigned units = turned + (p.dh - p.rot) / V;
-  const unsigned total = (unsigned)nh * nt * units;
-
-  auto locate = [&](unsigned i, const char*& src, char*& dst, unsigned& u, int& t) {
-    u = i % units;
-    const unsigned j = i / units;
-    t = (int)(j % (unsigned)nt);
-    int h = h0 + (int)(j / (unsigned)nt);
-    const int which = h >= p.Hq;
-    if (which) h -= p.Hq;
-    src = p.x[which] + s * p.xs[which][0] + h * p.xs[which][1] + (long long)(t0 + t) * p.xs[which][2];
-    dst = p.y[which] + s * p.ys[which][0] + h * p.ys[which][1] + (long long)(t0 + t) * p.ys[which][2];
-  };
-
-  for (int i = threadIdx.x; i < nt * pairs; i += kThreads) {
-    const int t = i / pairs, f = i - t * pairs;
-    const double turns = (double)p.pos[(long long)s * p.T + t0 + t] * (p.freq[f] * 0.15915494309189533577);
-    float sn, cs;
-    sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
-    cosine[t * pairs + f] = cs * p.factor;
-    sine[t * pairs + f] = sn * p.factor;
+  const int turned = pairs / P;                                // units that are turned; the others are copied
+  const int u = threadIdx.x % p.units, rest = threadIdx.x / p.units;
+  const int tok = rest % p.tile, group = rest / p.tile;
+  const int s = blockIdx.x / p.tiles, t = (blockIdx.x % p.tiles) * p.tile + tok;
+  if (group >= p.groups || t >= p.T) return;
+  const bool turn = u < turned;
+  // element offsets of the unit's two parts
+  int ea, eb;
+  if (VEC) {
+    ea = (HALF && !turn ? u + turned : u) * V;
+    eb = HALF ? ea + pairs : ea;
+  } else {
+    ea = turn ? (HALF ? u : 2 * u) : p.rot + u - turned;
+    eb = HALF ? u + pairs : 2 * u + 1;
   }
-  __syncthreads();
-
-  for (unsigned base = threadIdx.x; base < total; base += kThreads * kUnits) {
-    if constexpr (VEC) {
-      Vec16<T> a[kUnits], b[kUnits];
+  float cs[P], sn[P];
+  bool ready = false;
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) {
-        const unsigned i = base + k * kThreads;
-        if (i >= total) break;
-        const char* src; char* dst; unsigned u; int t;
-        locate(i, src, dst, u, t);
-        if (HALF && u < turned) {
-          a[k].raw = *reinterpret_cast<const uint4*>(src + u * 16);
-          b[k].raw = *reinterpret_cast<const uint4*>(src + u * 16 + pairs * sizeof(T));
-        } else {   // copied vectors of the half layout lie behind twice the rotated units
-          a[k].raw = *reinterpret_cast<const uint4*>(src + (HALF ? u + turned : u) * 16);
+  for (int which = 0; which < 2; ++which) {
+    const char* x = p.x[which] + s * p.xs[which][0] + (long long)t * p.xs[which][2];
+    char* y = p.y[which] + s * p.ys[which][0] + (long long)t * p.ys[which][2];
+    const int step = p.groups * p.splits;
+    for (int h = blockIdx.y * p.groups + group; h < p.heads[which]; h += step * kRows) {
+      Vec16<T> a[kRows], b[kRows];
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        const int hk = h + k * step;
+        if (hk < p.heads[which]) {
+          const T* row = reinterpret_cast<const T*>(x + hk * p.xs[which][1]);
+          if (VEC) {
+            a[k].raw = *reinterpret_cast<const uint4*>(row + ea);
+            if (HALF && turn) b[k].raw = *reinterpret_cast<const uint4*>(row + eb);
+          } else {
+            a[k].e[0] = row[ea];
+            if (turn) b[k].e[0] = row[eb];
+          }
+        }
+      }
+      if (!ready) {                                            // behind the first loads
+        ready = true;
+        if (turn) {
+          const double pos = (double)p.pos[(long long)s * p.T + t] * 0.15915494309189533577;
+#pragma unroll
+          for (int i = 0; i < P; ++i) {
+            const double turns = pos * p.freq[u * P + i];
+            sincospif(2.f * (float)(turns - rint(turns)), &sn[i], &cs[i]);
+            cs[i] *= p.factor;
+            sn[i] *= p.factor;
+          }
         }
       }
 #pragma unroll
-      for (int k = 0; k < kUnits; ++k) {
-        const unsigned i = base + k * kThreads;
-        if (i >= total) break;
-        const char* src; char* dst; unsigned u; int t;
-        locate(i, src, dst, u, t);
-        if (u >= turned) {
-          *reinterpret_cast<uint4*>(dst + (HALF ? u + turned : u) * 16) = a[k].raw;
-        } else if (HALF) {
-          const float* cs = cosine + t * pairs + u * V;
-          const float* sn = sine + t * pairs + u * V;
+      for (int k = 0; k < kRows; ++k) {
+        const int hk = h + k * step;
+        if (hk < p.heads[which]) {
+          T* row = reinterpret_cast<T*>(y + hk * p.ys[which][1]);
+          if (turn) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float x = to_f32<T>(a[k].e[e]), y = to_f32<T>(b[k].e[e]);
-            a[k].e[e] = from_f32<T>(x * cs[e] - y * sn[e]);
-            b[k].e[e] = from_f32<T>(y * cs[e] + x * sn[e]);
+            for (int i = 0; i < P; ++i) {
+              T& ta = (VEC && !HALF) ? a[k].e[(2 * i) % (16 / (int)sizeof(T))] : a[k].e[i];
+              T& tb = (VEC && !HALF) ? a[k].e[(2 * i + 1) % (16 / (int)sizeof(T))] : b[k].e[i];
+              const float va = to_f32<T>(ta), vb = to_f32<T>(tb);
+              ta = from_f32<T>(va * cs[i] - vb * sn[i]);
+              tb = from_f32<T>(vb * cs[i] + va * sn[i]);
+            }
           }
-          *reinterpret_cast<uint4*>(dst + u * 16) = a[k].raw;
-          *reinterpret_cast<uint4*>(dst + u * 16 + pairs * sizeof(T)) = b[k].raw;
-        } else {
-          const float* cs = cosine + t * pairs + u * (V / 2);
-          const float* sn = sine + t * pairs + u * (V / 2);
-#pragma unroll
-          for (int e = 0; e < V / 2; ++e) {
-            const float x = to_f32<T>(a[k].e[2 * e]), y = to_f32<T>(a[k].e[2 * e + 1]);
-            a[k].e[2 * e] = from_f32<T>(x * cs[e] - y * sn[e]);
-            a[k].e[2 * e + 1] = from_f32<T>(y * cs[e] + x * sn[e]);
+          if (VEC) {
+            *reinterpret_cast<uint4*>(row + ea) = a[k].raw;
+            if (HALF && turn) *reinterpret_cast<uint4*>(row + eb) = b[k].raw;
+          } else {
+            row[ea] = a[k].e[0];
+            if (turn) row[eb] = b[k].e[0];
           }
-          *reinterpret_cast<uint4*>(dst + u * 16) = a[k].raw;
-        }
-      }
-    } else {
-      for (int k = 0; k < kUnits; ++k) {
-        const unsigned i = base + k * kThreads;
-        if (i >= total) break;
-        const char* src; char* dst; unsigned u; int t;
-        locate(i, src, dst, u, t);
-        const T* xr = reinterpret_cast<const T*>(src);
-        T* yr = reinterpret_cast<T*>(dst);
-        if (u < turned) {
-          const int ia = HALF ? u : 2 * u, ib = HALF ? u + pairs : 2 * u + 1;
-          const float x = to_f32<T>(xr[ia]), y = to_f32<T>(xr[ib]);
-          const float cs = cosine[t * pairs + u], sn = sine[t * pairs + u];
-          yr[ia] = from_f32<T>(x * cs - y * sn);
-          yr[ib] = from_f32<T>(y * cs + x * sn);
-        } else {
-          yr[p.rot + (u - turned)] = xr[p.rot + (u - turned)];
         }
       }
     }
@@ -149,17 +126,31 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
 }
 
 template <typename T>
-cudaError_t launch_typed(const RopeArgs& p, int layout, dim3 grid, size_t smem, cudaStream_t st) {
+cudaError_t launch_typed(RopeArgs p, int layout, int nseq, int sm_count, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(T);
   // whole vectors only where the rotated part (each half of it in the half layout) divides into them
   const bool half = layout == CKV_ROPE_HALF;
   const bool vec = (half ? p.rot / 2 : p.rot) % V == 0;
+  p.units = vec ? (half ? p.rot / 2 : p.rot) / V + (p.dh - p.rot) / V : p.rot / 2 + (p.dh - p.rot);   // at most 256
+  p.tile = kThreads / p.units < p.T ? kThreads / p.units : p.T;
+  p.tiles = (p.T + p.tile - 1) / p.tile;
+  p.groups = kThreads / (p.units * p.tile);
+  const int most = p.heads[0] > p.heads[1] ? p.heads[0] : p.heads[1];
+  if (p.groups > most) p.groups = most;
+  const long long ctas = (long long)p.tiles * nseq;
+  if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
+  // heads are spread over CTAs as well until every SM has eight (each of them computes the tile's angles again), but
+  // not below four rows a thread
+  const int turns = (most + p.groups * kRows - 1) / (p.groups * kRows);
+  p.splits = (int)((8LL * sm_count + ctas - 1) / ctas);
+  if (p.splits > turns) p.splits = turns;
+  const dim3 grid((unsigned)ctas, (unsigned)p.splits);
   if (half) {
-    if (vec) rope_kernel<T, true, true><<<grid, kThreads, smem, st>>>(p);
-    else rope_kernel<T, false, true><<<grid, kThreads, smem, st>>>(p);
+    if (vec) rope_kernel<T, true, true><<<grid, kThreads, 0, st>>>(p);
+    else rope_kernel<T, false, true><<<grid, kThreads, 0, st>>>(p);
   } else {
-    if (vec) rope_kernel<T, true, false><<<grid, kThreads, smem, st>>>(p);
-    else rope_kernel<T, false, false><<<grid, kThreads, smem, st>>>(p);
+    if (vec) rope_kernel<T, true, false><<<grid, kThreads, 0, st>>>(p);
+    else rope_kernel<T, false, false><<<grid, kThreads, 0, st>>>(p);
   }
   return cudaGetLastError();
 }
@@ -177,20 +168,9 @@ cudaError_t launch_rope(const RopeDims& d, const void* q, const void* k, const i
     p.ys[0][i] = d.qos[i] * es; p.ys[1][i] = d.kos[i] * es;
   }
   p.pos = pos; p.freq = freq; p.factor = d.factor;
-  p.T = d.T; p.Hq = d.Hq; p.H = d.Hq + d.Hk; p.dh = d.dh; p.rot = d.rot;
-  p.tile = d.T < 16 ? d.T : 16;
-  p.tiles = (d.T + p.tile - 1) / p.tile;
-  const long long ctas = (long long)p.tiles * d.nseq;
-  if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
-  // few tokens: the heads are spread over CTAs too (each then computes the tile's angles again)
-  long long split = (2LL * sm_count + ctas - 1) / ctas;
-  const int most = (p.H + 3) / 4;       // at least four heads a CTA
-  if (split > most) split = most;
-  p.heads = (int)((p.H + split - 1) / split);
-  const dim3 grid((unsigned)ctas, (unsigned)((p.H + p.heads - 1) / p.heads));
-  const size_t smem = (size_t)p.tile * p.rot * sizeof(float);
-  const cudaError_t e = d.dtype == CKV_F32 ? launch_typed<float>(p, d.layout, grid, smem, st)
-                                           : launch_typed<__nv_bfloat16>(p, d.layout, grid, smem, st);
+  p.T = d.T; p.heads[0] = d.Hq; p.heads[1] = d.Hk; p.dh = d.dh; p.rot = d.rot;
+  const cudaError_t e = d.dtype == CKV_F32 ? launch_typed<float>(p, d.layout, d.nseq, sm_count, st)
+                                           : launch_typed<__nv_bfloat16>(p, d.layout, d.nseq, sm_count, st);
   *launches += 1;
   return e;
 }
