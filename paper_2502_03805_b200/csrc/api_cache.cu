@@ -130,7 +130,7 @@ int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* c, const
   if (!guard.ok) return CKV_ECUDA;
   int launches = 0;
   const cudaError_t e = ckv::launch_cache_store(d, K, V, n, ss, idx, offsets, idx_rows, counts, start, lens_out,
-                                                h->status_word, (cudaStream_t)stream, &launches);
+                                                h->sm_count, h->status_word, (cudaStream_t)stream, &launches);
   h->launches += launches;
   return record_cuda(h, e);
 }

@@ -149,8 +149,8 @@ cudaError_t launch_rope(const RopeDims& d, const void* q, const void* k, const i
                         void* q_out, void* k_out, int sm_count, cudaStream_t st, int* launches);
 cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V, int n, const long long* stride,
                                const int32_t* idx, const int32_t* offsets, long long idx_rows, const int32_t* counts,
-                               const int32_t* start, int32_t* lens_out, int* status_word, cudaStream_t st,
-                               int* launches);
+                               const int32_t* start, int32_t* lens_out, int sm_count, int* status_word,
+                               cudaStream_t st, int* launches);
 cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right,
                               void* K_out, void* V_out, int* status_word, cudaStream_t st, int* launches);
 size_t decode_workspace_bytes(const CacheDims& d);
