@@ -256,8 +256,12 @@ class PagedCache(_Owner):
         self._ws_bytes = B.criticalkv_decode_workspace_bytes(self.desc)   # also refuses a bad description
         self._ws = None
         self._out_shape = (nseq, Hq, dh)
+        # what attend's outputs look like: torch.empty_like costs half of torch.empty with a shape, a type and a device
+        self._out_like = torch.empty(self._out_shape, dtype=self.torch_dtype, device=dev)
+        self._lse_like = torch.empty((nseq, Hq), dtype=torch.float32, device=dev)
         self._ref = C.byref(self.desc)
         self._take_handle(handle, dev)
+        self._decode = self._lib.criticalkv_decode
 
     @classmethod
     def allocate(cls, *, nseq, Hq, Hkv, dh, dtype, rows, format="plain", page_size=64, device=0, **kw):
@@ -364,17 +368,19 @@ class PagedCache(_Owner):
     def attend(self, q, lens, out=None, lse=None, *, ws=None, stream=None):
         """Attention of one new token per sequence: q [nseq, Hq, dh] over the lens[s, g] rows of every head.  Returns
         (out [nseq, Hq, dh], lse float32 [nseq, Hq])."""
-        if out is None or lse is None or (ws is None and self._ws is None):
+        strides, size = self._plan((_sig(q), _sig(lens), _sig(out), _sig(lse), _sig(ws)), self._describe_attend, q, lens,
+                                   out, lse, ws)
+        if stream is None:
+            out = torch.empty_like(self._out_like) if out is None else out
+            lse = torch.empty_like(self._lse_like) if lse is None else lse
+            ws = self.workspace() if ws is None else ws
+        else:
             with self._allocating(stream):
-                out = torch.empty(self._out_shape, dtype=self.torch_dtype, device=self.device) if out is None else out
-                lse = torch.empty(self._out_shape[:2], dtype=torch.float32, device=self.device) if lse is None else lse
+                out = torch.empty_like(self._out_like) if out is None else out
+                lse = torch.empty_like(self._lse_like) if lse is None else lse
                 ws = self.workspace() if ws is None else ws
-        elif ws is None:
-            ws = self._ws
-        strides, size = self._plan(("attend", _sig(q), _sig(lens), _sig(out), _sig(lse), _sig(ws)), self._describe_attend,
-                                   q, lens, out, lse, ws)
-        rc = self._lib.criticalkv_decode(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(),
-                                         lse.data_ptr(), ws.data_ptr(), size, self._on(stream))
+        rc = self._decode(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                          ws.data_ptr(), size, self._on(stream))
         if rc:
             self._fail(rc, "criticalkv_decode")
         return out, lse
@@ -383,8 +389,10 @@ class PagedCache(_Owner):
         dev, shape = self.device, self._out_shape
         _need(q, "q", shape, self.torch_dtype, dev, dense=False)
         _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, dev)
-        _need(out, "out", shape, self.torch_dtype, dev)
-        _need(lse, "lse", shape[:2], torch.float32, dev)
-        if ws.device != dev or not ws.is_contiguous():
+        if out is not None:
+            _need(out, "out", shape, self.torch_dtype, dev)
+        if lse is not None:
+            _need(lse, "lse", shape[:2], torch.float32, dev)
+        if ws is not None and (ws.device != dev or not ws.is_contiguous()):
             raise ValueError(f"ws must be contiguous on {dev}")
-        return B._strides(_row_strides(q, "q")), ws.numel() * ws.element_size()
+        return B._strides(_row_strides(q, "q")), self._ws_bytes if ws is None else ws.numel() * ws.element_size()

@@ -11,6 +11,7 @@
 
 #include <atomic>
 
+#include "launch_early.cuh"
 #include "paged_common.cuh"
 
 namespace ckv {
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p)
   constexpr int WARPS = kJoinThreads / 32, E = DH / 64;   // pairs of elements a lane
   __shared__ float o_s[WARPS][DH];
   __shared__ float m_s[WARPS], l_s[WARPS];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  wait_for_previous_kernel();
   const int cta = blockIdx.x;
   const int2 what = p.join[cta];
   if (what.x < 0) return;
@@ -286,18 +287,10 @@ inline int decode_grid(const DecodeArgs& p, int resident, int tile) {
   return grid < 1 ? 1 : (int)grid;
 }
 
-// The join may be scheduled while the decode kernel drains; it waits for it before it reads anything.
 template <typename T, int DH> cudaError_t launch_decode_join(const DecodeArgs& p, int grid, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid, (unsigned)(p.G < p.chunk_rows ? p.G : p.chunk_rows));
-  cfg.blockDim = dim3(kJoinThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, decode_join_kernel<T, DH>, p);
+  return launch_early<DecodeArgs>(decode_join_kernel<T, DH>,
+                                  dim3((unsigned)grid, (unsigned)(p.G < p.chunk_rows ? p.G : p.chunk_rows)), kJoinThreads, 0,
+                                  st, p);
 }
 
 }  // namespace ckv

@@ -150,8 +150,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
     ptx::prefetch_tensormap(&v_map);
   }
   ptx::fence_barrier_init();
+  wait_for_previous_kernel();
   const Walk walk = plan<T, DH, S::kTile>(p);              // contains barriers: the mbarriers are visible behind it
-  asm volatile("griddepcontrol.launch_dependents;");
 
   // The segment behind `g` (its item, first and tiles), or one with t0 == t1.
   auto following = [&](Segment g) {
@@ -668,8 +668,8 @@ template <int FMT, int DH, int NT> cudaError_t launch(const DecodeArgs& p, int d
   for (int i = 0; i < 2; ++i)
     if (!page_map<Shape<FMT, DH, NT>>(&maps[i], p, i, min(1 << p.c.page_shift, 16 * Shape<FMT, DH, NT>::kSub))) return cudaErrorInvalidValue;
   const int grid = decode_grid(p, per_sm * sm_count, Shape<FMT, DH, NT>::kTile);
-  kernel<<<grid, kDecodeThreads, smem, st>>>(p, maps[0], maps[1]);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_early<DecodeArgs, CUtensorMap, CUtensorMap>(kernel, dim3(grid), kDecodeThreads, smem, st, p,
+                                                                           maps[0], maps[1]);
   if (e != cudaSuccess) return e;
   return launch_decode_join<__nv_bfloat16, DH>(p, grid, st);
 }

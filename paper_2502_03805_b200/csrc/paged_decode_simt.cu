@@ -61,10 +61,10 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
   constexpr int ROW_BYTES = DH * (FMT == CKV_CACHE_PLAIN ? (int)sizeof(T) : 1);
   constexpr int PIECES = DH / 16;               // pieces of four elements a quad lane has of a row
   constexpr int LPR = DH / 4, KPI = 32 / LPR;   // values: lanes a row, rows at a time
-  __shared__ Shared<T, FMT, DH> sh;
+  __shared__ __align__(16) Shared<T, FMT, DH> sh;      // read and written 16 bytes at a time
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  wait_for_previous_kernel();
   const Walk walk = plan<T, DH, kTile>(p);
-  asm volatile("griddepcontrol.launch_dependents;");
   int2 join = make_int2(-1, 0);
   long long first = walk.first, t = walk.begin;
   for (int item = walk.item; t < walk.end; ++item) {
@@ -227,8 +227,8 @@ template <typename T, int FMT, int DH> cudaError_t launch(DecodeArgs p, int devi
   if (per_sm < 1) return cudaErrorInvalidDeviceFunction;
   cudaError_t e;
   const int grid = decode_grid(p, per_sm * sm_count, kTile);
-  decode_simt_kernel<T, FMT, DH><<<grid, kDecodeThreads, 0, st>>>(p);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  e = launch_early<DecodeArgs>(decode_simt_kernel<T, FMT, DH>, dim3(grid), kDecodeThreads, 0, st, p);
+  if (e != cudaSuccess) return e;
   return launch_decode_join<T, DH>(p, grid, st);
 }
 

@@ -7,6 +7,7 @@
 // Load: 16 bytes of output a lane, four rows of K and V in flight.
 #include <cuda_bf16.h>
 
+#include "launch_early.cuh"
 #include "paged_common.cuh"
 
 namespace ckv {
@@ -127,6 +128,7 @@ constexpr int store_lanes(int row_bytes) { return row_bytes / (16 * kPieces); }
 
 template <typename T, int FMT, int DH>
 __global__ void __launch_bounds__(kStoreThreads, kStoreCtas) store_kernel(StoreArgs p) {
+  wait_for_previous_kernel();
   constexpr int V = Piece<T>::V, LANES = store_lanes(DH * (int)sizeof(T)), ROWS = kStoreThreads / LANES;   // rows a pass
   const int item = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
   const int s = item / p.c.Hkv, g = item % p.c.Hkv;
@@ -214,6 +216,7 @@ __global__ void __launch_bounds__(kStoreThreads, kStoreCtas) store_kernel(StoreA
 
 // lens_out = start + rows where several CTAs read start and lens_out is start itself.
 __global__ void store_lengths_kernel(StoreArgs p, int items) {
+  wait_for_previous_kernel();
   const int item = blockIdx.x * blockDim.x + threadIdx.x;
   if (item >= items) return;
   long long first;
@@ -235,6 +238,7 @@ struct LoadArgs {
 
 template <typename T, int FMT, int DH>
 __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
+  wait_for_previous_kernel();
   constexpr int V = Piece<T>::V, LANES = DH / V, RPP = kThreads / LANES;
   const int item = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
   const int s = item / p.c.Hkv, g = item % p.c.Hkv;
@@ -364,17 +368,16 @@ cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V,
   if (p.chunks > most) p.chunks = most < 1 ? 1 : (int)most;
   const bool later = lens_out == start && lens_out != nullptr && p.chunks > 1;
   p.lens_out = later ? nullptr : lens_out;
+  cudaError_t e = cudaSuccess;
   by_type(d, [&](auto t, auto fmt, auto dh) {
-    store_kernel<decltype(t), decltype(fmt)::value, decltype(dh)::value>
-        <<<(unsigned)(items * p.chunks), kStoreThreads, 0, st>>>(p);
+    e = launch_early<StoreArgs>(store_kernel<decltype(t), decltype(fmt)::value, decltype(dh)::value>,
+                                dim3((unsigned)(items * p.chunks)), kStoreThreads, 0, st, p);
   });
   *launches += 1;
-  cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || !later) return e;
   p.lens_out = lens_out;
-  store_lengths_kernel<<<(unsigned)((items + 127) / 128), 128, 0, st>>>(p, (int)items);
   *launches += 1;
-  return cudaGetLastError();
+  return launch_early<StoreArgs, int>(store_lengths_kernel, dim3((unsigned)((items + 127) / 128)), 128, 0, st, p, (int)items);
 }
 
 cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right,
@@ -390,12 +393,13 @@ cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, co
   p.status = d.debug_checks ? status_word : nullptr;
   const int step = kThreads / (d.dh * es / 16) * kRows;
   p.chunks = chunks_for(n, step, items);
+  cudaError_t e = cudaSuccess;
   by_type(d, [&](auto t, auto fmt, auto dh) {
-    load_kernel<decltype(t), decltype(fmt)::value, decltype(dh)::value>
-        <<<(unsigned)(items * p.chunks), kThreads, 0, st>>>(p);
+    e = launch_early<LoadArgs>(load_kernel<decltype(t), decltype(fmt)::value, decltype(dh)::value>,
+                               dim3((unsigned)(items * p.chunks)), kThreads, 0, st, p);
   });
   *launches += 1;
-  return cudaGetLastError();
+  return e;
 }
 
 }  // namespace ckv

@@ -9,6 +9,7 @@
 #include <cuda_bf16.h>
 
 #include "ckv_internal.h"
+#include "launch_early.cuh"
 
 namespace ckv {
 namespace {
@@ -44,6 +45,7 @@ template <typename T> union Vec16 {
 // VEC units move 16-byte vectors, the others single elements (row parts that do not divide into vectors).
 template <typename T, bool VEC, bool HALF>
 __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs p) {
+  wait_for_previous_kernel();
   constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
   constexpr int P = (HALF || !VEC) ? V : V / 2;                // pairs a unit
   const int pairs = p.rot / 2;
@@ -146,14 +148,9 @@ cudaError_t launch_typed(RopeArgs p, int layout, int nseq, int sm_count, cudaStr
   p.splits = (int)((8LL * sm_count + ctas - 1) / ctas);
   if (p.splits > turns) p.splits = turns;
   const dim3 grid((unsigned)ctas, (unsigned)p.splits);
-  if (half) {
-    if (vec) rope_kernel<T, true, true><<<grid, kThreads, 0, st>>>(p);
-    else rope_kernel<T, false, true><<<grid, kThreads, 0, st>>>(p);
-  } else {
-    if (vec) rope_kernel<T, true, false><<<grid, kThreads, 0, st>>>(p);
-    else rope_kernel<T, false, false><<<grid, kThreads, 0, st>>>(p);
-  }
-  return cudaGetLastError();
+  const auto kernel = half ? (vec ? rope_kernel<T, true, true> : rope_kernel<T, false, true>)
+                           : (vec ? rope_kernel<T, true, false> : rope_kernel<T, false, false>);
+  return launch_early<RopeArgs>(kernel, grid, kThreads, 0, st, p);
 }
 
 }  // namespace

@@ -422,6 +422,16 @@ def test_decode(dtype, fmt, dh, G, Hkv, nseq, page, lens):
 
 
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "plain"), ("bf16", "e4m3"), ("f32", "int8"), ("f32", "plain")])
+@pytest.mark.parametrize("G", [1, 2, 3])
+def test_decode_of_one_long_head(dtype, fmt, G):
+    """All CTAs work on one KV head."""
+    lens = torch.full((1, 1), 30011, dtype=torch.int32)
+    cache = Cache(nseq=1, Hq=G, Hkv=1, dh=64, dtype=dtype, fmt=fmt, page=128, cols=235).fill(lens, 3)
+    q = torch.randn(1, G, 64, generator=gen(8)).to(R.DT[dtype])
+    check_decode(cache, q, lens, cache.c.attend(q.cuda(), lens.cuda()))
+
+
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "plain"), ("bf16", "e4m3"), ("f32", "int8"), ("f32", "plain")])
 def test_decode_of_few_long_heads(dtype, fmt):
     """One long head next to short and empty ones: the long one is split over most CTAs and joined."""
     lens = torch.tensor([[20011, 3], [0, 1]], dtype=torch.int32)
