@@ -366,7 +366,8 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
  * k_i) (lse may be NULL; it is what merging with attention over other keys needs).  A head without rows gives zeros and
  * -infinity.  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
  * bf16 queries run on tensor cores (stored 8-bit values enter exactly, sums and the softmax are float32); float32
- * queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
+ * queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores.  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) * ceil(max_pages *
+ * page_size / 64) exceeds 2^31 - 1.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
  * needs no initialisation; calls that may overlap on the GPU need workspaces of their own.
  */
 CKV_API int criticalkv_decode_workspace_bytes(const criticalkv_cache* c, size_t* bytes);

@@ -179,6 +179,8 @@ int criticalkv_decode(criticalkv_handle h, const criticalkv_cache* c, const void
     if (call.q_stride[i] < 0) return CKV_EINVAL;
     if (call.q_stride[i] % vec) return CKV_EALIGN;
   }
+  // the list of 64-row tiles of all heads is counted in 32 bits
+  if ((long long)d.nseq * d.Hkv * ((d.Hq / d.Hkv + 7) / 8) > 0x7fffffffLL / ((d.capacity + 63) / 64)) return CKV_ENOTSUP;
   if (d.nseq == 0) return CKV_OK;
   if (!q || !lens || !out || !ws) return CKV_EINVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned_to(lens, 4) || !aligned_to(lse, 4) || !aligned_to(ws, 256))

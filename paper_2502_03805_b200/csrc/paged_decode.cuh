@@ -18,7 +18,7 @@ namespace ckv {
 
 constexpr int kDecodeThreads = 128;
 constexpr int kDecodeWarps = kDecodeThreads / 32;
-constexpr int kDecodeMaxCtas = 1024;
+constexpr int kDecodeMaxCtas = 592;      // four a multiprocessor on 148
 constexpr int kJoinThreads = 256;
 
 struct DecodeArgs {
@@ -32,6 +32,7 @@ struct DecodeArgs {
   int2* join;                  // [CTA]: item that ends in this CTA and began in an earlier one (or -1), its first CTA
   int items, Hq, G;            // G = Hq / Hkv
   int chunks, chunk_rows;      // query heads of a KV head: chunks of at most chunk_rows
+  int part_rows;               // the most query heads an item has
   float scale_log2;            // scale * log2(e)
   int* status;                 // CKV_FLAG_DEBUG_CHECKS: where a violated bound is reported; null otherwise
   int* timeout;                // where a wait that ran out is reported
@@ -54,7 +55,7 @@ __device__ __forceinline__ int item_len(const DecodeArgs& p, int kv) {
 }
 
 __device__ __forceinline__ float* part_slot(const DecodeArgs& p, int dh, int cta, int slot) {
-  return p.part + ((long long)cta * 2 + slot) * p.chunk_rows * (dh + 2);
+  return p.part + ((long long)cta * 2 + slot) * p.part_rows * (dh + 2);
 }
 
 // weight of a partial sum with maximum m against the joint maximum (m == -inf: nothing was visible there)
@@ -91,26 +92,30 @@ struct Walk {
 // Fills the walk (all threads get the same values).  Items without rows are written here, spread over the CTAs.
 template <typename T, int DH, int TILE>
 __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
-  __shared__ int sums[kDecodeThreads];
-  __shared__ int warp_sums[kDecodeWarps];
+  __shared__ int upto[kDecodeThreads];                     // tiles of all items up to a thread's last (the host has
+  __shared__ int warp_sums[kDecodeWarps];                  // checked that they fit)
   const int tid = threadIdx.x;
   const int per = (p.items + kDecodeThreads - 1) / kDecodeThreads;
   const int lo = min(tid * per, p.items), hi = min(lo + per, p.items);
-  int mine = 0;
-  bool bad = false;
+  int incl = 0;
+  bool bad = false, empty = false;
+#pragma unroll 4
   for (int j = lo; j < hi; ++j) {
-    const int kv = j / p.chunks;
-    const int len = item_len(p, kv);
-    bad = bad || len != p.lens[kv];
-    mine += (len + TILE - 1) / TILE;
-    if (len == 0 && j % gridDim.x == blockIdx.x) {
-      const ItemRows it = item_rows(p, j);
-      for (int r = 0; r < it.rows; ++r)
-        for (int k = 0; k < DH / 2; ++k) put_out<T, DH>(p, it, r, k, 0.f, 0.f, 0.f, 0.f, true);
-    }
+    const int given = __ldg(p.lens + j / p.chunks);
+    const int len = (int)min(max((long long)given, 0LL), p.c.capacity);
+    bad = bad || len != given;
+    empty = empty || len == 0;
+    incl += (len + TILE - 1) / TILE;
   }
   if (bad && p.status != nullptr) atomicExch(p.status, (int)CKV_EBOUNDS);
-  int incl = mine;
+  if (empty) {
+    for (int j = lo; j < hi; ++j)
+      if (item_len(p, j / p.chunks) == 0 && j % gridDim.x == blockIdx.x) {
+        const ItemRows it = item_rows(p, j);
+        for (int r = 0; r < it.rows; ++r)
+          for (int k = 0; k < DH / 2; ++k) put_out<T, DH>(p, it, r, k, 0.f, 0.f, 0.f, 0.f, true);
+      }
+  }
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int v = __shfl_up_sync(0xffffffffu, incl, o);
@@ -118,13 +123,13 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
   }
   if ((tid & 31) == 31) warp_sums[tid >> 5] = incl;
   __syncthreads();
-  int before = 0, total = 0;
+  int total = 0;
 #pragma unroll
   for (int w = 0; w < kDecodeWarps; ++w) {
-    if (w < (tid >> 5)) before += warp_sums[w];
+    if (w < (tid >> 5)) incl += warp_sums[w];
     total += warp_sums[w];
   }
-  sums[tid] = before + incl;               // tiles of all items up to this thread's last
+  upto[tid] = incl;
   __syncthreads();
   Walk w;
   w.total = total;
@@ -138,9 +143,9 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
     int a = 0, b = kDecodeThreads - 1;     // first thread whose items reach behind tile `begin`
     while (a < b) {
       const int mid = (a + b) / 2;
-      if (sums[mid] > w.begin) b = mid; else a = mid + 1;
+      if (upto[mid] > w.begin) b = mid; else a = mid + 1;
     }
-    w.first = a ? sums[a - 1] : 0;
+    w.first = a ? upto[a - 1] : 0;
     w.item = a * per;
   }
   return w;
@@ -182,42 +187,68 @@ __device__ __forceinline__ void finish(const DecodeArgs& p, const ItemRows& it, 
   }
 }
 
+// Adds up a row's parts of CTAs c, c + step, ... <= c1 of an item that began in CTA c0 (in slot 1 there): four parts'
+// loads are in flight before the first is looked at, for most calls all there are.
+template <int DH>
+__device__ __forceinline__ void add_parts(const DecodeArgs& p, int r, int c0, int c1, int c, int step, float& m, float& l,
+                                          float2 (&acc)[DH / 64]) {
+  constexpr int FLY = 4, E = DH / 64;
+  m = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = make_float2(0.f, 0.f);
+  for (; c <= c1; c += FLY * step) {
+    float2 ml[FLY], v[FLY][E];
+#pragma unroll
+    for (int i = 0; i < FLY; ++i) {
+      const int ci = c + i * step;
+      ml[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[i][e] = make_float2(0.f, 0.f);
+      if (ci <= c1) {
+        const float* part = part_slot(p, DH, ci, ci == c0 ? 1 : 0) + r * (DH + 2);
+        ml[i] = *reinterpret_cast<const float2*>(part + DH);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[i][e] = *reinterpret_cast<const float2*>(part + 2 * (threadIdx.x % 32 + 32 * e));
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < FLY; ++i) top = fmaxf(top, ml[i].x);
+    const float f = rescale(m, top);
+    m = top;
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) { acc[e].x *= f; acc[e].y *= f; }
+#pragma unroll
+    for (int i = 0; i < FLY; ++i) {
+      const float g = rescale(ml[i].x, top);
+      l += ml[i].y * g;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        acc[e].x += v[i][e].x * g;
+        acc[e].y += v[i][e].y * g;
+      }
+    }
+  }
+}
+
 // One CTA per (CTA of the decode kernel, row of its item): joins the item that ends in that CTA, if it began in an
-// earlier one.  Warps take the partials in turn, then meet in shared memory: a fixed order of additions.
+// earlier one.  Warps take the parts in turn, then meet in shared memory: a fixed order of additions.
 template <typename T, int DH>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p) {
   constexpr int WARPS = kJoinThreads / 32, E = DH / 64;   // pairs of elements a lane
-  __shared__ float o_s[WARPS][DH];
+  __shared__ __align__(8) float o_s[WARPS][DH];
   __shared__ float m_s[WARPS], l_s[WARPS];
   wait_for_previous_kernel();
-  const int cta = blockIdx.x;
-  const int2 what = p.join[cta];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = blockIdx.y;
+  const int2 what = p.join[blockIdx.x];
   if (what.x < 0) return;
   const ItemRows it = item_rows(p, what.x);
-  const int r = blockIdx.y;
   if (r >= it.rows) return;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  float m = -INFINITY, l = 0.f;
+  float m, l;
   float2 acc[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = make_float2(0.f, 0.f);
-#pragma unroll 2
-  for (int c = what.y + warp; c <= cta; c += WARPS) {
-    const float* part = part_slot(p, DH, c, c == what.y ? 1 : 0) + r * (DH + 2);
-    const float2 ml = *reinterpret_cast<const float2*>(part + DH);
-    float2 v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = *reinterpret_cast<const float2*>(part + 2 * (lane + 32 * e));
-    const float top = fmaxf(m, ml.x);
-    const float f = rescale(m, top), g = rescale(ml.x, top);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      acc[e].x = acc[e].x * f + v[e].x * g;
-      acc[e].y = acc[e].y * f + v[e].y * g;
-    }
-    l = l * f + ml.y * g;
-    m = top;
-  }
+  add_parts<DH>(p, r, what.y, blockIdx.x, what.y + warp, WARPS, m, l, acc);
 #pragma unroll
   for (int e = 0; e < E; ++e) *reinterpret_cast<float2*>(&o_s[warp][2 * (lane + 32 * e)]) = acc[e];
   if (lane == 0) { m_s[warp] = m; l_s[warp] = l; }
@@ -256,6 +287,7 @@ inline DecodeArgs decode_args(const CacheDims& d, const DecodeCall& call, int ch
   p.G = d.Hq / d.Hkv;
   p.chunk_rows = chunk_rows;
   p.chunks = (p.G + chunk_rows - 1) / chunk_rows;
+  p.part_rows = p.G < chunk_rows ? p.G : chunk_rows;
   p.items = d.nseq * d.Hkv * p.chunks;
   p.scale_log2 = d.scale * 1.4426950408889634f;
   p.status = d.debug_checks ? status_word : nullptr;
@@ -289,7 +321,7 @@ inline int decode_grid(const DecodeArgs& p, int resident, int tile) {
 
 template <typename T, int DH> cudaError_t launch_decode_join(const DecodeArgs& p, int grid, cudaStream_t st) {
   return launch_early<DecodeArgs>(decode_join_kernel<T, DH>,
-                                  dim3((unsigned)grid, (unsigned)(p.G < p.chunk_rows ? p.G : p.chunk_rows)), kJoinThreads, 0,
+                                  dim3((unsigned)grid, (unsigned)p.part_rows), kJoinThreads, 0,
                                   st, p);
 }
 

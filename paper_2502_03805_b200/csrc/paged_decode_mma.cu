@@ -635,7 +635,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
   if (!ok) {
     // a copy did not arrive in time: report it, and give what is still on its way a last chance before the CTA (and
     // with it the shared memory the copies write) goes away
-    if (threadIdx.x == 0 && p.timeout != nullptr) atomicExch(p.timeout, (int)CKV_ETIMEOUT);
+    if (threadIdx.x == 0) atomicExch(p.timeout, (int)CKV_ETIMEOUT);
     volatile uint32_t zero = 0;
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_wait_bounded(k_full, phase ^ i, &zero, 200000000ull);

@@ -244,7 +244,7 @@ template <typename T> cudaError_t by_format(const DecodeArgs& p, int format, int
 
 size_t decode_workspace_bytes(const CacheDims& d) {
   const int G = d.Hq / d.Hkv;
-  const size_t rows = G < kQ ? kQ : (G > 32 ? 32 : (G + 7) / 8 * 8);   // the most an item of either kernel has
+  const size_t rows = G < 16 ? G : 16;                   // the most an item of either kernel has
   return (kDecodeMaxCtas * (sizeof(int2) + 2 * rows * (d.dh + 2) * sizeof(float)) + 255) / 256 * 256;
 }
 

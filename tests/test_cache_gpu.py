@@ -421,6 +421,24 @@ def test_decode(dtype, fmt, dh, G, Hkv, nseq, page, lens):
     assert B.criticalkv_last_path(simt.handle) & 256
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dh,G,page,lens", [(128, 4, 16, "short"), (64, 8, 64, "edges"), (128, 16, 32, "edges"),
+                                            (64, 3, 16, "one"), (128, 20, 128, "short")])
+def test_decode_of_many_short_heads(fmt, dh, G, page, lens):
+    """More heads than CTAs, each of a few rows: every warp works on its own.  One head is long and split over many."""
+    nseq, Hkv = 60, 8
+    lens = LENS[lens](nseq, Hkv)
+    lens[31, 3] = 3001
+    cols = -(-3001 // page)
+    cache = Cache(nseq=nseq, Hq=G * Hkv, Hkv=Hkv, dh=dh, dtype="bf16", fmt=fmt, page=page, cols=cols).fill(lens, G)
+    q = (1.5 * torch.randn(nseq, G * Hkv, dh, generator=gen(G + 1))).bfloat16()
+    got = cache.c.attend(q.cuda(), lens.cuda())
+    check_decode(cache, q, lens, got)
+    again = cache.c.attend(q.cuda(), lens.cuda())
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    assert cache.c.device_status() == 0
+
+
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "plain"), ("bf16", "e4m3"), ("f32", "int8"), ("f32", "plain")])
 @pytest.mark.parametrize("G", [1, 2, 3])
 def test_decode_of_one_long_head(dtype, fmt, G):

@@ -85,6 +85,8 @@ def test_decode_refuses_bad_arguments(lib, fake):
         assert rc(**{name: at}) == B.CKV_EALIGN
     assert rc(q_stride=(0, 68)) == B.CKV_EALIGN and rc(q_stride=(-512, 0)) == B.CKV_EINVAL
     assert rc(ws_bytes=B.criticalkv_decode_workspace_bytes(c) - 1) == B.CKV_EWORKSPACE
+    huge = _cache(nseq=1 << 12, max_pages=1 << 23)          # more tiles than 32 bits count
+    assert B.criticalkv_decode(fake, huge, 256, None, 256, 256, None, 256, ws_bytes=1 << 30, check=False) == B.CKV_ENOTSUP
     assert B.criticalkv_decode(fake, _cache(nseq=0), None, None, None, None, None, None, ws_bytes=0, check=False) == B.CKV_OK
 
 
