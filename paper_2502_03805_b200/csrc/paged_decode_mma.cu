@@ -98,7 +98,7 @@ template <int FMT, int DH, int NT> struct Shape {
 
 // Cache row that row i of the matrix instruction stands for (i + 8: 8 further).  In the K read the eight lanes that
 // are served together hold two neighbouring i and all c: their rows must differ in bit 2; in the V read they hold rows
-// kRowOf(0, 2, 4, 6) or (1, 3, 5, 7): those must differ in bits 1-2.
+// row_of(0, 2, 4, 6) or (1, 3, 5, 7): those must differ in bits 1-2.
 __device__ __forceinline__ int row_of(int i) { return (0x37156240 >> (4 * i)) & 7; }   // 0 4 2 6 5 1 7 3
 
 template <int FMT, int DH, int NT> struct alignas(1024) Slots {   // of a warp
