@@ -2,8 +2,10 @@
 //
 // A warp takes 16 rows of a 64-row tile.  Logits: the four lanes of a quad share rows r and r + 8, each with a quarter
 // of the elements, the queries come from shared memory (one 16-byte read per 8 products).  Softmax: lane = (query row,
-// four cache rows), running maximum and sum in float32.  Values: a lane owns four elements and keeps the sums of all
-// eight query rows, the weights come from shared memory.  Products, weights and sums are float32 throughout.
+// two or four cache rows), running maximum and sum in float32.  Values: a lane owns four elements and keeps the sums of
+// all query rows of the item (four, or eight where the group is larger: half the products of a group of four would be of
+// rows that do not exist), the weights come from shared memory.  Products, weights and sums are float32 throughout.
+// Half of the values and the page of the next rows are loaded before the logits.
 #include <cuda_bf16.h>
 
 #include "paged_decode.cuh"
@@ -11,7 +13,7 @@
 namespace ckv {
 namespace {
 
-constexpr int kTile = 64, kWarpRows = kTile / kDecodeWarps, kQ = 8;   // cache rows a tile and a warp, query rows a chunk
+constexpr int kTile = 64, kWarpRows = kTile / kDecodeWarps;   // cache rows a tile and a warp
 
 // Four consecutive elements of a stored row, at element offset e.
 template <typename T, int FMT> struct Four {
@@ -47,7 +49,7 @@ template <typename T, int FMT> struct Four {
   }
 };
 
-template <typename T, int FMT, int DH> struct Shared {
+template <int DH, int kQ> struct Shared {   // kQ: query rows an item
   float q[kQ][DH];
   float s[kDecodeWarps][kQ][kWarpRows + 4];     // logits
   float w[kDecodeWarps][kWarpRows][kQ];         // weights
@@ -56,12 +58,13 @@ template <typename T, int FMT, int DH> struct Shared {
   float m[kDecodeWarps][kQ], l[kDecodeWarps][kQ];
 };
 
-template <typename T, int FMT, int DH>
+template <typename T, int FMT, int DH, int kQ>
 __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs p) {
   constexpr int ROW_BYTES = DH * (FMT == CKV_CACHE_PLAIN ? (int)sizeof(T) : 1);
   constexpr int PIECES = DH / 16;               // pieces of four elements a quad lane has of a row
   constexpr int LPR = DH / 4, KPI = 32 / LPR;   // values: lanes a row, rows at a time
-  __shared__ __align__(16) Shared<T, FMT, DH> sh;      // read and written 16 bytes at a time
+  constexpr int WL = 32 / kQ, WR = kWarpRows / WL;   // weights: lanes a query row, cache rows a lane
+  __shared__ __align__(16) Shared<DH, kQ> sh;      // read and written 16 bytes at a time
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   wait_for_previous_kernel();
   const Walk walk = plan<T, DH, kTile>(p);
@@ -83,26 +86,34 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
     }
     __syncthreads();
 
-    const int row = lane >> 2, c = lane & 3;
-    float m = -INFINITY, l = 0.f;               // of query row `row`; l holds this lane's share of the sum
+    const int row = lane >> 2, c = lane & 3;    // logits: cache rows row, row + 8
+    const int wq = lane / WL, wr = lane % WL * WR;   // weights: query row wq, cache rows wr...
+    float m = -INFINITY, l = 0.f;               // of query row wq; l holds this lane's share of the sum
     float acc[kQ][4];
 #pragma unroll
     for (int r = 0; r < kQ; ++r)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
 
+    const int32_t* pages = p.c.table + (long long)it.kv * p.c.max_pages;
+    const auto page_of = [&](int tile) {        // page_size is a multiple of 16: a warp's rows lie in one page
+      const int base = tile * kTile + warp * kWarpRows;
+      return tile < t1 && base < len ? __ldg(pages + (base >> p.c.page_shift)) : 0;
+    };
+    int page = page_of(t0);
     for (int tile = t0; tile < t1; ++tile) {
       const int base = tile * kTile + warp * kWarpRows;
-      int here = min(len - base, kWarpRows);    // page_size is a multiple of 16: the rows lie in one page
+      const int here = min(len - base, kWarpRows);
       if (here <= 0) break;
-      const int page = p.c.table[(long long)it.kv * p.c.max_pages + (base >> p.c.page_shift)];
-      if (page < 0 || page >= p.c.num_pages) {
+      const int at_page = page;
+      page = page_of(tile + 1);
+      if (at_page < 0 || at_page >= p.c.num_pages) {
         if (p.status != nullptr) atomicExch(p.status, (int)CKV_EBOUNDS);
         continue;
       }
       const int in_page = base & ((1 << p.c.page_shift) - 1);
-      const long long off = page * p.c.page_stride + (long long)in_page * ROW_BYTES;
-      const long long slot = ((long long)page << p.c.page_shift) + in_page;
+      const long long off = at_page * p.c.page_stride + (long long)in_page * ROW_BYTES;
+      const long long slot = ((long long)at_page << p.c.page_shift) + in_page;
       const char* K = p.c.page[0] + off;
       const char* V = p.c.page[1] + off;
 
@@ -119,6 +130,16 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
           else k[h][j].clear();
         }
       }
+      Four<T, FMT> v[8 / KPI];
+      const auto load_v = [&](int b) {
+#pragma unroll
+        for (int j = 0; j < 8 / KPI; ++j) {
+          const int i = b + j * KPI + lane / LPR;
+          if (i < here) v[j].load(V + i * ROW_BYTES, 4 * (lane % LPR));
+          else v[j].clear();
+        }
+      };
+      load_v(0);
       float s[kQ][2];
 #pragma unroll
       for (int r = 0; r < kQ; ++r) s[r][0] = s[r][1] = 0.f;
@@ -146,25 +167,28 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
         }
       __syncwarp();
 
-      // ---- weights: lane = (query row `row`, cache rows 4c..4c+3)
-      const float4 sv = *reinterpret_cast<const float4*>(&sh.s[warp][row][4 * c]);
-      const float ls[4] = {sv.x, sv.y, sv.z, sv.w};
-      float top = fmaxf(fmaxf(ls[0], ls[1]), fmaxf(ls[2], ls[3]));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // ---- weights
+      float ls[WR];
+#pragma unroll
+      for (int j = 0; j < WR; ++j) ls[j] = sh.s[warp][wq][wr + j];
+      float top = ls[0];
+#pragma unroll
+      for (int j = 1; j < WR; ++j) top = fmaxf(top, ls[j]);
+#pragma unroll
+      for (int o = 1; o < WL; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       top = fmaxf(top, m);
       const float f = rescale(m, top);
       m = top;
       l *= f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < WR; ++j) {
         const float w = ls[j] == -INFINITY ? 0.f : exp2f(ls[j] - top);
         l += w;
         float vs = 1.f;
-        if (FMT != CKV_CACHE_PLAIN && 4 * c + j < here) vs = p.c.scale[1][slot + 4 * c + j];
-        sh.w[warp][4 * c + j][row] = w * vs;
+        if (FMT != CKV_CACHE_PLAIN && wr + j < here) vs = p.c.scale[1][slot + wr + j];
+        sh.w[warp][wr + j][wq] = w * vs;
       }
-      if (c == 0) sh.f[warp][row] = f;
+      if (wr == 0) sh.f[warp][wq] = f;
       __syncwarp();
 
       // ---- values
@@ -176,19 +200,16 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
       }
 #pragma unroll
       for (int b = 0; b < kWarpRows; b += 8) {
-        Four<T, FMT> v[8 / KPI];
+        if (b > 0) load_v(b);
 #pragma unroll
         for (int j = 0; j < 8 / KPI; ++j) {
           const int i = b + j * KPI + lane / LPR;
-          if (i < here) v[j].load(V + i * ROW_BYTES, 4 * (lane % LPR));
-          else v[j].clear();
-        }
+          float w[kQ];
 #pragma unroll
-        for (int j = 0; j < 8 / KPI; ++j) {
-          const int i = b + j * KPI + lane / LPR;
-          const float4 w0 = *reinterpret_cast<const float4*>(&sh.w[warp][i][0]);
-          const float4 w1 = *reinterpret_cast<const float4*>(&sh.w[warp][i][4]);
-          const float w[kQ] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+          for (int r = 0; r < kQ; r += 4) {
+            const float4 w4 = *reinterpret_cast<const float4*>(&sh.w[warp][i][r]);
+            w[r] = w4.x; w[r + 1] = w4.y; w[r + 2] = w4.z; w[r + 3] = w4.w;
+          }
           float x[4];
           v[j].get(x);
 #pragma unroll
@@ -200,9 +221,9 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
       __syncwarp();
     }
 
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
-    if (c == 0) { sh.m[warp][row] = m; sh.l[warp][row] = l; }
+#pragma unroll
+    for (int o = 1; o < WL; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (wr == 0) { sh.m[warp][wq] = m; sh.l[warp][wq] = l; }
 #pragma unroll
     for (int r = 0; r < kQ; ++r) {
       if (KPI == 2) {
@@ -221,15 +242,20 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
   if (threadIdx.x == 0) p.join[blockIdx.x] = join;
 }
 
-template <typename T, int FMT, int DH> cudaError_t launch(DecodeArgs p, int device, int sm_count, cudaStream_t st) {
+template <typename T, int FMT, int DH, int kQ> cudaError_t launch_rows(const DecodeArgs& p, int device, int sm_count, cudaStream_t st) {
+  const auto kernel = decode_simt_kernel<T, FMT, DH, kQ>;
   static LaunchSetup setup;
-  const int per_sm = setup.resident(decode_simt_kernel<T, FMT, DH>, device, 0);
+  const int per_sm = setup.resident(kernel, device, 0);
   if (per_sm < 1) return cudaErrorInvalidDeviceFunction;
-  cudaError_t e;
   const int grid = decode_grid(p, per_sm * sm_count, kTile);
-  e = launch_early<DecodeArgs>(decode_simt_kernel<T, FMT, DH>, dim3(grid), kDecodeThreads, 0, st, p);
+  const cudaError_t e = launch_early<DecodeArgs>(kernel, dim3(grid), kDecodeThreads, 0, st, p);
   if (e != cudaSuccess) return e;
   return launch_decode_join<T, DH>(p, grid, st);
+}
+
+template <typename T, int FMT, int DH> cudaError_t launch(const DecodeArgs& p, int device, int sm_count, cudaStream_t st) {
+  return p.chunk_rows == 4 ? launch_rows<T, FMT, DH, 4>(p, device, sm_count, st)
+                           : launch_rows<T, FMT, DH, 8>(p, device, sm_count, st);
 }
 
 template <typename T> cudaError_t by_format(const DecodeArgs& p, int format, int dh, int device, int sm_count, cudaStream_t st) {
@@ -250,7 +276,7 @@ size_t decode_workspace_bytes(const CacheDims& d) {
 
 cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word, cudaStream_t st,
                                int* launches) {
-  const DecodeArgs p = decode_args(d, call, kQ, status_word);
+  const DecodeArgs p = decode_args(d, call, d.Hq / d.Hkv <= 4 ? 4 : 8, status_word);
   *launches += 2;
   return d.dtype == CKV_F32 ? by_format<float>(p, d.format, d.dh, device, sm_count, st)
                             : by_format<__nv_bfloat16>(p, d.format, d.dh, device, sm_count, st);
