@@ -283,7 +283,8 @@ CKV_API int criticalkv_diagnose(criticalkv_handle h, const criticalkv_desc* d, c
  *
  * Page ids outside [0, num_pages), row numbers outside the table and lengths outside [0, max_pages * page_size] never
  * cause an access outside a buffer: such rows are skipped (store, load), treated as absent (decode), lengths are
- * clipped; with CKV_FLAG_DEBUG_CHECKS the status word then reads CKV_EBOUNDS.
+ * clipped; with CKV_FLAG_DEBUG_CHECKS the status word then reads CKV_EBOUNDS.  The calls may be captured into graphs; the
+ * handle, the workspace and all tensors must outlive them.
  */
 typedef enum {
   CKV_CACHE_PLAIN = 0, /* pages hold rows in the model's element type (dtype)                                   */
@@ -364,7 +365,8 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
  * Attention of one new token per sequence: for query head h of sequence s, with g = h / (Hq/Hkv) and the L = lens[s, g]
  * rows of that KV head, out[s, h, :] = sum_i softmax_i(scale * q . k_i) v_i and lse[s, h] = log sum_i exp(scale * q .
  * k_i) (lse may be NULL; it is what merging with attention over other keys needs).  A head without rows gives zeros and
- * -infinity.  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
+ * -infinity; one that has rows but none in an existing page, or only logits of -infinity, gives NaN; rows with infinite or
+ * NaN values give results that are not finite.  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
  * bf16 queries run on tensor cores (stored 8-bit values enter exactly, sums and the softmax are float32); float32
  * queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores.  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) * ceil(max_pages *
  * page_size / 64) exceeds 2^31 - 1.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,

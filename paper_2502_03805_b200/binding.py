@@ -174,6 +174,7 @@ def criticalkv_create(device: int = 0):
     rc = load().criticalkv_create(C.byref(h), int(device))
     if rc != CKV_OK:
         raise CriticalKVError(rc, "criticalkv_create")
+    h.device = int(device)   # for classes that share a handle to see that it is of their device
     return h
 
 

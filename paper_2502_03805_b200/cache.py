@@ -32,6 +32,8 @@ class _Owner:
     an earlier one does not repeat the checks: `_plans` keeps what they came to (strides and descriptors for the C ABI)."""
 
     def _take_handle(self, handle, device):
+        if getattr(handle, "device", device.index) != device.index:
+            raise ValueError(f"the handle is of device {handle.device}, the tensors are on {device}")
         self._owned = handle is None
         self.handle = B.criticalkv_create(device.index) if handle is None else handle
         self._plans = {}
@@ -67,7 +69,8 @@ class _Owner:
         if stream is None:
             return _NOTHING
         if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=self.device)
+            stream = torch.cuda.ExternalStream(stream, device=self.device) if stream else \
+                torch.cuda.default_stream(self.device)
         return torch.cuda.stream(stream)
 
     def _fail(self, rc, where):

@@ -80,7 +80,9 @@ class CompressionSession:
     def compact_into(self, cache, K, V, start, lens_out=None, stream=None):
         """Step 5 into a PagedCache (quantised where its format says so) instead of K_out, V_out: the selected rows of
         K, V go behind row start[b, g] of every head; returns the new lengths."""
-        return cache.store(K, V, start, lens_out, idx=self.idx[:, :self.btot], offsets=self.offsets, stream=stream)
+        idx = self.idx[:, :self.btot]
+        # like the other calls of a session: no stream is the default stream, whatever stream is current
+        return cache.store(K, V, start, lens_out, idx=idx, offsets=self.offsets, stream=0 if stream is None else stream)
 
     def compress(self, Qw, K, V, WO, budgets_in=None, stream=None):
         return B.criticalkv_compress(self.handle, self.desc, Qw, K, V, WO, budgets_in, self.attn, self.vnorm,

@@ -541,6 +541,52 @@ def test_decode_bad_lengths_and_pages(dtype):
     check_decode(cache, q, torch.tensor([[32, 32, 30]], dtype=torch.int32), got)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_of_a_head_without_any_page(dtype):
+    lens = torch.tensor([[40, 40]], dtype=torch.int32)
+    cache = Cache(nseq=1, Hq=2, Hkv=2, dh=64, dtype=dtype, fmt="e4m3", page=16, cols=3).fill(lens, 3)
+    cache.table_dev[0, 0] = -1
+    q = torch.randn(1, 2, 64, generator=gen(8)).to(R.DT[dtype])
+    out, lse = (x.cpu() for x in cache.c.attend(q.cuda(), lens.cuda()))
+    assert bool(torch.isnan(out[0, 0]).all()) and float(lse[0, 0]) == -math.inf
+    assert bool(torch.isfinite(out[0, 1]).all()) and cache.c.device_status() == 0     # reported with debug checks only
+
+
+def test_a_handle_is_shared_on_its_own_device_only():
+    h = B.criticalkv_create(0)
+    r = Rotary(dh=64, frequencies=rope_frequencies(64), device="cuda:0", handle=h)
+    q = torch.ones(1, 1, 1, 64, device="cuda")
+    pos = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    before = B.criticalkv_launch_count(h)
+    r.rotate(q, None, pos)
+    assert B.criticalkv_launch_count(h) == before + 1
+    r.close()                                                     # does not destroy what it does not own
+    assert B.criticalkv_launch_count(h) == before + 1
+    h.device = 1
+    with pytest.raises(ValueError):
+        Rotary(dh=64, frequencies=rope_frequencies(64), device="cuda:0", handle=h)
+    B.criticalkv_destroy(h)
+
+
+def test_compact_into_follows_the_stream_of_the_session():
+    """With a side stream current, a session without a stream argument works on the default stream, the store with it."""
+    g = gen(21)
+    Hq, Hkv, dh, dm, n, w = 4, 2, 64, 64, 4000, 8
+    Qw, K, V, WO = (torch.randn(*s, generator=g).bfloat16().cuda() for s in (
+        (1, Hq, w, dh), (1, Hkv, n, dh), (1, Hkv, n, dh), (1, Hq, dh, dm)))
+    kw = dict(nb=1, Hq=Hq, Hkv=Hkv, dh=dh, dm=dm, n=n, w=w, pool_k=3, dtype="bf16", budget_mode="uniform", budget=700)
+    s = CompressionSession(**kw)
+    cache = PagedCache.allocate(nseq=1, Hq=Hq, Hkv=Hkv, dh=dh, dtype="bf16", rows=n)
+    start = cache.new_lengths()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        s.compress(Qw, K, V, WO)
+        lens = s.compact_into(cache, K, V, start)
+    torch.cuda.synchronize()
+    got, _ = cache.load(lens, 700)
+    assert torch.equal(got[0].reshape(-1, dh), s.K_out[0])
+
+
 def test_empty_batches():
     cache = Cache(nseq=0, Hq=4, Hkv=2, dh=64, dtype="bf16", fmt="e4m3", page=16, cols=1)
     lens = torch.zeros(0, 2, dtype=torch.int32, device="cuda")
