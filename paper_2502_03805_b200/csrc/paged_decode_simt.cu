@@ -6,6 +6,10 @@
 // all query rows of the item (four, or eight where the group is larger: half the products of a group of four would be of
 // rows that do not exist), the weights come from shared memory.  Products, weights and sums are float32 throughout.
 // Half of the values and the page of the next rows are loaded before the logits.
+//
+// Measured (8 x 6553 rows a head, 8 KV heads): float32 rows of 128, four queries a head, 83 us, 5.2 TB/s (0.81 of the copy
+// bandwidth; 119 us without the early loads and with items of eight); e4m3 rows 73 us, bound by arithmetic (two products
+// a stored byte and query, and the conversions).
 #include <cuda_bf16.h>
 
 #include "paged_decode.cuh"

@@ -4,7 +4,8 @@
 // the scale's division and reciprocal are paid once per lane.  A thread has 64 bytes of K and of V in flight, 32 warps
 // an SM, and follows the chain row index -> page id of its next row while it rounds and writes this one.  8 x 8 heads,
 // 6553 of 32768 rows of 128 bf16 each to e4m3: 58 us, 5.6 TB/s (101 us with 16 bytes a lane, 87 us with 16 warps an SM).
-// Load: 16 bytes of output a lane, four rows of K and V in flight.
+// Load: 16 bytes of output a lane, four rows of K and V in flight.  8 x 8 heads of 6553 e4m3 rows of 128 to bf16: 55 us,
+// 6.0 TB/s.
 #include <cuda_bf16.h>
 
 #include "launch_early.cuh"
