@@ -75,18 +75,18 @@ __device__ __forceinline__ void put_out(const DecodeArgs& p, const ItemRows& it,
                                         float l, bool empty) {
   const long long row = (long long)it.s * p.Hq + it.head + r;
   // l == 0 with rows present (every logit -inf) is 0 / 0, as in the formula
-  if (empty) put2<T>(p.out + (row * DH + 2 * pair) * sizeof(T), 0.f, 0.f);
-  else put2<T>(p.out + (row * DH + 2 * pair) * sizeof(T), a / l, b / l);
+  const float inv = empty ? 0.f : 1.f / l;
+  put2<T>(p.out + (row * DH + 2 * pair) * sizeof(T), a * inv, b * inv);
   if (pair == 0 && p.lse != nullptr) p.lse[row] = empty ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 // A CTA's range of the tile list, and the walk over the items in it.
 struct Walk {
-  long long begin, end;        // tiles
+  int begin, end;              // tiles (the host has checked that they fit)
   int item;                    // first item
-  long long first;             // its first tile in the list
-  long long total;
-  int ctas;                    // CTAs that have work (all others return)
+  int first;                   // its first tile in the list
+  int total;
+  int ctas;                    // CTAs that have work (all others have an empty range)
 };
 
 // Fills the walk (all threads get the same values).  Items without rows are written here, spread over the CTAs.
@@ -133,13 +133,13 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
   __syncthreads();
   Walk w;
   w.total = total;
-  w.ctas = (int)min((long long)gridDim.x, w.total);
+  w.ctas = min((int)gridDim.x, total);
   w.begin = w.end = 0;
   w.item = 0;
   w.first = 0;
   if ((int)blockIdx.x < w.ctas) {
-    w.begin = w.total * blockIdx.x / w.ctas;
-    w.end = w.total * (blockIdx.x + 1) / w.ctas;
+    w.begin = (int)((long long)total * blockIdx.x / w.ctas);
+    w.end = (int)((long long)total * (blockIdx.x + 1) / w.ctas);
     int a = 0, b = kDecodeThreads - 1;     // first thread whose items reach behind tile `begin`
     while (a < b) {
       const int mid = (a + b) / 2;
@@ -152,7 +152,7 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
 }
 
 // CTA whose range holds a tile: the largest i with total * i / ctas <= tile.
-__device__ __forceinline__ int cta_of(const Walk& w, long long tile) { return (int)(((tile + 1) * w.ctas - 1) / w.total); }
+__device__ __forceinline__ int cta_of(const Walk& w, int tile) { return (int)(((tile + 1LL) * w.ctas - 1) / w.total); }
 
 // Joins the warps' results of one group of NR rows and hands them on: to the output when the CTA did the whole item,
 // else to the partial slot.  o_s [warp][NR][DH] unnormalised sums, m_s, l_s [warp][NR].  All threads call it, and the
@@ -233,8 +233,9 @@ __device__ __forceinline__ void add_parts(const DecodeArgs& p, int r, int c0, in
   }
 }
 
-// One CTA per (CTA of the decode kernel, row of its item): joins the item that ends in that CTA, if it began in an
-// earlier one.  Warps take the parts in turn, then meet in shared memory: a fixed order of additions.
+// CTAs (i, y): the item that ends in CTA i of the decode kernel, if it began in an earlier one.  Up to eight parts: y = 0
+// does it all, a warp a row.  More: y is the row, whose parts the warps take in turn before they meet in shared memory.
+// A fixed order of additions either way.
 template <typename T, int DH>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p) {
   constexpr int WARPS = kJoinThreads / 32, E = DH / 64;   // pairs of elements a lane
@@ -245,9 +246,18 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p)
   const int2 what = p.join[blockIdx.x];
   if (what.x < 0) return;
   const ItemRows it = item_rows(p, what.x);
-  if (r >= it.rows) return;
   float m, l;
   float2 acc[E];
+  if ((int)blockIdx.x - what.y < 8) {
+    if (r > 0) return;
+    for (int row = warp; row < it.rows; row += WARPS) {
+      add_parts<DH>(p, row, what.y, blockIdx.x, what.y, 1, m, l, acc);
+#pragma unroll
+      for (int e = 0; e < E; ++e) put_out<T, DH>(p, it, row, lane + 32 * e, acc[e].x, acc[e].y, m, l, false);
+    }
+    return;
+  }
+  if (r >= it.rows) return;
   add_parts<DH>(p, r, what.y, blockIdx.x, what.y + warp, WARPS, m, l, acc);
 #pragma unroll
   for (int e = 0; e < E; ++e) *reinterpret_cast<float2*>(&o_s[warp][2 * (lane + 32 * e)]) = acc[e];

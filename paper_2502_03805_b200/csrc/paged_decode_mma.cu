@@ -133,7 +133,7 @@ template <int SUB> struct Step {
 // A CTA's part of an item: tiles [t0, t1) of it.
 struct Segment {
   int item, kv, len, tiles, t0, t1;
-  long long first;                                         // the item's first tile in the list of all tiles
+  int first;                                               // the item's first tile in the list of all tiles
 };
 
 template <int FMT, int DH, int NT>
@@ -167,8 +167,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
       g.kv = g.item / p.chunks;
       g.len = item_len(p, g.kv);
       g.tiles = (g.len + S::kTile - 1) / S::kTile;
-      g.t0 = (int)max(walk.begin - g.first, 0LL);
-      g.t1 = (int)min((long long)g.tiles, walk.end - g.first);
+      g.t0 = max(walk.begin - g.first, 0);
+      g.t1 = min(g.tiles, walk.end - g.first);
       if (g.t1 > g.t0) return g;
     }
   };
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
         float top = sh.m[0][row];
 #pragma unroll
         for (int w = 1; w < kDecodeWarps; ++w) top = fmaxf(top, sh.m[w][row]);
-        const float f = rescale(m[n][x], top);
+        const float f = m[n][x] == -INFINITY ? 0.f : ptx::ex2_approx(m[n][x] - top);
         float sum = l[n][x];
         sum += __shfl_xor_sync(0xffffffffu, sum, 4);
         sum += __shfl_xor_sync(0xffffffffu, sum, 8);

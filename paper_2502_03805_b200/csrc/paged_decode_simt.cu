@@ -73,13 +73,13 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
   wait_for_previous_kernel();
   const Walk walk = plan<T, DH, kTile>(p);
   int2 join = make_int2(-1, 0);
-  long long first = walk.first, t = walk.begin;
+  int first = walk.first, t = walk.begin;
   for (int item = walk.item; t < walk.end; ++item) {
     const ItemRows it = item_rows(p, item);
     const int len = item_len(p, it.kv);
     const int tiles = (len + kTile - 1) / kTile;
     if (first + tiles <= t) { first += tiles; continue; }
-    const int t0 = (int)(t - first), t1 = (int)min((long long)tiles, walk.end - first);
+    const int t0 = t - first, t1 = min(tiles, walk.end - first);
 
     __syncthreads();
     for (int i = threadIdx.x; i < kQ * DH; i += kDecodeThreads) {
