@@ -41,14 +41,19 @@ struct DecodeArgs {
 struct ItemRows {   // the query heads of an item
   int s, head, rows, kv;       // sequence, first query head, number of heads, sequence * Hkv + KV head
 };
-__device__ __forceinline__ ItemRows item_rows(const DecodeArgs& p, int item) {
+__device__ __forceinline__ ItemRows item_rows(const DecodeArgs& p, int kv, int chunk) {
   ItemRows r;
-  const int chunk = item % p.chunks;
-  r.kv = item / p.chunks;
-  r.s = r.kv / p.c.Hkv;
-  r.head = (r.kv % p.c.Hkv) * p.G + chunk * p.chunk_rows;
+  r.kv = kv;
+  r.s = kv / p.c.Hkv;
+  r.head = (kv - r.s * p.c.Hkv) * p.G + chunk * p.chunk_rows;
   r.rows = min(p.chunk_rows, p.G - chunk * p.chunk_rows);
   return r;
+}
+// sequence * Hkv + KV head of an item; most calls have one chunk, and a division is twenty instructions
+__device__ __forceinline__ int kv_of(const DecodeArgs& p, int item) { return p.chunks == 1 ? item : item / p.chunks; }
+__device__ __forceinline__ ItemRows item_rows(const DecodeArgs& p, int item) {
+  const int kv = kv_of(p, item);
+  return item_rows(p, kv, item - kv * p.chunks);
 }
 __device__ __forceinline__ int item_len(const DecodeArgs& p, int kv) {
   return (int)min(max((long long)p.lens[kv], 0LL), p.c.capacity);
@@ -101,7 +106,7 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
   bool bad = false, empty = false;
 #pragma unroll 4
   for (int j = lo; j < hi; ++j) {
-    const int given = __ldg(p.lens + j / p.chunks);
+    const int given = __ldg(p.lens + kv_of(p, j));
     const int len = (int)min(max((long long)given, 0LL), p.c.capacity);
     bad = bad || len != given;
     empty = empty || len == 0;
@@ -110,7 +115,7 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
   if (bad && p.status != nullptr) atomicExch(p.status, (int)CKV_EBOUNDS);
   if (empty) {
     for (int j = lo; j < hi; ++j)
-      if (item_len(p, j / p.chunks) == 0 && j % gridDim.x == blockIdx.x) {
+      if (item_len(p, kv_of(p, j)) == 0 && j % gridDim.x == blockIdx.x) {
         const ItemRows it = item_rows(p, j);
         for (int r = 0; r < it.rows; ++r)
           for (int k = 0; k < DH / 2; ++k) put_out<T, DH>(p, it, r, k, 0.f, 0.f, 0.f, 0.f, true);

@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
       g.item += 1;
       g.t0 = g.t1 = 0;
       if (g.first >= walk.end) return g;
-      g.kv = g.item / p.chunks;
+      g.kv = kv_of(p, g.item);
       g.len = item_len(p, g.kv);
       g.tiles = (g.len + S::kTile - 1) / S::kTile;
       g.t0 = max(walk.begin - g.first, 0);
@@ -239,8 +239,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
   const int k_row = row_of(r);
   // The queries of an item as they are stored, in the element order of the K pieces.
   uint32_t q[NT][S::kChunks][S::kQWords];
-  auto load_queries = [&](int item) {
-    const ItemRows it = item_rows(p, item);
+  auto load_queries = [&](const Segment& g) {
+    const ItemRows it = item_rows(p, g.kv, g.item - g.kv * p.chunks);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int row = 8 * n + r;
@@ -285,13 +285,13 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
   if (seg.t0 < seg.t1) {
     advance(cur);
     advance(next);
-    load_queries(seg.item);
+    load_queries(seg);
     check(cur);
     fetch(cur, true);
     fetch(cur, false);
   }
   while (seg.t0 < seg.t1 && ok) {
-    const ItemRows it = item_rows(p, seg.item);
+    const ItemRows it = item_rows(p, seg.kv, seg.item - seg.kv * p.chunks);
     float to_log2[NT][2];                      // factor of the products for query columns 2c, 2c+1
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
 #pragma unroll
         for (int u = 1; u < SUB; ++u) whole_step = whole_step && (u % together != 0 || cur.page[u] >= 0);
       }
-      if (tile + 1 == seg.t1 && after.t0 < after.t1) load_queries(after.item);
+      if (tile + 1 == seg.t1 && after.t0 < after.t1) load_queries(after);
 
       // ---- weights.  s[n][u][2h + x]: cache row k_row + 8h of group u, query 8n + 2c + x
       if (!whole_step) {
