@@ -17,6 +17,8 @@ from . import binding as B
 _TORCH_DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
 _NAME = {v: k for k, v in _TORCH_DTYPE.items()}
 _NOTHING = contextlib.nullcontext()
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (     # handle of a device's current stream
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 _CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
 
 
@@ -29,7 +31,8 @@ class _Owner:
     """The handle of an object: the caller's, or one of its own that is destroyed with it.
 
     A decode step is a handful of microseconds, so a call whose tensors have the types, shapes, strides and devices of
-    an earlier one does not repeat the checks: `_plans` keeps what they came to (strides and descriptors for the C ABI)."""
+    an earlier one does not repeat the checks: `_plans` keeps what they came to (strides and descriptors for the C ABI).
+    The calls spell out the signatures of their tensors (a function call for each would cost as much as a launch)."""
 
     def _take_handle(self, handle, device):
         if getattr(handle, "device", device.index) != device.index:
@@ -38,14 +41,12 @@ class _Owner:
         self.handle = B.criticalkv_create(device.index) if handle is None else handle
         self._plans = {}
         self._lib = B.load()
+        self._index = device.index
 
-    def _plan(self, key, make, *args):
-        plan = self._plans.get(key)
-        if plan is None:
-            plan = make(*args)
-            if len(self._plans) >= 256:      # prompts of ever new lengths
-                self._plans.clear()
-            self._plans[key] = plan
+    def _keep(self, key, plan):
+        if len(self._plans) >= 256:      # prompts of ever new lengths
+            self._plans.clear()
+        self._plans[key] = plan
         return plan
 
     def close(self):
@@ -61,7 +62,7 @@ class _Owner:
 
     def _on(self, stream):
         if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self.device.index)
+            return _raw_stream(self._index)
         return stream if isinstance(stream, int) else stream.cuda_stream
 
     def _allocating(self, stream):
@@ -172,6 +173,7 @@ class Rotary(_Owner):
         self.device = _device_of(self.freq, "frequencies")
         self.dh, self.rot, self.layout, self.factor = dh, 2 * self.freq.numel(), layout, float(factor)
         self._take_handle(handle, self.device)
+        self._rope, self._freq_at = self._lib.criticalkv_rope, self.freq.data_ptr()
 
     def rotate(self, q, k, positions, q_out=None, k_out=None, stream=None):
         """q [nseq, Hq, T, dh] and k [nseq, Hk, T, dh] (or None), any strides with contiguous rows; positions int32
@@ -181,11 +183,12 @@ class Rotary(_Owner):
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device) if q_out is None else q_out
                 if k is not None and k_out is None:
                     k_out = torch.empty(k.shape, dtype=k.dtype, device=self.device)
-        desc = self._plan((_sig(q), _sig(k), _sig(positions), _sig(q_out), _sig(k_out)), self._describe, q, k, positions,
-                          q_out, k_out)
-        rc = self._lib.criticalkv_rope(self.handle, desc, q.data_ptr(), None if k is None else k.data_ptr(),
-                                       positions.data_ptr(), self.freq.data_ptr(), q_out.data_ptr(),
-                                       None if k is None else k_out.data_ptr(), self._on(stream))
+        key = (q.dtype, q.shape, q.stride(), q.get_device(), _sig(k), positions.dtype, positions.shape, positions.stride(),
+               positions.get_device(), q_out.dtype, q_out.shape, q_out.stride(), q_out.get_device(), _sig(k_out))
+        desc = self._plans.get(key) or self._keep(key, self._describe(q, k, positions, q_out, k_out))
+        rc = self._rope(self.handle, desc, q.data_ptr(), None if k is None else k.data_ptr(), positions.data_ptr(),
+                        self._freq_at, q_out.data_ptr(), None if k is None else k_out.data_ptr(),
+                        _raw_stream(self._index) if stream is None else self._on(stream))
         if rc:
             self._fail(rc, "criticalkv_rope")
         return q_out, k_out
@@ -264,7 +267,8 @@ class PagedCache(_Owner):
         self._lse_like = torch.empty((nseq, Hq), dtype=torch.float32, device=dev)
         self._ref = C.byref(self.desc)
         self._take_handle(handle, dev)
-        self._decode = self._lib.criticalkv_decode
+        self._decode, self._store = self._lib.criticalkv_decode, self._lib.criticalkv_cache_store
+        self._load = self._lib.criticalkv_cache_load
 
     @classmethod
     def allocate(cls, *, nseq, Hq, Hkv, dh, dtype, rows, format="plain", page_size=64, device=0, **kw):
@@ -292,15 +296,17 @@ class PagedCache(_Owner):
         if lens_out is None:
             with self._allocating(stream):
                 lens_out = torch.empty((self.nseq, self.Hkv), dtype=torch.int32, device=self.device)
-        n, idx_rows, strides = self._plan(("store", _sig(K), _sig(V), _sig(start), _sig(lens_out), _sig(idx),
-                                           _sig(offsets), _sig(counts)), self._describe_store, K, V, start, lens_out,
-                                          idx, offsets, counts)
+        key = (K.dtype, K.shape, K.stride(), K.get_device(), V.dtype, V.shape, V.stride(), V.get_device(), start.dtype,
+               start.shape, start.stride(), start.get_device(), lens_out.dtype, lens_out.shape, lens_out.stride(),
+               lens_out.get_device(), _sig(idx), _sig(offsets), _sig(counts))
+        n, idx_rows, strides = self._plans.get(key) or self._keep(
+            key, self._describe_store(K, V, start, lens_out, idx, offsets, counts))
         if idx_rows == 0:      # no list, or an empty one, whose address could not be passed (n is 0 then)
             idx = offsets = None
-        rc = self._lib.criticalkv_cache_store(
+        rc = self._store(
             self.handle, self._ref, K.data_ptr(), V.data_ptr(), n, strides, None if idx is None else idx.data_ptr(),
             None if offsets is None else offsets.data_ptr(), idx_rows, None if counts is None else counts.data_ptr(),
-            start.data_ptr(), lens_out.data_ptr(), self._on(stream))
+            start.data_ptr(), lens_out.data_ptr(), _raw_stream(self._index) if stream is None else self._on(stream))
         if rc:
             self._fail(rc, "criticalkv_cache_store")
         return lens_out
@@ -340,10 +346,11 @@ class PagedCache(_Owner):
             with self._allocating(stream):
                 K_out = torch.zeros((self.nseq, self.Hkv, n, self.dh), dtype=self.torch_dtype, device=self.device)
                 V_out = torch.zeros_like(K_out)
-        n, strides = self._plan(("load", n, _sig(lens), _sig(K_out), _sig(V_out)), self._describe_load, lens, n, K_out,
-                                V_out)
-        rc = self._lib.criticalkv_cache_load(self.handle, self._ref, lens.data_ptr(), n, strides, 1 if align_right else 0,
-                                             K_out.data_ptr(), V_out.data_ptr(), self._on(stream))
+        key = (n, lens.dtype, lens.shape, lens.stride(), lens.get_device(), K_out.dtype, K_out.shape, K_out.stride(),
+               K_out.get_device(), V_out.dtype, V_out.shape, V_out.stride(), V_out.get_device())
+        n, strides = self._plans.get(key) or self._keep(key, self._describe_load(lens, n, K_out, V_out))
+        rc = self._load(self.handle, self._ref, lens.data_ptr(), n, strides, 1 if align_right else 0, K_out.data_ptr(),
+                        V_out.data_ptr(), _raw_stream(self._index) if stream is None else self._on(stream))
         if rc:
             self._fail(rc, "criticalkv_cache_load")
         return K_out, V_out
@@ -371,8 +378,9 @@ class PagedCache(_Owner):
     def attend(self, q, lens, out=None, lse=None, *, ws=None, stream=None):
         """Attention of one new token per sequence: q [nseq, Hq, dh] over the lens[s, g] rows of every head.  Returns
         (out [nseq, Hq, dh], lse float32 [nseq, Hq])."""
-        strides, size = self._plan((_sig(q), _sig(lens), _sig(out), _sig(lse), _sig(ws)), self._describe_attend, q, lens,
-                                   out, lse, ws)
+        key = (q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(), lens.get_device(),
+               _sig(out), _sig(lse), _sig(ws))
+        strides, size = self._plans.get(key) or self._keep(key, self._describe_attend(q, lens, out, lse, ws))
         if stream is None:
             out = torch.empty_like(self._out_like) if out is None else out
             lse = torch.empty_like(self._lse_like) if lse is None else lse
@@ -383,7 +391,7 @@ class PagedCache(_Owner):
                 lse = torch.empty_like(self._lse_like) if lse is None else lse
                 ws = self.workspace() if ws is None else ws
         rc = self._decode(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                          ws.data_ptr(), size, self._on(stream))
+                          ws.data_ptr(), size, _raw_stream(self._index) if stream is None else self._on(stream))
         if rc:
             self._fail(rc, "criticalkv_decode")
         return out, lse
