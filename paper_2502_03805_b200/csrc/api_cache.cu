@@ -49,7 +49,7 @@ int resolve_cache(const criticalkv_cache* c, CacheDims* o) {
   o->nseq = c->nseq; o->Hq = c->Hq; o->Hkv = c->Hkv; o->dh = c->dh; o->dtype = c->dtype; o->format = c->format;
   o->page_shift = shift; o->num_pages = c->num_pages; o->max_pages = c->max_pages;
   o->capacity = capacity;
-  o->scale = c->scale > 0.f ? c->scale : (float)(1.0 / sqrt((double)c->dh));
+  o->scale = c->scale > 0.f ? (double)c->scale : 1.0 / sqrt((double)c->dh);
   o->debug_checks = (c->flags & CKV_FLAG_DEBUG_CHECKS) ? 1 : 0;
   o->k_pages = c->k_pages; o->v_pages = c->v_pages;
   o->k_scale = c->k_scale; o->v_scale = c->v_scale;

@@ -129,7 +129,7 @@ struct CacheDims {
   int nseq, Hq, Hkv, dh, dtype, format, page_shift, num_pages, max_pages;
   long long page_stride;                    // elements
   long long capacity;                       // rows a head can hold
-  float scale;
+  double scale;
   int debug_checks;
   void* k_pages;
   void* v_pages;

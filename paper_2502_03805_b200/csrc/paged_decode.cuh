@@ -33,7 +33,7 @@ struct DecodeArgs {
   int items, Hq, G;            // G = Hq / Hkv
   int chunks, chunk_rows;      // query heads of a KV head: chunks of at most chunk_rows
   int part_rows;               // the most query heads an item has
-  float scale_log2;            // scale * log2(e)
+  float scale_log2, scale_rest;   // scale * log2(e), and what its rounding to a float left out
   int* status;                 // CKV_FLAG_DEBUG_CHECKS: where a violated bound is reported; null otherwise
   int* timeout;                // where a wait that ran out is reported
 };
@@ -304,7 +304,8 @@ inline DecodeArgs decode_args(const CacheDims& d, const DecodeCall& call, int ch
   p.chunks = (p.G + chunk_rows - 1) / chunk_rows;
   p.part_rows = p.G < chunk_rows ? p.G : chunk_rows;
   p.items = d.nseq * d.Hkv * p.chunks;
-  p.scale_log2 = d.scale * 1.4426950408889634f;
+  p.scale_log2 = (float)(d.scale * 1.4426950408889634);
+  p.scale_rest = (float)(d.scale * 1.4426950408889634 - (double)p.scale_log2);
   p.status = d.debug_checks ? status_word : nullptr;
   p.timeout = status_word;
   return p;

@@ -4,11 +4,12 @@
 // of the elements, the queries come from shared memory (one 16-byte read per 8 products).  Softmax: lane = (query row,
 // two or four cache rows), running maximum and sum in float32.  Values: a lane owns four elements and keeps the sums of
 // all query rows of the item (four, or eight where the group is larger: half the products of a group of four would be of
-// rows that do not exist), the weights come from shared memory.  Products, weights and sums are float32 throughout.
+// rows that do not exist), the weights come from shared memory.  Products, weights and sums are float32 throughout; the
+// scale enters with the rest of its rounding, and only the difference of a logit to the maximum is rounded.
 // Half of the values and the page of the next rows are loaded before the logits.
 //
-// Measured (8 x 6553 rows a head, 8 KV heads): float32 rows of 128, four queries a head, 83 us, 5.2 TB/s (0.81 of the copy
-// bandwidth; 119 us without the early loads and with items of eight); e4m3 rows 73 us, bound by arithmetic (two products
+// Measured (8 x 6553 rows a head, 8 KV heads): float32 rows of 128, four queries a head, 80 us, 5.4 TB/s (0.84 of the copy
+// bandwidth; 119 us without the early loads and with items of eight); e4m3 rows 64 us, bound by arithmetic (two products
 // a stored byte and query, and the conversions).
 #include <cuda_bf16.h>
 
@@ -55,15 +56,16 @@ template <typename T, int FMT> struct Four {
 
 template <int DH, int kQ> struct Shared {   // kQ: query rows an item
   float q[kQ][DH];
-  float s[kDecodeWarps][kQ][kWarpRows + 4];     // logits
+  float s[kDecodeWarps][kQ][kWarpRows + 4];     // logits before the scale
   float w[kDecodeWarps][kWarpRows][kQ];         // weights
   float f[kDecodeWarps][kQ];                    // rescaling of the sums
   float o[kDecodeWarps][kQ][DH];
   float m[kDecodeWarps][kQ], l[kDecodeWarps][kQ];
 };
 
+// CTAs an SM: four where the sums of four query rows leave the registers for it, three with eight (two to four measured)
 template <typename T, int FMT, int DH, int kQ>
-__global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs p) {
+__global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_kernel(DecodeArgs p) {
   constexpr int ROW_BYTES = DH * (FMT == CKV_CACHE_PLAIN ? (int)sizeof(T) : 1);
   constexpr int PIECES = DH / 16;               // pieces of four elements a quad lane has of a row
   constexpr int LPR = DH / 4, KPI = 32 / LPR;   // values: lanes a row, rows at a time
@@ -167,7 +169,7 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
           float v = s[r][h];
           v += __shfl_xor_sync(0xffffffffu, v, 1);
           v += __shfl_xor_sync(0xffffffffu, v, 2);
-          if ((r >> 1) == c) sh.s[warp][r][row + 8 * h] = row + 8 * h < here ? v * ks[h] * p.scale_log2 : -INFINITY;
+          if ((r >> 1) == c) sh.s[warp][r][row + 8 * h] = row + 8 * h < here ? v * ks[h] : -INFINITY;
         }
       __syncwarp();
 
@@ -180,13 +182,14 @@ __global__ void __launch_bounds__(kDecodeThreads) decode_simt_kernel(DecodeArgs 
       for (int j = 1; j < WR; ++j) top = fmaxf(top, ls[j]);
 #pragma unroll
       for (int o = 1; o < WL; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      top = fmaxf(top, m);
+      top = fmaxf(top * p.scale_log2, m);
       const float f = rescale(m, top);
       m = top;
       l *= f;
 #pragma unroll
       for (int j = 0; j < WR; ++j) {
-        const float w = ls[j] == -INFINITY ? 0.f : exp2f(ls[j] - top);
+        // the difference to the maximum is rounded, not the logit: fma, and both parts of the factor
+        const float w = ls[j] == -INFINITY ? 0.f : exp2f(fmaf(ls[j], p.scale_log2, -top) + ls[j] * p.scale_rest);
         l += w;
         float vs = 1.f;
         if (FMT != CKV_CACHE_PLAIN && wr + j < here) vs = p.c.scale[1][slot + wr + j];

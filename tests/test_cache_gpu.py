@@ -488,13 +488,15 @@ def test_decode_large_and_tiny_queries():
             check_decode(cache, q, lens, cache.c.attend(q.cuda(), lens.cuda()), scale=1.0 / (8 * size) if size else 1.0)
 
 
+@pytest.mark.parametrize("scale", [0.0, 0.1, 0.13])     # scale * log2(e) rounds down and up
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "plain"), ("bf16", "e4m3"), ("bf16", "int8"), ("f32", "plain"), ("f32", "int8")])
-def test_decode_infinities_and_nan(dtype, fmt):
+def test_decode_infinities_and_nan(dtype, fmt, scale):
     """Rows with a NaN or an infinity make the heads that read them NaN, as in the formula, and no others; logits of
     -infinity have weight 0."""
     nan = math.nan
     lens = torch.tensor([[70, 70, 70, 70]], dtype=torch.int32)
-    cache = Cache(nseq=1, Hq=4, Hkv=4, dh=64, dtype=dtype, fmt=fmt, page=16, cols=5).fill(lens, 3)
+    cache = Cache(nseq=1, Hq=4, Hkv=4, dh=64, dtype=dtype, fmt=fmt, page=16, cols=5, scale=scale).fill(lens, 3)
+    scale = scale or 0.125
     q = torch.randn(1, 4, 64, generator=gen(8)).to(R.DT[dtype])
     page = cache.table[0, :, 2].long().tolist()
     where = (cache.v, cache.k) if fmt == "plain" else (cache.vs, cache.ks)
@@ -510,7 +512,7 @@ def test_decode_infinities_and_nan(dtype, fmt):
         cache.k[page[3], 4, 0] = -math.inf if float(q[0, 3, 0]) > 0 else math.inf
         out, lse = (x.cpu().double() for x in cache.c.attend(q.cuda(), lens.cuda()))
         K, V = (R.head_rows(x, cache.table[0, 3], 70, 16) for x in cache.values())
-        logit = K @ q[0, 3].double() / 8.0
+        logit = K @ q[0, 3].double() * scale
         assert float(logit.min()) == -math.inf
         assert abs(float(lse[0, 3]) - float(torch.logsumexp(logit, 0))) < 1e-4
         want = torch.softmax(logit, 0) @ V
