@@ -3,9 +3,11 @@
 //
 // The angle is reduced to a fraction of a turn in float64 (pos * freq loses up to pos * 2^-24 radians in float32: 0.008
 // at position 131072) and only then goes to sincospif.  All heads of a token share its rot/2 angles, so a thread owns
-// one unit of one token's rows (16 bytes of a pair's first elements and 16 of its second), keeps the unit's cosines and
-// sines in registers and walks over the heads, two rows in flight, 32 warps an SM.  Bound by HBM: every row is read and
-// written once (32768 tokens of 40 heads of 128 bf16: 108 us, 6.2 TB/s; four rows in flight on 16 warps: 153 us).
+// one unit of one token's rows (half layout: 16 bytes of a pair's first elements and 16 of its second; interleaved: 16
+// bytes), keeps the unit's cosines and sines in registers and walks over the heads, 64 bytes in flight, 32 warps an SM.
+// Elements that are only copied form units of the same size.  Bound by HBM: every row is read and written once (32768
+// tokens of 40 heads of 128 bf16: 106 us, 6.3 TB/s; four rows in flight on 16 warps: 153 us; a quarter of the elements
+// turned: within 1 % of all of them, 22 % slower while copied units were 16 bytes).
 #include <cuda_bf16.h>
 
 #include "ckv_internal.h"
@@ -15,7 +17,6 @@ namespace ckv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 2;         // rows in flight per thread
 
 struct RopeArgs {
   const char* x[2];              // q, k
@@ -42,12 +43,16 @@ template <typename T> union Vec16 {
   T e[16 / sizeof(T)];
 };
 
+// Rows in flight per thread: 32 bytes of each (half layout, two rows), 16 bytes (interleaved, four), or an element or two.
+constexpr int rows_in_flight(bool vec, bool half) { return vec && half ? 2 : 4; }
+
 // VEC units move 16-byte vectors, the others single elements (row parts that do not divide into vectors).
 template <typename T, bool VEC, bool HALF>
 __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs p) {
   wait_for_previous_kernel();
   constexpr int V = VEC ? 16 / (int)sizeof(T) : 1;
   constexpr int P = (HALF || !VEC) ? V : V / 2;                // pairs a unit
+  constexpr int kRows = rows_in_flight(VEC, HALF);
   const int pairs = p.rot / 2;
   const int turned = pairs / P;                                // units that are turned; the others are copied
   const int u = threadIdx.x % p.units, rest = threadIdx.x / p.units;
@@ -55,11 +60,17 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs p) {
   const int s = blockIdx.x / p.tiles, t = (blockIdx.x % p.tiles) * p.tile + tok;
   if (group >= p.groups || t >= p.T) return;
   const bool turn = u < turned;
-  // element offsets of the unit's two parts
+  // element offsets of the unit's two parts; the copied vectors of the half layout go by two as well
   int ea, eb;
-  if (VEC) {
-    ea = (HALF && !turn ? u + turned : u) * V;
-    eb = HALF ? ea + pairs : ea;
+  bool two = turn;
+  if (VEC && HALF) {
+    const int copied = (p.dh - p.rot) / V, i = u - turned;
+    ea = turn ? u * V : p.rot + i * V;
+    eb = turn ? ea + pairs : ea + (copied + 1) / 2 * V;
+    two = eb < p.dh;
+  } else if (VEC) {
+    ea = eb = u * V;
+    two = false;
   } else {
     ea = turn ? (HALF ? u : 2 * u) : p.rot + u - turned;
     eb = HALF ? u + pairs : 2 * u + 1;
@@ -80,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs p) {
           const T* row = reinterpret_cast<const T*>(x + hk * p.xs[which][1]);
           if (VEC) {
             a[k].raw = *reinterpret_cast<const uint4*>(row + ea);
-            if (HALF && turn) b[k].raw = *reinterpret_cast<const uint4*>(row + eb);
+            if (HALF && two) b[k].raw = *reinterpret_cast<const uint4*>(row + eb);
           } else {
             a[k].e[0] = row[ea];
             if (turn) b[k].e[0] = row[eb];
@@ -117,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs p) {
           }
           if (VEC) {
             *reinterpret_cast<uint4*>(row + ea) = a[k].raw;
-            if (HALF && turn) *reinterpret_cast<uint4*>(row + eb) = b[k].raw;
+            if (HALF && two) *reinterpret_cast<uint4*>(row + eb) = b[k].raw;
           } else {
             row[ea] = a[k].e[0];
             if (turn) row[eb] = b[k].e[0];
@@ -134,7 +145,8 @@ cudaError_t launch_typed(RopeArgs p, int layout, int nseq, int sm_count, cudaStr
   // whole vectors only where the rotated part (each half of it in the half layout) divides into them
   const bool half = layout == CKV_ROPE_HALF;
   const bool vec = (half ? p.rot / 2 : p.rot) % V == 0;
-  p.units = vec ? (half ? p.rot / 2 : p.rot) / V + (p.dh - p.rot) / V : p.rot / 2 + (p.dh - p.rot);   // at most 256
+  p.units = !vec ? p.rot / 2 + p.dh - p.rot                                     // at most 256
+            : half ? p.rot / 2 / V + ((p.dh - p.rot) / V + 1) / 2 : p.dh / V;
   p.tile = kThreads / p.units < p.T ? kThreads / p.units : p.T;
   p.tiles = (p.T + p.tile - 1) / p.tile;
   p.groups = kThreads / (p.units * p.tile);
@@ -143,8 +155,8 @@ cudaError_t launch_typed(RopeArgs p, int layout, int nseq, int sm_count, cudaStr
   const long long ctas = (long long)p.tiles * nseq;
   if (ctas > 0x7fffffffLL) return cudaErrorInvalidValue;
   // heads are spread over CTAs as well until every SM has eight (each of them computes the tile's angles again), but
-  // not below two rows a thread
-  const int turns = (most + p.groups * kRows - 1) / (p.groups * kRows);
+  // not below the rows a thread has in flight
+  const int per_turn = p.groups * rows_in_flight(vec, half), turns = (most + per_turn - 1) / per_turn;
   p.splits = (int)((8LL * sm_count + ctas - 1) / ctas);
   if (p.splits > turns) p.splits = turns;
   const dim3 grid((unsigned)ctas, (unsigned)p.splits);
