@@ -25,8 +25,8 @@
 // elements 2^-29 below it.
 //
 // Measured: 2 x 131072 bf16 rows a head, 40 query heads on 8, 168 us, 6.4 TB/s (0.98 of the copy bandwidth); 32 x 6553
-// e4m3 rows a head, 32 query heads on 8, 85 us, 5.3 TB/s (0.82), bound by instruction latency: 168 registers leave three
-// CTAs an SM, and with 128 the sums spill (122 us).  1 x 819 bf16 rows: 7.8 us, a chain of latencies.
+// e4m3 rows a head, 32 query heads on 8, 82 us, 5.5 TB/s (0.85), bound by instruction latency: 168 registers leave three
+// CTAs an SM, and with 128 the sums spill (122 us).  1 x 819 bf16 rows: 7.9 us, a chain of latencies.
 #include "paged_decode.cuh"
 #include "sm100_ptx.cuh"
 #include "tma_host.h"

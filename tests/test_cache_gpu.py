@@ -46,16 +46,18 @@ def check_rope(got, x, pos, freq, layout, factor, dtype):
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("nseq,Hq,Hk,T,dh,rot", [
     (1, 32, 8, 1, 128, 128), (3, 5, 1, 17, 64, 64), (2, 8, 2, 33, 128, 64), (1, 2, 2, 100, 64, 6), (7, 4, 4, 1, 64, 20),
-    (1, 1, 1, 3, 8, 2), (1, 3, 1, 5, 256, 256), (2, 1, 1, 16, 96, 48), (40, 12, 3, 1, 64, 32)])
+    (1, 1, 1, 3, 8, 2), (1, 3, 1, 5, 256, 256), (2, 1, 1, 16, 96, 48), (40, 12, 3, 1, 64, 32),
+    (1, 2, 2, 9, 40, 16), (2, 9, 1, 70, 24, 16), (1, 1, 0, 5, 16, 16), (3, 70, 0, 2, 128, 32)])
 def test_rope_shapes(dtype, layout, nseq, Hq, Hk, T, dh, rot):
     g = gen(1)
     q, k = (torch.randn(nseq, H, T, dh, generator=g).to(R.DT[dtype]) for H in (Hq, Hk))
     pos = torch.randint(0, 140000, (nseq, T), generator=g, dtype=torch.int32)
     freq = rope_frequencies(rot, 500000.0)
     r = Rotary(dh=dh, frequencies=freq, layout=layout, device="cuda:0")
-    qo, ko = r.rotate(q.cuda(), k.cuda(), pos.cuda())
+    qo, ko = r.rotate(q.cuda(), k.cuda() if Hk else None, pos.cuda())
     check_rope(qo, q, pos, freq, layout, 1.0, dtype)
-    check_rope(ko, k, pos, freq, layout, 1.0, dtype)
+    if Hk:
+        check_rope(ko, k, pos, freq, layout, 1.0, dtype)
 
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
@@ -247,6 +249,18 @@ def test_store_of_selected_rows_strided_source_interleaved_pool(fmt):
     assert torch.equal(lens.cpu(), (start + counts).to(torch.int32)) and cache.intact()
 
 
+def test_store_of_the_same_row_several_times():
+    g = gen(31)
+    cache = Cache(nseq=1, Hq=1, Hkv=1, dh=64, dtype="f32", fmt="e4m3", page=16, cols=2)
+    K, V = (torch.randn(1, 1, 4, 64, generator=g) for _ in range(2))
+    rows = [2, 2, 0, 2, 3, 0, 0]
+    before = cache.bits()
+    lens = cache.c.store(K.cuda(), V.cuda(), cache.c.new_lengths(), idx=torch.tensor([rows], dtype=torch.int32, device="cuda"),
+                         offsets=torch.tensor([[0, 7]], dtype=torch.int32, device="cuda"))
+    assert int(lens) == 7
+    assert same(cache.bits(), expect_store(cache, before, K, V, lambda s, h: rows, torch.zeros(1, 1, dtype=torch.int32)))
+
+
 @pytest.mark.parametrize("n", [1, 5000])      # one CTA a head, and many (a second launch then updates the lengths)
 def test_store_updates_its_own_lengths_and_honours_counts(n):
     g = gen(n)
@@ -413,6 +427,7 @@ def test_decode(dtype, fmt, dh, G, Hkv, nseq, page, lens):
     check_decode(cache, q, lens, got)
     assert out.intact() and lse.intact() and ws.intact() and cache.intact()
     assert cache.c.device_status() == 0
+    assert B.criticalkv_last_path(cache.c.handle) & 384 == (128 if dtype == "bf16" else 256)
     again = cache.c.attend(q.cuda(), lens.cuda())                              # another workspace: the same bits
     assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
     simt = PagedCache(Hq=G * Hkv, dtype=dtype, format=fmt, k_pages=cache.k, v_pages=cache.v, k_scale=cache.ks,
