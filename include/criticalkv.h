@@ -90,7 +90,8 @@ enum {
                                      layer at a time that is about twice as fast.  Same results bit for bit      */
   CKV_FLAG_SELECT_NO_CLUSTER = 1u << 8, /* criticalkv_select: no thread-block clusters in steps 3-4 (the separate
                                      kernels then give every head one CTA), for contexts where cluster launches are
-                                     not wanted.  Same results bit for bit                                      */
+                                     not wanted.  Same results bit for bit.  criticalkv_decode: none either, small calls
+                                     take two launches instead of one; the sums are added in another order        */
   CKV_FLAG_DEBUG_CHECKS = 1u << 6, /* device-side checks in criticalkv_select, criticalkv_compact and
                                      criticalkv_gather_positions: every index read from idx / offsets / budgets and
                                      every output position is tested against the bounds the descriptor implies
@@ -305,7 +306,8 @@ typedef struct {
   int32_t page_size;     /* rows a page: 16, 32, 64, 128 or 256                                                 */
   int32_t num_pages;     /* pages in the pool, >= 1                                                             */
   int32_t max_pages;     /* columns of the page table, >= 1; a head holds at most max_pages * page_size rows    */
-  uint32_t flags;        /* CKV_FLAG_FORCE_SIMT (criticalkv_decode), CKV_FLAG_DEBUG_CHECKS                      */
+  uint32_t flags;        /* CKV_FLAG_FORCE_SIMT and CKV_FLAG_SELECT_NO_CLUSTER (criticalkv_decode),
+                            CKV_FLAG_DEBUG_CHECKS                                                               */
   float scale;           /* logit scale; <= 0 selects 1/sqrt(dh)                                                */
   uint32_t reserved;     /* must be 0                                                                           */
   int64_t page_stride;   /* elements of k_pages / v_pages from one page to the next, 0 = page_size * dh         */

@@ -31,7 +31,7 @@ int resolve_cache(const criticalkv_cache* c, CacheDims* o) {
     default: return CKV_ENOTSUP;
   }
   if (c->num_pages < 1 || c->max_pages < 1) return CKV_EINVAL;
-  if (c->flags & ~(uint32_t)(CKV_FLAG_FORCE_SIMT | CKV_FLAG_DEBUG_CHECKS)) return CKV_EINVAL;
+  if (c->flags & ~(uint32_t)(CKV_FLAG_FORCE_SIMT | CKV_FLAG_DEBUG_CHECKS | CKV_FLAG_SELECT_NO_CLUSTER)) return CKV_EINVAL;
   if (c->reserved != 0 || !isfinite(c->scale)) return CKV_EINVAL;
   const long long capacity = (long long)c->max_pages << shift;
   // row numbers are 32-bit, and so is the number of a call's (sequence, query head) pairs
@@ -51,6 +51,7 @@ int resolve_cache(const criticalkv_cache* c, CacheDims* o) {
   o->capacity = capacity;
   o->scale = c->scale > 0.f ? (double)c->scale : 1.0 / sqrt((double)c->dh);
   o->debug_checks = (c->flags & CKV_FLAG_DEBUG_CHECKS) ? 1 : 0;
+  o->allow_cluster = (c->flags & CKV_FLAG_SELECT_NO_CLUSTER) ? 0 : 1;
   o->k_pages = c->k_pages; o->v_pages = c->v_pages;
   o->k_scale = c->k_scale; o->v_scale = c->v_scale;
   o->page_table = c->page_table;

@@ -131,6 +131,7 @@ struct CacheDims {
   long long capacity;                       // rows a head can hold
   double scale;
   int debug_checks;
+  int allow_cluster;                        // 0: decode without thread-block clusters
   void* k_pages;
   void* v_pages;
   float* k_scale;

@@ -13,19 +13,28 @@ __device__ __forceinline__ void wait_for_previous_kernel() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// cluster: CTAs of a thread-block cluster (0: none).
 template <typename... P>
-cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, P... args) {
+cudaError_t launch_early_in_clusters(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, cudaStream_t st,
+                                     P... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename... P>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, P... args) {
+  return launch_early_in_clusters<P...>(kernel, grid, threads, smem, 0, st, args...);
 }
 
 }  // namespace ckv

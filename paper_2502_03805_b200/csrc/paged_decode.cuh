@@ -6,6 +6,9 @@
 // a CTA has at most two incomplete items: the one its range begins inside (partial slot 0) and the one that begins in
 // the range and goes on behind it (slot 1).  Their unnormalised sums with the running maximum and sum go to the
 // workspace; decode_join_kernel adds them up in CTA order, so equal inputs give equal bits.
+//
+// Few items of few tiles (by the size of the page table) are instead given to a team of CTAs each, a thread-block cluster,
+// whose parts meet in distributed shared memory: one launch instead of two.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -20,6 +23,7 @@ constexpr int kDecodeThreads = 128;
 constexpr int kDecodeWarps = kDecodeThreads / 32;
 constexpr int kDecodeMaxCtas = 592;      // four a multiprocessor on 148
 constexpr int kJoinThreads = 256;
+constexpr int kMaxTeam = 16;             // CTAs that share an item where items have teams, at most
 
 struct DecodeArgs {
   Pages c;
@@ -33,6 +37,8 @@ struct DecodeArgs {
   int items, Hq, G;            // G = Hq / Hkv
   int chunks, chunk_rows;      // query heads of a KV head: chunks of at most chunk_rows
   int part_rows;               // the most query heads an item has
+  int team;                    // CTAs i * team ... are a cluster and item i is theirs; 0: all items are one list
+  int allow_cluster;           // host: whether a team may be chosen
   float scale_log2, scale_rest;   // scale * log2(e), and what its rounding to a float left out
   int* status;                 // CKV_FLAG_DEBUG_CHECKS: where a violated bound is reported; null otherwise
   int* timeout;                // where a wait that ran out is reported
@@ -156,15 +162,85 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
   return w;
 }
 
+// The walk of a CTA of a team: its share of the team's one item.
+template <typename T, int DH, int TILE>
+__device__ __forceinline__ Walk team_walk(const DecodeArgs& p) {
+  Walk w;
+  const int rank = blockIdx.x % p.team;
+  w.item = blockIdx.x / p.team;
+  const int kv = kv_of(p, w.item), len = item_len(p, kv);
+  w.total = (len + TILE - 1) / TILE;
+  w.first = 0;
+  w.ctas = p.team;
+  w.begin = w.total * rank / p.team;       // few tiles: decode_team
+  w.end = w.total * (rank + 1) / p.team;
+  if (rank == 0) {
+    if (threadIdx.x == 0 && len != p.lens[kv] && p.status != nullptr) atomicExch(p.status, (int)CKV_EBOUNDS);
+    if (len == 0) {
+      const ItemRows it = item_rows(p, w.item);
+      for (int i = threadIdx.x; i < it.rows * (DH / 2); i += kDecodeThreads)
+        put_out<T, DH>(p, it, i / (DH / 2), i % (DH / 2), 0.f, 0.f, 0.f, 0.f, true);
+    }
+  }
+  return w;
+}
+
+// A team's parts: every CTA of it calls this, also those without a tile.  parts [row][DH + 2] of the CTA: sums, maximum,
+// sum of weights, filled where the CTA had tiles but not all of them; otherwise the sum of weights is 0.  The results are
+// spread over the team's threads; each adds up the parts in order.
+__device__ __forceinline__ float2 load_of_team(const float* mine, int rank) {
+  uint32_t at;
+  float2 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void team_barrier() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+template <typename T, int DH>
+__device__ __forceinline__ void join_team(const DecodeArgs& p, const Walk& w, const float* parts) {
+  team_barrier();
+  if (w.total > 1) {                       // a single tile was one CTA's, which has written the result
+    const ItemRows it = item_rows(p, w.item);
+    for (int i = blockIdx.x % p.team * kDecodeThreads + threadIdx.x; i < it.rows * (DH / 2); i += p.team * kDecodeThreads) {
+      const int r = i / (DH / 2), pair = i % (DH / 2);
+      const float* row = parts + r * (DH + 2);
+      float2 ml[kMaxTeam], v[kMaxTeam];
+#pragma unroll
+      for (int c = 0; c < kMaxTeam; ++c) {
+        ml[c] = v[c] = make_float2(-INFINITY, 0.f);
+        if (c < p.team) {
+          ml[c] = load_of_team(row + DH, c);
+          v[c] = load_of_team(row + 2 * pair, c);
+        }
+      }
+      float top = -INFINITY, a = 0.f, b = 0.f, l = 0.f;
+#pragma unroll
+      for (int c = 0; c < kMaxTeam; ++c) top = fmaxf(top, ml[c].x);
+#pragma unroll
+      for (int c = 0; c < kMaxTeam; ++c)
+        if (ml[c].y != 0.f) {              // else nothing was visible there, and its sums may not have been written
+          const float f = rescale(ml[c].x, top);
+          a += f * v[c].x;
+          b += f * v[c].y;
+          l += f * ml[c].y;
+        }
+      put_out<T, DH>(p, it, r, pair, a, b, top, l, false);
+    }
+  }
+  team_barrier();                          // nobody leaves while its parts are read
+}
+
 // CTA whose range holds a tile: the largest i with total * i / ctas <= tile.
 __device__ __forceinline__ int cta_of(const Walk& w, int tile) { return (int)(((tile + 1LL) * w.ctas - 1) / w.total); }
 
 // Joins the warps' results of one group of NR rows and hands them on: to the output when the CTA did the whole item,
-// else to the partial slot.  o_s [warp][NR][DH] unnormalised sums, m_s, l_s [warp][NR].  All threads call it, and the
+// else to its part.  o_s [warp][NR][DH] unnormalised sums, m_s, l_s [warp][NR].  All threads call it, and the
 // buffers may be reused behind the barrier that the caller places.
 template <typename T, int DH, int NR>
 __device__ __forceinline__ void finish(const DecodeArgs& p, const ItemRows& it, const float* o_s, const float* m_s,
-                                       const float* l_s, int row0, bool whole, int slot) {
+                                       const float* l_s, int row0, bool whole, float* parts) {
   constexpr int PAIRS = DH / 2;
   for (int i = threadIdx.x; i < NR * PAIRS; i += kDecodeThreads) {
     const int r = i / PAIRS, k = i % PAIRS;
@@ -185,7 +261,7 @@ __device__ __forceinline__ void finish(const DecodeArgs& p, const ItemRows& it, 
     if (whole) {
       put_out<T, DH>(p, it, row0 + r, k, a, b, top, l, false);
     } else {
-      float* part = part_slot(p, DH, blockIdx.x, slot) + (row0 + r) * (DH + 2);
+      float* part = parts + (row0 + r) * (DH + 2);
       *reinterpret_cast<float2*>(part + 2 * k) = make_float2(a, b);
       if (k == 0) *reinterpret_cast<float2*>(part + DH) = make_float2(top, l);
     }
@@ -308,24 +384,64 @@ inline DecodeArgs decode_args(const CacheDims& d, const DecodeCall& call, int ch
   p.scale_rest = (float)(d.scale * 1.4426950408889634 - (double)p.scale_log2);
   p.status = d.debug_checks ? status_word : nullptr;
   p.timeout = status_word;
+  p.team = 0;
+  p.allow_cluster = d.allow_cluster;
   return p;
 }
 
-// What a kernel needs to know once per device: CTAs an SM holds, and leave for its dynamic shared memory.
+// What a kernel needs to know once per device (asked for on its first launch there): CTAs an SM holds, and teams of 16 and
+// of 8 that can run at once, which is fewer than CTAs / 16 or 8, since a cluster lies in one group of multiprocessors.
 struct LaunchSetup {
   static constexpr int kDevices = 64;
-  std::atomic<int> per_sm[kDevices] = {};
-  template <typename K> int resident(K kernel, int device, int smem) {
-    int n = device < kDevices ? per_sm[device].load(std::memory_order_acquire) : 0;
-    if (n > 0) return n;
+  struct Fit {
+    std::atomic<int> per_sm{0};
+    std::atomic<int> teams[2] = {};
+  } fit[kDevices];
+  template <typename K> const Fit* of(K kernel, int device, int smem) {
+    if (device >= kDevices) return nullptr;
+    Fit& f = fit[device];
+    if (f.per_sm.load(std::memory_order_acquire) > 0) return &f;
     if (smem > 48 * 1024 - 2048 &&
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-      return 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kDecodeThreads, smem) != cudaSuccess) return 0;
-    if (device < kDevices) per_sm[device].store(n, std::memory_order_release);
-    return n;
+      return nullptr;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return nullptr;
+    for (int i = 0; i < 2; ++i) {
+      cudaLaunchConfig_t cfg = {};
+      cudaLaunchAttribute attr;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = (unsigned)(kMaxTeam >> i);
+      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+      cfg.gridDim = dim3((unsigned)(kMaxTeam * 64));
+      cfg.blockDim = dim3(kDecodeThreads);
+      cfg.dynamicSmemBytes = (size_t)smem;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      int teams = 0;
+      if (cudaOccupancyMaxActiveClusters(&teams, kernel, &cfg) != cudaSuccess) {
+        teams = 0;
+        cudaGetLastError();
+      }
+      f.teams[i].store(teams, std::memory_order_relaxed);
+    }
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kDecodeThreads, smem) != cudaSuccess || n < 1) return nullptr;
+    f.per_sm.store(n, std::memory_order_release);
+    return &f;
   }
 };
+
+// CTAs an item's team has, 0: no teams.  All teams run at once, and a CTA has at most three tiles (by the table's size, the
+// lengths are not known here): with more the even split over all CTAs and its join are as fast (2600 rows, 3.3 tiles a CTA:
+// 11.9 us a call with teams, 11.6 without).  One launch instead of two.  A call with teams and without, and on the device,
+// us, heads of 128, 8 KV heads of bf16 rows: 1 sequence x 819 rows 9.3 and 11.7 (8.2 and 8.0), 3 sequences 9.9 and 11.6
+// (8.9 and 9.9), 6 sequences 10.7 and 13.3 (10.3 and 12.8); 5 sequences x 1237 int8 rows, 2 KV heads of 64, float32
+// queries: 9.1 and 11.6 (8.0 and 7.2).  More teams than run at once: 24 of 16 CTAs 14.9 us on the device against 9.9.
+inline int decode_team(const DecodeArgs& p, const LaunchSetup::Fit& fit, int tile) {
+  const long long tiles = (p.c.capacity + tile - 1) / tile;
+  for (int i = 0; i < 2; ++i)
+    if (p.allow_cluster && p.items <= fit.teams[i].load(std::memory_order_relaxed) && tiles <= 3 * (kMaxTeam >> i)) return kMaxTeam >> i;
+  return 0;
+}
 
 // One CTA per resident slot, fewer when even full heads have fewer tiles than that.
 inline int decode_grid(const DecodeArgs& p, int resident, int tile) {

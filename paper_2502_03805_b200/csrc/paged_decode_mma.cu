@@ -118,6 +118,7 @@ template <int FMT, int DH, int NT> struct Shared {
   Scales<FMT, DH, NT> scales[kDecodeWarps];
   float o[kDecodeWarps][4][DH];                            // four queries at a time
   float m[kDecodeWarps][16], l[kDecodeWarps][16], top[16];
+  alignas(8) float parts[8 * NT][DH + 2];                  // of a CTA of a team
   uint64_t full[kDecodeWarps][2];                          // K and V of a warp have arrived
   uint32_t late;                                           // a copy did not arrive in time: the other waits give up too
 };
@@ -155,7 +156,9 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
   }
   ptx::fence_barrier_init();
   wait_for_previous_kernel();
-  const Walk walk = plan<T, DH, S::kTile>(p);              // contains barriers: the mbarriers are visible behind it
+  const Walk walk = p.team ? team_walk<T, DH, S::kTile>(p) : plan<T, DH, S::kTile>(p);
+  if (threadIdx.x < 8 * NT) *reinterpret_cast<float2*>(&sh.parts[threadIdx.x][DH]) = make_float2(-INFINITY, 0.f);
+  __syncthreads();                                         // the mbarriers are visible
 
   // The segment behind `g` (its item, first and tiles), or one with t0 == t1.
   auto following = [&](Segment g) {
@@ -626,7 +629,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
           if (whole) {
             put_out<T, DH>(p, it, row, pair, sum.x, sum.y, sh.top[row], total, false);
           } else {
-            float* part = part_slot(p, DH, blockIdx.x, seg.t0 > 0 ? 0 : 1) + row * (DH + 2);
+            float* part = p.team ? sh.parts[row] : part_slot(p, DH, blockIdx.x, seg.t0 > 0 ? 0 : 1) + row * (DH + 2);
             *reinterpret_cast<float2*>(part + 2 * pair) = sum;
             if (pair == 0) *reinterpret_cast<float2*>(part + DH) = make_float2(sh.top[row], total);
           }
@@ -646,7 +649,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
       ptx::mbar_wait_bounded(v_full, phase ^ i, &zero, 200000000ull);
     }
   }
-  if (threadIdx.x == 0) p.join[blockIdx.x] = join;
+  if (p.team) join_team<T, DH>(p, walk, &sh.parts[0][0]);
+  else if (threadIdx.x == 0) p.join[blockIdx.x] = join;
 }
 
 // Pages as TMA sees them: bytes in spans of 128 (or 64) x spans of a row x rows of a page x pages.
@@ -662,25 +666,29 @@ template <typename S> bool page_map(CUtensorMap* m, const DecodeArgs& p, int whi
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int FMT, int DH, int NT> cudaError_t launch(const DecodeArgs& p, int device, int sm_count, cudaStream_t st) {
+template <int FMT, int DH, int NT>
+cudaError_t launch(DecodeArgs p, int device, int sm_count, cudaStream_t st, int* launches) {
   const auto kernel = decode_mma_kernel<FMT, DH, NT>;
   constexpr int smem = (int)sizeof(Shared<FMT, DH, NT>) + 1024;   // the slots start on a multiple of 1024
   static LaunchSetup setup;
-  const int per_sm = setup.resident(kernel, device, smem);
-  if (per_sm < 1) return cudaErrorInvalidDeviceFunction;
+  const LaunchSetup::Fit* fit = setup.of(kernel, device, smem);
+  if (!fit) return cudaErrorInvalidDeviceFunction;
   CUtensorMap maps[2];
   for (int i = 0; i < 2; ++i)
     if (!page_map<Shape<FMT, DH, NT>>(&maps[i], p, i, min(1 << p.c.page_shift, 16 * Shape<FMT, DH, NT>::kSub))) return cudaErrorInvalidValue;
-  const int grid = decode_grid(p, per_sm * sm_count, Shape<FMT, DH, NT>::kTile);
-  const cudaError_t e = launch_early<DecodeArgs, CUtensorMap, CUtensorMap>(kernel, dim3(grid), kDecodeThreads, smem, st, p,
-                                                                           maps[0], maps[1]);
-  if (e != cudaSuccess) return e;
+  p.team = decode_team(p, *fit, Shape<FMT, DH, NT>::kTile);
+  const int grid = p.team ? p.items * p.team : decode_grid(p, fit->per_sm * sm_count, Shape<FMT, DH, NT>::kTile);
+  *launches += 1;
+  const cudaError_t e = launch_early_in_clusters<DecodeArgs, CUtensorMap, CUtensorMap>(kernel, dim3(grid), kDecodeThreads, smem,
+                                                                                       p.team, st, p, maps[0], maps[1]);
+  if (e != cudaSuccess || p.team) return e;
+  *launches += 1;
   return launch_decode_join<__nv_bfloat16, DH>(p, grid, st);
 }
 
-template <int FMT> cudaError_t by_shape(const DecodeArgs& p, int dh, int device, int sm_count, cudaStream_t st) {
-  if (p.chunk_rows == 8) return dh == 64 ? launch<FMT, 64, 1>(p, device, sm_count, st) : launch<FMT, 128, 1>(p, device, sm_count, st);
-  return dh == 64 ? launch<FMT, 64, 2>(p, device, sm_count, st) : launch<FMT, 128, 2>(p, device, sm_count, st);
+template <int FMT> cudaError_t by_shape(const DecodeArgs& p, int dh, int device, int sm_count, cudaStream_t st, int* launches) {
+  if (p.chunk_rows == 8) return dh == 64 ? launch<FMT, 64, 1>(p, device, sm_count, st, launches) : launch<FMT, 128, 1>(p, device, sm_count, st, launches);
+  return dh == 64 ? launch<FMT, 64, 2>(p, device, sm_count, st, launches) : launch<FMT, 128, 2>(p, device, sm_count, st, launches);
 }
 
 }  // namespace
@@ -689,10 +697,9 @@ cudaError_t launch_decode_mma(const CacheDims& d, const DecodeCall& call, int de
                               int* launches) {
   // queries of a KV head: 8 or 16 an item; more than 16 read the cache once per 16
   const DecodeArgs p = decode_args(d, call, d.Hq / d.Hkv <= 8 ? 8 : 16, status_word);
-  *launches += 2;
-  if (d.format == CKV_CACHE_PLAIN) return by_shape<CKV_CACHE_PLAIN>(p, d.dh, device, sm_count, st);
-  if (d.format == CKV_CACHE_E4M3) return by_shape<CKV_CACHE_E4M3>(p, d.dh, device, sm_count, st);
-  return by_shape<CKV_CACHE_INT8>(p, d.dh, device, sm_count, st);
+  if (d.format == CKV_CACHE_PLAIN) return by_shape<CKV_CACHE_PLAIN>(p, d.dh, device, sm_count, st, launches);
+  if (d.format == CKV_CACHE_E4M3) return by_shape<CKV_CACHE_E4M3>(p, d.dh, device, sm_count, st, launches);
+  return by_shape<CKV_CACHE_INT8>(p, d.dh, device, sm_count, st, launches);
 }
 
 }  // namespace ckv

@@ -61,6 +61,7 @@ template <int DH, int kQ> struct Shared {   // kQ: query rows an item
   float f[kDecodeWarps][kQ];                    // rescaling of the sums
   float o[kDecodeWarps][kQ][DH];
   float m[kDecodeWarps][kQ], l[kDecodeWarps][kQ];
+  alignas(8) float parts[kQ][DH + 2];           // of a CTA of a team
 };
 
 // CTAs an SM: four where the sums of four query rows leave the registers for it, three with eight (two to four measured)
@@ -73,7 +74,8 @@ __global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_k
   __shared__ __align__(16) Shared<DH, kQ> sh;      // read and written 16 bytes at a time
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   wait_for_previous_kernel();
-  const Walk walk = plan<T, DH, kTile>(p);
+  const Walk walk = p.team ? team_walk<T, DH, kTile>(p) : plan<T, DH, kTile>(p);
+  if (threadIdx.x < kQ) *reinterpret_cast<float2*>(&sh.parts[threadIdx.x][DH]) = make_float2(-INFINITY, 0.f);
   int2 join = make_int2(-1, 0);
   int first = walk.first, t = walk.begin;
   for (int item = walk.item; t < walk.end; ++item) {
@@ -241,36 +243,43 @@ __global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_k
         *reinterpret_cast<float4*>(&sh.o[warp][r][4 * lane]) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
     }
     __syncthreads();
-    finish<T, DH, kQ>(p, it, &sh.o[0][0][0], &sh.m[0][0], &sh.l[0][0], 0, t0 == 0 && t1 == tiles, t0 > 0 ? 0 : 1);
+    finish<T, DH, kQ>(p, it, &sh.o[0][0][0], &sh.m[0][0], &sh.l[0][0], 0, t0 == 0 && t1 == tiles,
+                      p.team ? &sh.parts[0][0] : part_slot(p, DH, blockIdx.x, t0 > 0 ? 0 : 1));
     if (t0 > 0 && t1 == tiles) join = make_int2(item, cta_of(walk, first));
     t = first + t1;
     first += tiles;
   }
-  if (threadIdx.x == 0) p.join[blockIdx.x] = join;
+  if (p.team) join_team<T, DH>(p, walk, &sh.parts[0][0]);
+  else if (threadIdx.x == 0) p.join[blockIdx.x] = join;
 }
 
-template <typename T, int FMT, int DH, int kQ> cudaError_t launch_rows(const DecodeArgs& p, int device, int sm_count, cudaStream_t st) {
+template <typename T, int FMT, int DH, int kQ> cudaError_t launch_rows(DecodeArgs p, int device, int sm_count, cudaStream_t st,
+                                                                               int* launches) {
   const auto kernel = decode_simt_kernel<T, FMT, DH, kQ>;
   static LaunchSetup setup;
-  const int per_sm = setup.resident(kernel, device, 0);
-  if (per_sm < 1) return cudaErrorInvalidDeviceFunction;
-  const int grid = decode_grid(p, per_sm * sm_count, kTile);
-  const cudaError_t e = launch_early<DecodeArgs>(kernel, dim3(grid), kDecodeThreads, 0, st, p);
-  if (e != cudaSuccess) return e;
+  const LaunchSetup::Fit* fit = setup.of(kernel, device, 0);
+  if (!fit) return cudaErrorInvalidDeviceFunction;
+  p.team = decode_team(p, *fit, kTile);
+  const int grid = p.team ? p.items * p.team : decode_grid(p, fit->per_sm * sm_count, kTile);
+  *launches += 1;
+  const cudaError_t e = launch_early_in_clusters<DecodeArgs>(kernel, dim3(grid), kDecodeThreads, 0, p.team, st, p);
+  if (e != cudaSuccess || p.team) return e;
+  *launches += 1;
   return launch_decode_join<T, DH>(p, grid, st);
 }
 
-template <typename T, int FMT, int DH> cudaError_t launch(const DecodeArgs& p, int device, int sm_count, cudaStream_t st) {
-  return p.chunk_rows == 4 ? launch_rows<T, FMT, DH, 4>(p, device, sm_count, st)
-                           : launch_rows<T, FMT, DH, 8>(p, device, sm_count, st);
+template <typename T, int FMT, int DH> cudaError_t launch(const DecodeArgs& p, int device, int sm_count, cudaStream_t st, int* launches) {
+  return p.chunk_rows == 4 ? launch_rows<T, FMT, DH, 4>(p, device, sm_count, st, launches)
+                           : launch_rows<T, FMT, DH, 8>(p, device, sm_count, st, launches);
 }
 
-template <typename T> cudaError_t by_format(const DecodeArgs& p, int format, int dh, int device, int sm_count, cudaStream_t st) {
+template <typename T> cudaError_t by_format(const DecodeArgs& p, int format, int dh, int device, int sm_count, cudaStream_t st,
+                                             int* launches) {
   if (format == CKV_CACHE_PLAIN)
-    return dh == 64 ? launch<T, CKV_CACHE_PLAIN, 64>(p, device, sm_count, st) : launch<T, CKV_CACHE_PLAIN, 128>(p, device, sm_count, st);
+    return dh == 64 ? launch<T, CKV_CACHE_PLAIN, 64>(p, device, sm_count, st, launches) : launch<T, CKV_CACHE_PLAIN, 128>(p, device, sm_count, st, launches);
   if (format == CKV_CACHE_E4M3)
-    return dh == 64 ? launch<T, CKV_CACHE_E4M3, 64>(p, device, sm_count, st) : launch<T, CKV_CACHE_E4M3, 128>(p, device, sm_count, st);
-  return dh == 64 ? launch<T, CKV_CACHE_INT8, 64>(p, device, sm_count, st) : launch<T, CKV_CACHE_INT8, 128>(p, device, sm_count, st);
+    return dh == 64 ? launch<T, CKV_CACHE_E4M3, 64>(p, device, sm_count, st, launches) : launch<T, CKV_CACHE_E4M3, 128>(p, device, sm_count, st, launches);
+  return dh == 64 ? launch<T, CKV_CACHE_INT8, 64>(p, device, sm_count, st, launches) : launch<T, CKV_CACHE_INT8, 128>(p, device, sm_count, st, launches);
 }
 
 }  // namespace
@@ -284,9 +293,8 @@ size_t decode_workspace_bytes(const CacheDims& d) {
 cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word, cudaStream_t st,
                                int* launches) {
   const DecodeArgs p = decode_args(d, call, d.Hq / d.Hkv <= 4 ? 4 : 8, status_word);
-  *launches += 2;
-  return d.dtype == CKV_F32 ? by_format<float>(p, d.format, d.dh, device, sm_count, st)
-                            : by_format<__nv_bfloat16>(p, d.format, d.dh, device, sm_count, st);
+  return d.dtype == CKV_F32 ? by_format<float>(p, d.format, d.dh, device, sm_count, st, launches)
+                            : by_format<__nv_bfloat16>(p, d.format, d.dh, device, sm_count, st, launches);
 }
 
 }  // namespace ckv

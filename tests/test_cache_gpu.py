@@ -473,6 +473,26 @@ def test_decode_of_few_long_heads(dtype, fmt):
     check_decode(cache, q, lens, cache.c.attend(q.cuda(), lens.cuda()))
 
 
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "plain"), ("bf16", "e4m3"), ("f32", "int8"), ("f32", "plain")])
+@pytest.mark.parametrize("dh,G,Hkv", [(128, 4, 2), (64, 16, 1), (64, 1, 7), (128, 9, 1), (64, 8, 25), (64, 20, 2)])
+@pytest.mark.parametrize("rows", [16, 48, 130, 384, 760])
+def test_decode_with_clusters_and_without(dtype, fmt, dh, G, Hkv, rows):
+    """Few short heads: one launch with a cluster a head; two launches without.  Every length from none to full in turn."""
+    cache = Cache(nseq=1, Hq=G * Hkv, Hkv=Hkv, dh=dh, dtype=dtype, fmt=fmt, page=16, cols=(rows + 15) // 16)
+    full = torch.full((1, Hkv), rows, dtype=torch.int32)
+    cache.fill(full, 2)
+    apart = PagedCache(Hq=G * Hkv, dtype=dtype, format=fmt, k_pages=cache.k, v_pages=cache.v, k_scale=cache.ks,
+                       v_scale=cache.vs, page_table=cache.table_dev, flags=B.CKV_FLAG_SELECT_NO_CLUSTER)
+    q = torch.randn(1, G * Hkv, dh, generator=gen(3)).to(R.DT[dtype])
+    for lens in (full, torch.zeros_like(full), (full - torch.arange(Hkv) * 7).clamp(min=0).to(torch.int32),
+                 torch.arange(1, Hkv + 1, dtype=torch.int32).view(1, Hkv).clamp(max=rows)):
+        for c, launches in ((cache.c, 1), (apart, 2)):
+            before = B.criticalkv_launch_count(c.handle)
+            got = c.attend(q.cuda(), lens.cuda())
+            assert B.criticalkv_launch_count(c.handle) - before == launches
+            check_decode(cache, q, lens, got)
+
+
 def test_decode_strided_queries_scale_and_shared_pages():
     lens = torch.tensor([[50, 20], [50, 33]], dtype=torch.int32)
     cache = Cache(nseq=2, Hq=8, Hkv=2, dh=64, dtype="bf16", fmt="plain", page=16, cols=4, scale=0.31).fill(lens, 3)
