@@ -158,22 +158,24 @@ class ChunkedPrefillCompressor:
 
     def to_cache(self, cache, start=None, stream=None):
         """Writes the retained rows into a PagedCache of one sequence (decoding starts from there) and returns the
-        lengths of its heads."""
+        lengths of its heads.  All of it is done on `stream` (None: the current one), on which the rows must be ready."""
         if self.K is None:
             raise ValueError("nothing has been compressed yet")
-        start = cache.new_lengths() if start is None else start
-        if self.budget_mode == "uniform":
-            return cache.store(self.K[None], self.V[None], start, stream=stream)
-        # heads of different lengths: one list of rows, head g's part from offsets[g]
-        counts = [int(k.shape[0]) for k in self.K]
-        n = max(max(counts), 1)
-        K = torch.zeros((1, self.Hkv, n, self.dh), dtype=self.K[0].dtype, device=self.device)
-        V = torch.zeros_like(K)
-        for g, c in enumerate(counts):
-            K[0, g, :c], V[0, g, :c] = self.K[g], self.V[g]
-        idx = torch.cat([torch.arange(c, dtype=torch.int32) for c in counts])[None].to(self.device)
-        offsets = torch.tensor([[sum(counts[:g]) for g in range(self.Hkv + 1)]], dtype=torch.int32, device=self.device)
-        return cache.store(K, V, start, idx=idx, offsets=offsets, stream=stream)
+        with cache._allocating(stream):
+            start = cache.new_lengths() if start is None else start
+            if self.budget_mode == "uniform":
+                return cache.store(self.K[None], self.V[None], start, stream=stream)
+            # heads of different lengths: one list of rows, head g's part from offsets[g]
+            counts = [int(k.shape[0]) for k in self.K]
+            n = max(max(counts), 1)
+            K = torch.zeros((1, self.Hkv, n, self.dh), dtype=self.K[0].dtype, device=self.device)
+            V = torch.zeros_like(K)
+            for g, c in enumerate(counts):
+                K[0, g, :c], V[0, g, :c] = self.K[g], self.V[g]
+            idx = torch.cat([torch.arange(c, dtype=torch.int32) for c in counts])[None].to(self.device)
+            offsets = torch.tensor([[sum(counts[:g]) for g in range(self.Hkv + 1)]], dtype=torch.int32,
+                                   device=self.device)
+            return cache.store(K, V, start, idx=idx, offsets=offsets, stream=stream)
 
     def _step_adaptive(self, Qw, K_chunk, V_chunk, WO, budget):
         Hkv, ln = self.Hkv, K_chunk.shape[1]

@@ -839,3 +839,28 @@ def test_chunked_prefill_into_a_cache_and_back(mode):
     assert int(off[-1]) == 50
     for h in range(Hkv):
         assert int(s.idx[0, int(off[h]):int(off[h + 1])].min()) >= int(valid[0, h])
+
+
+@pytest.mark.parametrize("mode", ["uniform", "adaptive"])
+def test_to_cache_on_a_stream_of_its_own(mode):
+    """All that to_cache launches goes to the stream it is given: a busy current stream does not hold any of it back."""
+    g = gen(14)
+    Hq, Hkv, dh, dm, w, n = 4, 2, 64, 64, 8, 90
+    ch = ChunkedPrefillCompressor(Hq=Hq, Hkv=Hkv, dh=dh, dm=dm, w=w, pool_k=3, dtype="bf16", budget_mode=mode)
+    ch.step(*(torch.randn(*s, generator=g).bfloat16().cuda() for s in (
+        (Hq, w, dh), (Hkv, n, dh), (Hkv, n, dh), (Hq, dh, dm))), 40 if mode == "uniform" else 80)
+    cache = PagedCache.allocate(nseq=1, Hq=Hq, Hkv=Hkv, dh=dh, dtype="bf16", rows=100)
+    blocks = [torch.full((1, Hkv), 77, dtype=torch.int32, device="cuda") for _ in range(64)]
+    del blocks                                       # what the allocator hands out next holds a wrong length
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)                   # about 0.2 s
+    lens = ch.to_cache(cache, stream=side)
+    side.synchronize()
+    assert not torch.cuda.default_stream().query()   # still asleep
+    torch.cuda.synchronize()
+    assert lens.cpu().tolist() == [[int(k.shape[0]) for k in ch.K]]
+    K, V = cache.load(lens, int(lens.max()))
+    for h in range(Hkv):
+        m = int(lens[0, h])
+        assert torch.equal(K[0, h, :m], ch.K[h]) and torch.equal(V[0, h, :m], ch.V[h])
