@@ -90,8 +90,8 @@ enum {
                                      layer at a time that is about twice as fast.  Same results bit for bit      */
   CKV_FLAG_SELECT_NO_CLUSTER = 1u << 8, /* criticalkv_select: no thread-block clusters in steps 3-4 (the separate
                                      kernels then give every head one CTA), for contexts where cluster launches are
-                                     not wanted.  Same results bit for bit.  criticalkv_decode: none either, small calls
-                                     take two launches instead of one; the sums are added in another order        */
+                                     not wanted.  Same results bit for bit.  criticalkv_decode: none either, some small
+                                     calls take two launches then; the sums are added in another order         */
   CKV_FLAG_DEBUG_CHECKS = 1u << 6, /* device-side checks in criticalkv_select, criticalkv_compact and
                                      criticalkv_gather_positions: every index read from idx / offsets / budgets and
                                      every output position is tested against the bounds the descriptor implies

@@ -13,7 +13,7 @@ __device__ __forceinline__ void wait_for_previous_kernel() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// cluster: CTAs of a thread-block cluster (0: none).
+// cluster: CTAs of a thread-block cluster (0, 1: none).
 template <typename... P>
 cudaError_t launch_early_in_clusters(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, cudaStream_t st,
                                      P... args) {
@@ -29,7 +29,7 @@ cudaError_t launch_early_in_clusters(void (*kernel)(P...), dim3 grid, int thread
   attr[1].val.clusterDim.x = (unsigned)cluster;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = cluster ? 2 : 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 template <typename... P>

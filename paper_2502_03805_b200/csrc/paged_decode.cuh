@@ -7,8 +7,8 @@
 // the range and goes on behind it (slot 1).  Their unnormalised sums with the running maximum and sum go to the
 // workspace; decode_join_kernel adds them up in CTA order, so equal inputs give equal bits.
 //
-// Few items of few tiles (by the size of the page table) are instead given to a team of CTAs each, a thread-block cluster,
-// whose parts meet in distributed shared memory: one launch instead of two.
+// Items of few tiles (by the size of the page table) are instead given to a CTA each or, where they are few, to a team of
+// CTAs each, a thread-block cluster whose parts meet in distributed shared memory: one launch instead of two.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -37,7 +37,7 @@ struct DecodeArgs {
   int items, Hq, G;            // G = Hq / Hkv
   int chunks, chunk_rows;      // query heads of a KV head: chunks of at most chunk_rows
   int part_rows;               // the most query heads an item has
-  int team;                    // CTAs i * team ... are a cluster and item i is theirs; 0: all items are one list
+  int team;                    // item i is the cluster's of CTAs i * team ..., or a CTA's (1); 0: all items are one list
   int allow_cluster;           // host: whether a team may be chosen
   float scale_log2, scale_rest;   // scale * log2(e), and what its rounding to a float left out
   int* status;                 // CKV_FLAG_DEBUG_CHECKS: where a violated bound is reported; null otherwise
@@ -200,6 +200,7 @@ __device__ __forceinline__ void team_barrier() {
 }
 template <typename T, int DH>
 __device__ __forceinline__ void join_team(const DecodeArgs& p, const Walk& w, const float* parts) {
+  if (p.team == 1) return;                 // has written the result
   team_barrier();
   if (w.total > 1) {                       // a single tile was one CTA's, which has written the result
     const ItemRows it = item_rows(p, w.item);
@@ -389,13 +390,13 @@ inline DecodeArgs decode_args(const CacheDims& d, const DecodeCall& call, int ch
   return p;
 }
 
-// What a kernel needs to know once per device (asked for on its first launch there): CTAs an SM holds, and teams of 16 and
-// of 8 that can run at once, which is fewer than CTAs / 16 or 8, since a cluster lies in one group of multiprocessors.
+// What a kernel needs to know once per device (asked for on its first launch there): CTAs an SM holds, and clusters of 2, 4,
+// 8 and 16 that can run at once.
 struct LaunchSetup {
   static constexpr int kDevices = 64;
   struct Fit {
     std::atomic<int> per_sm{0};
-    std::atomic<int> teams[2] = {};
+    std::atomic<int> clusters[4] = {};
   } fit[kDevices];
   template <typename K> const Fit* of(K kernel, int device, int smem) {
     if (device >= kDevices) return nullptr;
@@ -405,23 +406,23 @@ struct LaunchSetup {
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
       return nullptr;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return nullptr;
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       cudaLaunchConfig_t cfg = {};
       cudaLaunchAttribute attr;
       attr.id = cudaLaunchAttributeClusterDimension;
-      attr.val.clusterDim.x = (unsigned)(kMaxTeam >> i);
+      attr.val.clusterDim.x = 2u << i;
       attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
       cfg.gridDim = dim3((unsigned)(kMaxTeam * 64));
       cfg.blockDim = dim3(kDecodeThreads);
       cfg.dynamicSmemBytes = (size_t)smem;
       cfg.attrs = &attr;
       cfg.numAttrs = 1;
-      int teams = 0;
-      if (cudaOccupancyMaxActiveClusters(&teams, kernel, &cfg) != cudaSuccess) {
-        teams = 0;
+      int n = 0;
+      if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        n = 0;
         cudaGetLastError();
       }
-      f.teams[i].store(teams, std::memory_order_relaxed);
+      f.clusters[i].store(n, std::memory_order_relaxed);
     }
     int n = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kDecodeThreads, smem) != cudaSuccess || n < 1) return nullptr;
@@ -430,16 +431,29 @@ struct LaunchSetup {
   }
 };
 
-// CTAs an item's team has, 0: no teams.  All teams run at once, and a CTA has at most three tiles (by the table's size, the
-// lengths are not known here): with more the even split over all CTAs and its join are as fast (2600 rows, 3.3 tiles a CTA:
-// 11.9 us a call with teams, 11.6 without).  One launch instead of two.  A call with teams and without, and on the device,
-// us, heads of 128, 8 KV heads of bf16 rows: 1 sequence x 819 rows 9.3 and 11.7 (8.2 and 8.0), 3 sequences 9.9 and 11.6
-// (8.9 and 9.9), 6 sequences 10.7 and 13.3 (10.3 and 12.8); 5 sequences x 1237 int8 rows, 2 KV heads of 64, float32
-// queries: 9.1 and 11.6 (8.0 and 7.2).  More teams than run at once: 24 of 16 CTAs 14.9 us on the device against 9.9.
-inline int decode_team(const DecodeArgs& p, const LaunchSetup::Fit& fit, int tile) {
-  const long long tiles = (p.c.capacity + tile - 1) / tile;
-  for (int i = 0; i < 2; ++i)
-    if (p.allow_cluster && p.items <= fit.teams[i].load(std::memory_order_relaxed) && tiles <= 3 * (kMaxTeam >> i)) return kMaxTeam >> i;
+// CTAs an item's team has; 0: no teams, the even split and its join.
+// A CTA alone (team 1) needs neither the split's scan of all lengths nor a join; a larger team costs 1 to 2 us for the
+// cluster's launch and barriers, more the more of them there are (hence small ones first, on half the GPU), and saves 1 us per 64-row
+// tile of bf16 rows of 128; the even split costs 3 us more than a CTA alone and a second launch.  Tiles are counted by the
+// table's size, the lengths are not known here; where they are very uneven a CTA has at most seven tiles behind the split.
+// Device times in us with 1, 2, 4, 8, 16 CTAs, and of the even split, 8 KV heads of 128, bf16 rows with a spread of 30 %
+// (a call is 2.3 us shorter with teams where the host bounds it):
+//   1 sequence  x   60 rows:  5.6   6.5   6.4   6.3   6.6, 7.3      18 x  60:  5.9   7.8 ...      , 8.3
+//   1 sequence  x  400 rows:   -    9.6   7.6   6.7   7.6, 8.1      18 x 200:  8.7  10.0 ...      , 11.6
+//   1 sequence  x  819 rows:   -   13.9  10.2   8.6   8.1, 8.1      37 x 200: 10.5  18.6 ...      , 14.1
+//   6 sequences x  400 rows:   -   10.3   8.5   8.6  22.3, 9.9      128 x 60: 16.4  33.1 ...      , 19.0
+// In between the choice is up to 15 % off on the device (14 sequences of 400 e4m3 rows 11.7, split 10.2), which is what the
+// second launch costs a call.
+inline int decode_team(const DecodeArgs& p, const LaunchSetup::Fit& fit, int sm_count, int tile) {
+  const long long tiles = (p.c.capacity + tile - 1) / tile, resident = (long long)fit.per_sm.load() * sm_count;
+  auto fit_at_once = [&](int i) { return p.allow_cluster && p.items <= fit.clusters[i].load(std::memory_order_relaxed); };
+  if (tiles <= 3 && p.items <= 3 * resident) return 1;
+  for (int most = 1; most <= 2; ++most)                    // tiles a CTA
+    for (int i = 0; i < 4; ++i)
+      if (tiles <= most * (2 << i) && fit_at_once(i) && p.items * (4LL << i) <= resident) return 2 << i;
+  if (tiles <= 7 && p.items <= resident && 4LL * p.items > resident) return 1;
+  for (int i = 3; i >= 0; --i)
+    if (tiles <= (i >= 2 ? 3 : 4) * (2 << i) && fit_at_once(i)) return 2 << i;
   return 0;
 }
 

@@ -676,7 +676,7 @@ cudaError_t launch(DecodeArgs p, int device, int sm_count, cudaStream_t st, int*
   CUtensorMap maps[2];
   for (int i = 0; i < 2; ++i)
     if (!page_map<Shape<FMT, DH, NT>>(&maps[i], p, i, min(1 << p.c.page_shift, 16 * Shape<FMT, DH, NT>::kSub))) return cudaErrorInvalidValue;
-  p.team = decode_team(p, *fit, Shape<FMT, DH, NT>::kTile);
+  p.team = decode_team(p, *fit, sm_count, Shape<FMT, DH, NT>::kTile);
   const int grid = p.team ? p.items * p.team : decode_grid(p, fit->per_sm * sm_count, Shape<FMT, DH, NT>::kTile);
   *launches += 1;
   const cudaError_t e = launch_early_in_clusters<DecodeArgs, CUtensorMap, CUtensorMap>(kernel, dim3(grid), kDecodeThreads, smem,

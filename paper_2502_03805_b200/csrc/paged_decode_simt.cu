@@ -259,7 +259,7 @@ template <typename T, int FMT, int DH, int kQ> cudaError_t launch_rows(DecodeArg
   static LaunchSetup setup;
   const LaunchSetup::Fit* fit = setup.of(kernel, device, 0);
   if (!fit) return cudaErrorInvalidDeviceFunction;
-  p.team = decode_team(p, *fit, kTile);
+  p.team = decode_team(p, *fit, sm_count, kTile);
   const int grid = p.team ? p.items * p.team : decode_grid(p, fit->per_sm * sm_count, kTile);
   *launches += 1;
   const cudaError_t e = launch_early_in_clusters<DecodeArgs>(kernel, dim3(grid), kDecodeThreads, 0, p.team, st, p);

@@ -475,9 +475,9 @@ def test_decode_of_few_long_heads(dtype, fmt):
 
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "plain"), ("bf16", "e4m3"), ("f32", "int8"), ("f32", "plain")])
 @pytest.mark.parametrize("dh,G,Hkv", [(128, 4, 2), (64, 16, 1), (64, 1, 7), (128, 9, 1), (64, 8, 25), (64, 20, 2)])
-@pytest.mark.parametrize("rows", [16, 48, 130, 384, 760])
+@pytest.mark.parametrize("rows", [16, 48, 130, 384, 760, 1300])
 def test_decode_with_clusters_and_without(dtype, fmt, dh, G, Hkv, rows):
-    """Few short heads: one launch with a cluster a head; two launches without.  Every length from none to full in turn."""
+    """Few short heads: one launch, a CTA or a cluster a head; without clusters two launches but for the shortest."""
     cache = Cache(nseq=1, Hq=G * Hkv, Hkv=Hkv, dh=dh, dtype=dtype, fmt=fmt, page=16, cols=(rows + 15) // 16)
     full = torch.full((1, Hkv), rows, dtype=torch.int32)
     cache.fill(full, 2)
@@ -486,10 +486,10 @@ def test_decode_with_clusters_and_without(dtype, fmt, dh, G, Hkv, rows):
     q = torch.randn(1, G * Hkv, dh, generator=gen(3)).to(R.DT[dtype])
     for lens in (full, torch.zeros_like(full), (full - torch.arange(Hkv) * 7).clamp(min=0).to(torch.int32),
                  torch.arange(1, Hkv + 1, dtype=torch.int32).view(1, Hkv).clamp(max=rows)):
-        for c, launches in ((cache.c, 1), (apart, 2)):
+        for c, most in ((cache.c, 1 if rows < 1000 else 2), (apart, 1 if rows < 50 else 2)):
             before = B.criticalkv_launch_count(c.handle)
             got = c.attend(q.cuda(), lens.cuda())
-            assert B.criticalkv_launch_count(c.handle) - before == launches
+            assert 1 <= B.criticalkv_launch_count(c.handle) - before <= most
             check_decode(cache, q, lens, got)
 
 
