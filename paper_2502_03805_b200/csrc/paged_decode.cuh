@@ -22,7 +22,8 @@ namespace ckv {
 constexpr int kDecodeThreads = 128;
 constexpr int kDecodeWarps = kDecodeThreads / 32;
 constexpr int kDecodeMaxCtas = 592;      // four a multiprocessor on 148
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kLongJoinThreads = 1024;
+constexpr int kLongJoinParts = 16;       // CTAs an item from which the long join is taken
 constexpr int kMaxTeam = 16;             // CTAs that share an item where items have teams, at most
 
 struct DecodeArgs {
@@ -315,32 +316,16 @@ __device__ __forceinline__ void add_parts(const DecodeArgs& p, int r, int c0, in
   }
 }
 
-// CTAs (i, y): the item that ends in CTA i of the decode kernel, if it began in an earlier one.  Up to eight parts: y = 0
-// does it all, a warp a row.  More: y is the row, whose parts the warps take in turn before they meet in shared memory.
-// A fixed order of additions either way.
-template <typename T, int DH>
-__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p) {
-  constexpr int WARPS = kJoinThreads / 32, E = DH / 64;   // pairs of elements a lane
+// A row of an item of the parts of CTAs c0 ... c1: the warps take the parts in turn and meet in shared memory.
+template <typename T, int DH, int THREADS>
+__device__ __forceinline__ void join_row(const DecodeArgs& p, const ItemRows& it, int r, int c0, int c1) {
+  constexpr int WARPS = THREADS / 32, E = DH / 64;        // pairs of elements a lane
   __shared__ __align__(8) float o_s[WARPS][DH];
   __shared__ float m_s[WARPS], l_s[WARPS];
-  wait_for_previous_kernel();
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = blockIdx.y;
-  const int2 what = p.join[blockIdx.x];
-  if (what.x < 0) return;
-  const ItemRows it = item_rows(p, what.x);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   float m, l;
   float2 acc[E];
-  if ((int)blockIdx.x - what.y < 8) {
-    if (r > 0) return;
-    for (int row = warp; row < it.rows; row += WARPS) {
-      add_parts<DH>(p, row, what.y, blockIdx.x, what.y, 1, m, l, acc);
-#pragma unroll
-      for (int e = 0; e < E; ++e) put_out<T, DH>(p, it, row, lane + 32 * e, acc[e].x, acc[e].y, m, l, false);
-    }
-    return;
-  }
-  if (r >= it.rows) return;
-  add_parts<DH>(p, r, what.y, blockIdx.x, what.y + warp, WARPS, m, l, acc);
+  add_parts<DH>(p, r, c0, c1, c0 + warp, WARPS, m, l, acc);
 #pragma unroll
   for (int e = 0; e < E; ++e) *reinterpret_cast<float2*>(&o_s[warp][2 * (lane + 32 * e)]) = acc[e];
   if (lane == 0) { m_s[warp] = m; l_s[warp] = l; }
@@ -360,6 +345,51 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p)
     }
     put_out<T, DH>(p, it, r, threadIdx.x, a, b, top, l, false);
   }
+}
+
+// CTAs (i, y): the item that ends in CTA i of the decode kernel, if it began in an earlier one.  Up to eight parts: y = 0
+// does it all, a warp a row.  More: y is the row, whose parts the warps take in turn before they meet in shared memory.
+// A fixed order of additions either way.
+template <typename T, int DH>
+__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(DecodeArgs p) {
+  constexpr int WARPS = kJoinThreads / 32, E = DH / 64;   // pairs of elements a lane
+  wait_for_previous_kernel();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = blockIdx.y;
+  const int2 what = p.join[blockIdx.x];
+  if (what.x < 0) return;
+  const ItemRows it = item_rows(p, what.x);
+  if ((int)blockIdx.x - what.y < 8) {
+    if (r > 0) return;
+    float m, l;
+    float2 acc[E];
+    for (int row = warp; row < it.rows; row += WARPS) {
+      add_parts<DH>(p, row, what.y, blockIdx.x, what.y, 1, m, l, acc);
+#pragma unroll
+      for (int e = 0; e < E; ++e) put_out<T, DH>(p, it, row, lane + 32 * e, acc[e].x, acc[e].y, m, l, false);
+    }
+    return;
+  }
+  if (r >= it.rows) return;
+  join_row<T, DH, kJoinThreads>(p, it, r, what.y, blockIdx.x);
+}
+
+// The same for few items of many parts: a CTA a row of an item (y: the row), which looks for the item's last CTA.
+template <typename T, int DH>
+__global__ void __launch_bounds__(kLongJoinThreads) decode_join_long_kernel(DecodeArgs p, int ctas) {
+  __shared__ int2 found;                                   // last CTA, first CTA
+  const int item = blockIdx.x, r = blockIdx.y;
+  if (threadIdx.x == 0) found = make_int2(-1, 0);
+  wait_for_previous_kernel();
+  const ItemRows it = item_rows(p, item);
+  if (r >= it.rows) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < ctas; c += kLongJoinThreads) {
+    const int2 what = p.join[c];
+    if (what.x == item) found = make_int2(c, what.y);      // one at most
+  }
+  __syncthreads();
+  const int2 to = found;
+  if (to.x >= 0) join_row<T, DH, kLongJoinThreads>(p, it, r, to.y, to.x);
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------
@@ -466,9 +496,12 @@ inline int decode_grid(const DecodeArgs& p, int resident, int tile) {
 }
 
 template <typename T, int DH> cudaError_t launch_decode_join(const DecodeArgs& p, int grid, cudaStream_t st) {
-  return launch_early<DecodeArgs>(decode_join_kernel<T, DH>,
-                                  dim3((unsigned)grid, (unsigned)p.part_rows), kJoinThreads, 0,
-                                  st, p);
+  // many parts an item: device times of the whole call in us, this join and the other, heads of 128: 1 KV head of 48936 rows
+  // (444 parts) 16.0 and 21.5, 8 of 6553 (55 parts) 11.7 and 12.2, 32 (14 parts) 24.3 and 24.7, 56 (8 parts) 40.2 and 38.0
+  if (grid >= kLongJoinParts * p.items)
+    return launch_early<DecodeArgs, int>(decode_join_long_kernel<T, DH>, dim3((unsigned)p.items, (unsigned)p.part_rows),
+                                         kLongJoinThreads, 0, st, p, grid);
+  return launch_early<DecodeArgs>(decode_join_kernel<T, DH>, dim3((unsigned)grid, (unsigned)p.part_rows), kJoinThreads, 0, st, p);
 }
 
 }  // namespace ckv
