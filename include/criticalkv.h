@@ -369,8 +369,10 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
  * k_i) (lse may be NULL; it is what merging with attention over other keys needs).  A head without rows gives zeros and
  * -infinity; one that has rows but none in an existing page, or only logits of -infinity, gives NaN; rows with infinite or
  * NaN values give results that are not finite.  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
- * bf16 queries run on tensor cores (stored 8-bit values enter exactly, sums and the softmax are float32); float32
- * queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores.  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) * ceil(max_pages *
+ * bf16 queries run on tensor cores: stored 8-bit values enter exactly, sums and the softmax are float32, and a weight
+ * enters its product with the values rounded to 16 bits (plain pages) or, times the row's scale, to 22 bits and no finer than
+ * 2^-40 of the head's largest such product (8-bit pages).  float32 queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores,
+ * in float32 throughout.  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) * ceil(max_pages *
  * page_size / 64) exceeds 2^31 - 1.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
  * needs no initialisation; calls that may overlap on the GPU need workspaces of their own.
  */

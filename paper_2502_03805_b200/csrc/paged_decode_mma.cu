@@ -18,15 +18,16 @@
 // after V^T P^T, also across the end of an item: 8 KB a warp and 12 warps an SM are on their way.  The 128-byte swizzle
 // and the order of the rows (row_of) keep both reads free of bank conflicts.
 // Softmax statistics are float32; the running maximum is only reduced over the warp (and the sums only rescaled) in
-// steps in which some lane sees a larger logit.  The weights enter the second product as the sum of two bf16 numbers
-// (16 bits) for bf16 pages; for 8-bit pages, whose codes are exact halves, as halves (11 bits) of weight * scale of the
-// row / the largest such product so far, so that rows of very different norms keep their precision.  The queries of
+// steps in which some lane sees a larger logit.  The weights enter the second product as the sum of two 16-bit numbers:
+// for bf16 pages two bf16 (16 bits); for 8-bit pages, whose codes are exact halves, two halves (22 bits) of weight * scale
+// of the row * 2^15 / the largest such product so far.  What is below 2^-40 of that largest product is lost, so rows of very
+// different norms and long tails of small weights keep theirs.  The queries of
 // 8-bit pages become halves after a scaling by a power of two that puts the largest of a row at 2^14: exact but for
 // elements 2^-29 below it.
 //
 // Measured: 2 x 131072 bf16 rows a head, 40 query heads on 8, 168 us, 6.4 TB/s (0.98 of the copy bandwidth); 32 x 6553
-// e4m3 rows a head, 32 query heads on 8, 82 us, 5.5 TB/s (0.85), bound by instruction latency: 168 registers leave three
-// CTAs an SM, and with 128 the sums spill (122 us).  1 x 819 bf16 rows: 7.9 us, a chain of latencies.
+// e4m3 rows a head, 32 query heads on 8, 87 us, 5.2 TB/s (0.80; 82 us with weights of 11 bits, whose error is seen where
+// values cancel), bound by instruction latency: 168 registers leave three CTAs an SM, and with 128 the sums spill (122 us).  1 x 819 bf16 rows: 7.9 us, a chain of latencies.
 #include "paged_decode.cuh"
 #include "sm100_ptx.cuh"
 #include "tma_host.h"
@@ -76,6 +77,10 @@ template <int FMT> __device__ __forceinline__ void codes_to_halves(uint32_t four
     high = *reinterpret_cast<const uint32_t*>(&y);
   }
 }
+
+// The largest product of a weight and a row's scale so far, as a half (8-bit pages): the top of the range, so that a long
+// tail of small weights keeps its part of the sums.
+constexpr float kTopWeight = 32768.f;
 
 template <int FMT, int DH, int NT> struct Shape {
   static constexpr bool kPlain = FMT == CKV_CACHE_PLAIN;
@@ -328,7 +333,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
     }
 
     float o[NT][S::kMTiles][4];
-    // running maximum, this lane's share of the sum, largest weight * scale so far and its inverse
+    // running maximum, this lane's share of the sum, largest weight * scale so far and kTopWeight / that
     float m[NT][2], l[NT][2], big[NT][2], inv[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -482,16 +487,23 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
               most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 4));
               most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 8));
               most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 16));
-              inv[n][x] = most[x] > 0.f ? __frcp_rn(most[x]) : 0.f;
-              f[x] = big[n][x] * inv[n][x];
+              const float one = most[x] > 0.f ? __frcp_rn(most[x]) : 0.f;
+              f[x] = big[n][x] * one;
               big[n][x] = most[x];
+              inv[n][x] = one * kTopWeight;
             }
           }
 #pragma unroll
           for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              w_hi[n][u][h] = transpose8(pack_half(s[n][u][2 * h] * inv[n][0], s[n][u][2 * h + 1] * inv[n][1]));
+            {
+              const float a = s[n][u][2 * h] * inv[n][0], b = s[n][u][2 * h + 1] * inv[n][1];
+              const __half2 hi = __floats2half2_rn(a, b);
+              const float2 back = __half22float2(hi);
+              w_hi[n][u][h] = transpose8(*reinterpret_cast<const uint32_t*>(&hi));
+              w_lo[n][u][h] = transpose8(pack_half(a - back.x, b - back.y));
+            }
         }
         if (moved) {
 #pragma unroll
@@ -552,10 +564,14 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
               }
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
 #pragma unroll
               for (int e = 0; e < 2; ++e)
                 mma_f16(o[n][i + e], a[e][0], a[e][1], a[e][2], a[e][3], w_hi[n][u][0], w_hi[n][u][1]);
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                mma_f16(o[n][i + e], a[e][0], a[e][1], a[e][2], a[e][3], w_lo[n][u][0], w_lo[n][u][1]);
+            }
           }
         }
       }
@@ -590,7 +606,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
           sh.l[warp][row] = sum * f;
           if (warp == 0) sh.top[row] = top;
         }
-        big[n][x] = S::kPlain ? f : f * big[n][x];         // factor of the sums
+        big[n][x] = S::kPlain ? f : f * (big[n][x] * (1.f / kTopWeight));   // factor of the sums
       }
     const bool whole = seg.t0 == 0 && seg.t1 == seg.tiles;
 #pragma unroll
