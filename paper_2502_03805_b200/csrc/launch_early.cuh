@@ -7,7 +7,9 @@
 namespace ckv {
 
 // Every kernel that is launched early calls this first: nothing but its own shared memory is touched before it, so
-// that nothing is read before it is written and nothing overwritten before it is read.
+// that nothing is read before it is written and nothing overwritten before it is read.  Loads for data that is constant
+// while a kernel runs (__ldg, ld.global.nc, what const __restrict__ pointers become) are not for these kernels: the one in
+// front may still write while they are resident, and such a load is held behind the wait by nothing.
 __device__ __forceinline__ void wait_for_previous_kernel() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

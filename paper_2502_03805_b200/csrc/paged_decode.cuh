@@ -113,7 +113,7 @@ __device__ __forceinline__ Walk plan(const DecodeArgs& p) {
   bool bad = false, empty = false;
 #pragma unroll 4
   for (int j = lo; j < hi; ++j) {
-    const int given = __ldg(p.lens + kv_of(p, j));
+    const int given = p.lens[kv_of(p, j)];
     const int len = (int)min(max((long long)given, 0LL), p.c.capacity);
     bad = bad || len != given;
     empty = empty || len == 0;

@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
     for (int u = 0; u < SUB; ++u) {
       w.page[u] = -1;
       if (u == 0 || (together < SUB && u % together == 0)) {
-        if (w.here > 16 * u) w.page[u] = __ldg(pages + ((base + 16 * u) >> p.c.page_shift));
+        if (w.here > 16 * u) w.page[u] = pages[(base + 16 * u) >> p.c.page_shift];
       }
     }
   };
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
 #pragma unroll
         for (int h = 0; h < S::kQWords / 4; ++h) {
           uint4 v = make_uint4(0, 0, 0, 0);
-          if (row < it.rows) v = __ldg(reinterpret_cast<const uint4*>(src + 16 * S::kQWords * j + 16 * h));
+          if (row < it.rows) v = *reinterpret_cast<const uint4*>(src + 16 * S::kQWords * j + 16 * h);
           q[n][j][4 * h] = v.x; q[n][j][4 * h + 1] = v.y; q[n][j][4 * h + 2] = v.z; q[n][j][4 * h + 3] = v.w;
         }
     }

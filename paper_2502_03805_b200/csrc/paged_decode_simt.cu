@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_k
     const int32_t* pages = p.c.table + (long long)it.kv * p.c.max_pages;
     const auto page_of = [&](int tile) {        // page_size is a multiple of 16: a warp's rows lie in one page
       const int base = tile * kTile + warp * kWarpRows;
-      return tile < t1 && base < len ? __ldg(pages + (base >> p.c.page_shift)) : 0;
+      return tile < t1 && base < len ? pages[base >> p.c.page_shift] : 0;
     };
     int page = page_of(t0);
     for (int tile = t0; tile < t1; ++tile) {
