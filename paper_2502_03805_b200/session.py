@@ -79,10 +79,21 @@ class CompressionSession:
 
     def compact_into(self, cache, K, V, start, lens_out=None, stream=None):
         """Step 5 into a PagedCache (quantised where its format says so) instead of K_out, V_out: the selected rows of
-        K, V go behind row start[b, g] of every head; returns the new lengths."""
-        idx = self.idx[:, :self.btot]
-        # like the other calls of a session: no stream is the default stream, whatever stream is current
-        return cache.store(K, V, start, lens_out, idx=idx, offsets=self.offsets, stream=0 if stream is None else stream)
+        K, V go behind row start[b, g] of every head; returns the new lengths.  Without a stream it works on the default
+        one, like the other calls of a session; where another stream is current (the one a cache's and a rotary's calls
+        take), each of the two waits for the other."""
+        kw = dict(idx=self.idx[:, :self.btot], offsets=self.offsets)
+        if stream is not None:
+            return cache.store(K, V, start, lens_out, stream=stream, **kw)
+        if lens_out is None:      # of the current stream, on which the caller goes on
+            lens_out = torch.empty((cache.nseq, cache.Hkv), dtype=torch.int32, device=cache.device)
+        default, current = torch.cuda.default_stream(self.device), torch.cuda.current_stream(self.device)
+        if current != default:
+            default.wait_stream(current)
+        cache.store(K, V, start, lens_out, stream=0, **kw)
+        if current != default:
+            current.wait_stream(default)
+        return lens_out
 
     def compress(self, Qw, K, V, WO, budgets_in=None, stream=None):
         return B.criticalkv_compress(self.handle, self.desc, Qw, K, V, WO, budgets_in, self.attn, self.vnorm,
@@ -158,9 +169,14 @@ class ChunkedPrefillCompressor:
 
     def to_cache(self, cache, start=None, stream=None):
         """Writes the retained rows into a PagedCache of one sequence (decoding starts from there) and returns the
-        lengths of its heads.  All of it is done on `stream` (None: the current one), on which the rows must be ready."""
+        lengths of its heads.  All of it is done on `stream`, on which the rows must be ready, or without one on the
+        current stream, which then waits for the default stream, the one step() compresses on."""
         if self.K is None:
             raise ValueError("nothing has been compressed yet")
+        if stream is None:
+            default, current = torch.cuda.default_stream(self.device), torch.cuda.current_stream(self.device)
+            if current != default:
+                current.wait_stream(default)
         with cache._allocating(stream):
             start = cache.new_lengths() if start is None else start
             if self.budget_mode == "uniform":
