@@ -2,7 +2,8 @@
 
 Device-buffer plumbing around the C ABI, like session.py: shapes, types and devices of tensors are checked here, every
 number is computed by the kernels of libcriticalkv.  Work goes to torch's current stream of the tensors' device unless
-a stream is given.
+a stream is given.  The tensors of a call must be ready on that stream; what an object keeps for itself (pages, tables,
+frequencies, workspaces) may be dropped while calls are in flight.
 """
 from __future__ import annotations
 
@@ -19,6 +20,8 @@ _NAME = {v: k for k, v in _TORCH_DTYPE.items()}
 _NOTHING = contextlib.nullcontext()
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (     # handle of a device's current stream
     lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_capturing = torch.cuda.is_current_stream_capturing
 _CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
 
 
@@ -40,6 +43,7 @@ class _Owner:
         self._owned = handle is None
         self.handle = B.criticalkv_create(device.index) if handle is None else handle
         self._plans = {}
+        self._seen = set()               # streams that the tensors the object keeps are recorded on
         self._lib = B.load()
         self._index = device.index
 
@@ -65,14 +69,29 @@ class _Owner:
             return _raw_stream(self._index)
         return stream if isinstance(stream, int) else stream.cuda_stream
 
+    def _torch_stream(self, stream):
+        if stream is None:
+            return torch.cuda.current_stream(self.device)
+        if isinstance(stream, int):
+            return torch.cuda.ExternalStream(stream, device=self.device) if stream else \
+                torch.cuda.default_stream(self.device)
+        return stream
+
     def _allocating(self, stream):
         """Where outputs of a call on `stream` are allocated and cleared: on that stream, not on the current one."""
-        if stream is None:
-            return _NOTHING
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=self.device) if stream else \
-                torch.cuda.default_stream(self.device)
-        return torch.cuda.stream(stream)
+        return _NOTHING if stream is None else torch.cuda.stream(self._torch_stream(stream))
+
+    def _where(self, stream):
+        """The stream of a call for the C ABI.  On its first call there, the tensors that the object keeps are recorded on
+        it: their memory is not handed out again before the work in flight on it at their end is done."""
+        raw = _raw_stream(self._index) if stream is None else self._on(stream)
+        if raw not in self._seen:
+            at = self._torch_stream(stream)
+            for t in self._kept():
+                if t is not None:
+                    t.record_stream(at)
+            self._seen.add(raw)
+        return raw
 
     def _fail(self, rc, where):
         B._check(self.handle, rc, where, True)
@@ -187,11 +206,13 @@ class Rotary(_Owner):
                positions.get_device(), q_out.dtype, q_out.shape, q_out.stride(), q_out.get_device(), _sig(k_out))
         desc = self._plans.get(key) or self._keep(key, self._describe(q, k, positions, q_out, k_out))
         rc = self._rope(self.handle, desc, q.data_ptr(), None if k is None else k.data_ptr(), positions.data_ptr(),
-                        self._freq_at, q_out.data_ptr(), None if k is None else k_out.data_ptr(),
-                        _raw_stream(self._index) if stream is None else self._on(stream))
+                        self._freq_at, q_out.data_ptr(), None if k is None else k_out.data_ptr(), self._where(stream))
         if rc:
             self._fail(rc, "criticalkv_rope")
         return q_out, k_out
+
+    def _kept(self):
+        return (self.freq,)
 
     def _describe(self, q, k, positions, q_out, k_out):
         """Checks the tensors of a call and describes them to the C ABI."""
@@ -260,7 +281,7 @@ class PagedCache(_Owner):
                                  page_table=page_table, k_scale=k_scale, v_scale=v_scale, page_stride=strides[0],
                                  scale=scale, flags=flags)
         self._ws_bytes = B.criticalkv_decode_workspace_bytes(self.desc)   # also refuses a bad description
-        self._ws = None
+        self._ws = {}                    # workspaces by stream
         self._out_shape = (nseq, Hq, dh)
         # what attend's outputs look like: torch.empty_like costs half of torch.empty with a shape, a type and a device
         self._out_like = torch.empty(self._out_shape, dtype=self.torch_dtype, device=dev)
@@ -285,6 +306,9 @@ class PagedCache(_Owner):
         return cls(Hq=Hq, dtype=dtype, format=format, k_pages=pages[0], v_pages=pages[1], k_scale=scales[0],
                    v_scale=scales[1], page_table=table, **kw)
 
+    def _kept(self):
+        return self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table
+
     def new_lengths(self):
         """Lengths of an empty cache."""
         return torch.zeros((self.nseq, self.Hkv), dtype=torch.int32, device=self.device)
@@ -306,7 +330,7 @@ class PagedCache(_Owner):
         rc = self._store(
             self.handle, self._ref, K.data_ptr(), V.data_ptr(), n, strides, None if idx is None else idx.data_ptr(),
             None if offsets is None else offsets.data_ptr(), idx_rows, None if counts is None else counts.data_ptr(),
-            start.data_ptr(), lens_out.data_ptr(), _raw_stream(self._index) if stream is None else self._on(stream))
+            start.data_ptr(), lens_out.data_ptr(), self._where(stream))
         if rc:
             self._fail(rc, "criticalkv_cache_store")
         return lens_out
@@ -350,7 +374,7 @@ class PagedCache(_Owner):
                K_out.get_device(), V_out.dtype, V_out.shape, V_out.stride(), V_out.get_device())
         n, strides = self._plans.get(key) or self._keep(key, self._describe_load(lens, n, K_out, V_out))
         rc = self._load(self.handle, self._ref, lens.data_ptr(), n, strides, 1 if align_right else 0, K_out.data_ptr(),
-                        V_out.data_ptr(), _raw_stream(self._index) if stream is None else self._on(stream))
+                        V_out.data_ptr(), self._where(stream))
         if rc:
             self._fail(rc, "criticalkv_cache_load")
         return K_out, V_out
@@ -368,12 +392,30 @@ class PagedCache(_Owner):
             raise ValueError("K_out and V_out must have the same strides")
         return n, B._strides(strides)
 
-    def workspace(self):
-        """The decode workspace: allocated on first use and kept.  Calls of this object that may overlap on the GPU
-        (different streams, graphs replayed side by side) need `ws` arguments of their own."""
-        if self._ws is None:
-            self._ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
-        return self._ws
+    def workspace(self, stream=None):
+        """The decode workspace of a stream (None: the current one): allocated there on first use and kept.  Calls on
+        different streams have different ones, and while a stream is captured every call gets a new one from the graph's
+        memory, so that neither two graphs nor a graph and other calls share any."""
+        if stream is None:
+            return self._workspace(_raw_stream(self._index))
+        with self._allocating(stream):
+            return self._workspace(self._on(stream))
+
+    def _workspace(self, raw):
+        """raw: the current stream."""
+        if _current_device() == self._index:
+            captured = _capturing()
+        else:
+            with torch.cuda.device(self._index):
+                captured = _capturing()
+        if captured:
+            return torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
+        ws = self._ws.get(raw)
+        if ws is None:
+            if len(self._ws) >= 64:      # streams that come and go
+                self._ws.clear()
+            ws = self._ws[raw] = torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
+        return ws
 
     def attend(self, q, lens, out=None, lse=None, *, ws=None, stream=None):
         """Attention of one new token per sequence: q [nseq, Hq, dh] over the lens[s, g] rows of every head.  Returns
@@ -381,17 +423,18 @@ class PagedCache(_Owner):
         key = (q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(), lens.get_device(),
                _sig(out), _sig(lse), _sig(ws))
         strides, size = self._plans.get(key) or self._keep(key, self._describe_attend(q, lens, out, lse, ws))
+        raw = self._where(stream)
         if stream is None:
             out = torch.empty_like(self._out_like) if out is None else out
             lse = torch.empty_like(self._lse_like) if lse is None else lse
-            ws = self.workspace() if ws is None else ws
+            ws = self._workspace(raw) if ws is None else ws
         else:
             with self._allocating(stream):
                 out = torch.empty_like(self._out_like) if out is None else out
                 lse = torch.empty_like(self._lse_like) if lse is None else lse
-                ws = self.workspace() if ws is None else ws
+                ws = self._workspace(raw) if ws is None else ws
         rc = self._decode(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                          ws.data_ptr(), size, _raw_stream(self._index) if stream is None else self._on(stream))
+                          ws.data_ptr(), size, raw)
         if rc:
             self._fail(rc, "criticalkv_decode")
         return out, lse

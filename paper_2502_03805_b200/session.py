@@ -177,6 +177,10 @@ class ChunkedPrefillCompressor:
             default, current = torch.cuda.default_stream(self.device), torch.cuda.current_stream(self.device)
             if current != default:
                 current.wait_stream(default)
+        for rows in (self.K, self.V):      # the next step drops them, perhaps before they have been read
+            for x in (rows if isinstance(rows, list) else [rows]):
+                if x.is_cuda:
+                    x.record_stream(cache._torch_stream(stream))
         with cache._allocating(stream):
             start = cache.new_lengths() if start is None else start
             if self.budget_mode == "uniform":
