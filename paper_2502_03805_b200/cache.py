@@ -130,6 +130,18 @@ def _row_strides(t, what):
     return tuple(out[:0:-1])
 
 
+def _page_stride(t, what):
+    """Elements from page to page of a pool whose pages are contiguous and apart (the C ABI takes 0 for dense)."""
+    _, page_size, dh = t.shape
+    if t.is_contiguous():
+        return page_size * dh
+    if t.stride(2) != 1 or t.stride(1) != dh:
+        raise ValueError(f"{what}: the rows of a page must be contiguous")
+    if t.stride(0) < page_size * dh:
+        raise ValueError(f"{what}: pages expanded or laid over each other are not supported")
+    return t.stride(0)
+
+
 def rope_frequencies(rot, base=10000.0, scaling=None, *, factor=1.0, original=8192, low=1.0, high=4.0, beta_fast=32.0,
                      beta_slow=1.0):
     """Radians per position of the rot/2 pairs, as a float64 CPU tensor: base^(-2i/rot), adjusted for long contexts.
@@ -260,9 +272,7 @@ class PagedCache(_Owner):
         strides = []
         for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
             _need(t, what, k_pages.shape, code, dev, dense=False)
-            if not t.is_contiguous() and (t.stride(2) != 1 or t.stride(1) != dh):
-                raise ValueError(f"{what}: the rows of a page must be contiguous")
-            strides.append(page_size * dh if t.is_contiguous() else t.stride(0))
+            strides.append(_page_stride(t, what))
         if strides[0] != strides[1]:
             raise ValueError("k_pages and v_pages must have the same page stride")
         if (k_scale is None) != (format == "plain") or (v_scale is None) != (format == "plain"):
