@@ -347,7 +347,8 @@ CKV_API int criticalkv_rope(criticalkv_handle h, const criticalkv_rope_desc* d, 
  *   idx == NULL   rows 0..c-1, c = counts[s] (device int32 [nseq]) or n when counts is NULL;
  *   idx != NULL   rows idx[s, offsets[s,g] .. offsets[s,g+1]), the result of criticalkv_select (idx [nseq, idx_rows],
  *                 offsets [nseq, Hkv+1]); counts must be NULL.
- * lens_out[s, g] (may be NULL, may be `start` itself) = start + rows written, at most max_pages * page_size.  Other
+ * lens_out[s, g] (may be NULL, may be `start` itself, and must not overlap anything else that the call reads) = start +
+ * rows written, at most max_pages * page_size.  Other
  * rows of the pages keep their contents.  No page may be listed twice among the rows that one call writes.
  */
 CKV_API int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* c, const void* K, const void* V,

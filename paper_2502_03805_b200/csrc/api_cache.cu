@@ -13,6 +13,12 @@ using ckv::record_cuda;
 
 inline bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// Whether two arrays of int32 share memory.
+inline bool overlap(const int32_t* a, long long na, const int32_t* b, long long nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + 4 * (uintptr_t)nb && y < x + 4 * (uintptr_t)na;
+}
+
 int resolve_cache(const criticalkv_cache* c, CacheDims* o) {
   if (!c) return CKV_EINVAL;
   if (c->nseq < 0 || c->Hq < 1 || c->Hkv < 1 || c->Hq % c->Hkv != 0) return CKV_EINVAL;
@@ -124,9 +130,12 @@ int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* c, const
   if (!aligned16(K) || !aligned16(V) || !aligned_to(idx, 4) || !aligned_to(offsets, 4) || !aligned_to(counts, 4) ||
       !aligned_to(start, 4) || !aligned_to(lens_out, 4))
     return CKV_EALIGN;
-  // lens_out is start itself or another array
-  const long long apart = (const char*)lens_out - (const char*)start, size = 4LL * d.nseq * d.Hkv;
-  if (lens_out && apart != 0 && apart < size && apart > -size) return CKV_EINVAL;
+  // lens_out is start itself or an array apart from everything that the kernel reads while it is written
+  const long long heads = (long long)d.nseq * d.Hkv;
+  if (lens_out && ((lens_out != start && overlap(lens_out, heads, start, heads)) || overlap(lens_out, heads, counts, d.nseq) ||
+                   overlap(lens_out, heads, offsets, heads + d.nseq) || overlap(lens_out, heads, idx, d.nseq * (long long)idx_rows) ||
+                   overlap(lens_out, heads, d.page_table, heads * d.max_pages)))
+    return CKV_EINVAL;
   DeviceGuard guard(h->device);
   if (!guard.ok) return CKV_ECUDA;
   int launches = 0;

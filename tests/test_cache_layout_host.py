@@ -1,7 +1,11 @@
 """Pools of pages as the library is told of them."""
+import ctypes as C
+
 import pytest
 import torch
 
+from paper_2502_03805_b200 import binding as B
+from paper_2502_03805_b200 import build
 from paper_2502_03805_b200 import cache as cache_module
 
 
@@ -15,3 +19,24 @@ def test_page_strides():
                 torch.zeros(5, 16, 128)[..., :64], torch.zeros(5, 32, 64)[:, ::2], torch.zeros(5, 64, 16).transpose(1, 2)):
         with pytest.raises(ValueError):
             cache_module._page_stride(bad, "x")
+
+
+def test_lengths_may_not_overlap_what_a_store_reads():
+    """Every CTA of a head reads the counts, offsets and indices, one writes the new length: only `start` is read in a way
+    that allows it to be that array."""
+    build.build_library()
+    B.load()
+    fake = C.addressof(C.create_string_buffer(4096))
+    c = B.make_cache(nseq=2, Hq=2, Hkv=1, dh=64, dtype="bf16", format="plain", page_size=16, num_pages=4, max_pages=3,
+                     k_pages=1 << 20, v_pages=1 << 21, page_table=1 << 16)
+
+    def store(lens_out, counts=None, idx=None, offsets=None, start=4096):
+        return B.criticalkv_cache_store(fake, c, 1 << 22, 1 << 23, 8, None, idx, offsets, 5 if idx else 0, counts, start,
+                                        lens_out, check=False)
+
+    for at in (8192, 8196):
+        assert store(at, counts=8192) == store(8192, counts=at) == B.CKV_EINVAL
+    assert store(8192, idx=12288, offsets=8192) == store(8192 + 12, idx=12288, offsets=8192) == B.CKV_EINVAL
+    assert store(12288 + 36, idx=12288, offsets=8192) == B.CKV_EINVAL
+    assert store((1 << 16) + 20) == store((1 << 16) - 4) == B.CKV_EINVAL
+    assert store(4096 + 4) == store(4096 - 4) == B.CKV_EINVAL
