@@ -324,7 +324,7 @@ typedef struct {
    so far positions lose nothing; a negative position turns back. */
 typedef enum { CKV_ROPE_HALF = 0, CKV_ROPE_INTERLEAVED = 1 } criticalkv_rope_layout;
 typedef struct {
-  int32_t nseq, T;       /* sequences and tokens a sequence, >= 0 (0: nothing to do)                            */
+  int32_t nseq, T;       /* sequences and tokens a sequence, >= 0 (0: nothing to do), product at most 2^31 - 257  */
   int32_t Hq, Hk;        /* heads of q (>= 1) and of k (0: no k)                                                */
   int32_t dh;            /* row length, a multiple of 8, at most 256                                            */
   int32_t rot;           /* rotated elements, even, 2..dh                                                       */
@@ -373,8 +373,8 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
  * bf16 queries run on tensor cores: stored 8-bit values enter exactly, sums and the softmax are float32, and a weight
  * enters its product with the values rounded to 16 bits (plain pages) or, times the row's scale, to 22 bits and no finer than
  * 2^-40 of the head's largest such product (8-bit pages).  float32 queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores,
- * in float32 throughout.  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) * ceil(max_pages *
- * page_size / 64) exceeds 2^31 - 1.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
+ * in float32 throughout.  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) exceeds 2^26 or, times ceil(max_pages *
+ * page_size / 64), 2^31 - 1.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
  * needs no initialisation; calls that may overlap on the GPU need workspaces of their own.
  */
 CKV_API int criticalkv_decode_workspace_bytes(const criticalkv_cache* c, size_t* bytes);

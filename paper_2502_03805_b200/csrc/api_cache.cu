@@ -100,7 +100,8 @@ int criticalkv_rope(criticalkv_handle h, const criticalkv_rope_desc* d, const vo
       (rc = resolve_stride(d->q_out_stride, d->Hq, d->T, d->dh, d->dtype, o.qos)) != CKV_OK ||
       (rc = resolve_stride(d->k_out_stride, d->Hk, d->T, d->dh, d->dtype, o.kos)) != CKV_OK)
     return rc;
-  if ((long long)d->nseq * d->T > 0x7fffffffLL) return CKV_ENOTSUP;
+  // tokens are numbered in 32 bits, up to a whole tile of them behind the last
+  if ((long long)d->nseq * d->T > 0x7fffffffLL - 256) return CKV_ENOTSUP;
   if (d->nseq == 0 || d->T == 0) return CKV_OK;
   if (!q || !q_out || !pos || !freq || (d->Hk && (!k || !k_out))) return CKV_EINVAL;
   if (!aligned16(q) || !aligned16(q_out) || (d->Hk && (!aligned16(k) || !aligned16(k_out))) || !aligned_to(pos, 4) ||
@@ -189,8 +190,9 @@ int criticalkv_decode(criticalkv_handle h, const criticalkv_cache* c, const void
     if (call.q_stride[i] < 0) return CKV_EINVAL;
     if (call.q_stride[i] % vec) return CKV_EALIGN;
   }
-  // the list of 64-row tiles of all heads is counted in 32 bits
-  if ((long long)d.nseq * d.Hkv * ((d.Hq / d.Hkv + 7) / 8) > 0x7fffffffLL / ((d.capacity + 63) / 64)) return CKV_ENOTSUP;
+  // the list of 64-row tiles of all heads is counted in 32 bits, and so are the heads a thread further and sixteen times them
+  const long long items = (long long)d.nseq * d.Hkv * ((d.Hq / d.Hkv + 7) / 8);
+  if (items > 0x7fffffffLL / ((d.capacity + 63) / 64) || items > (1LL << 26)) return CKV_ENOTSUP;
   if (d.nseq == 0) return CKV_OK;
   if (!q || !lens || !out || !ws) return CKV_EINVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned_to(lens, 4) || !aligned_to(lse, 4) || !aligned_to(ws, 256))

@@ -40,3 +40,24 @@ def test_lengths_may_not_overlap_what_a_store_reads():
     assert store(12288 + 36, idx=12288, offsets=8192) == B.CKV_EINVAL
     assert store((1 << 16) + 20) == store((1 << 16) - 4) == B.CKV_EINVAL
     assert store(4096 + 4) == store(4096 - 4) == B.CKV_EINVAL
+
+
+def test_counts_that_pass_32_bits_inside_a_kernel_are_refused():
+    build.build_library()
+    B.load()
+    fake = C.addressof(C.create_string_buffer(4096))
+
+    def rope(nseq, T):       # the last tile of tokens may reach 255 tokens behind T
+        d = B.make_rope_desc(nseq=nseq, T=T, Hq=1, Hk=0, dh=8, rot=2, dtype="f32", layout="half")
+        return B.criticalkv_rope(fake, d, 16, None, 16, None, 16, None, check=False)      # refused for the null otherwise
+
+    assert rope(1, 2 ** 31 - 256) == rope(1, 2 ** 31 - 1) == rope(3, 2 ** 30) == B.CKV_ENOTSUP
+    assert rope(1, 2 ** 31 - 257) == rope(2, 2 ** 29) == B.CKV_EINVAL
+
+    def decode(nseq, Hq, Hkv):
+        c = B.make_cache(nseq=nseq, Hq=Hq, Hkv=Hkv, dh=64, dtype="bf16", format="plain", page_size=16, num_pages=4, max_pages=1,
+                         k_pages=1 << 20, v_pages=1 << 21, page_table=1 << 16)
+        return B.criticalkv_decode(fake, c, None, None, 256, 256, None, 256, ws_bytes=1 << 30, check=False)
+
+    assert decode((1 << 23) + 1, 8, 8) == decode(1 << 25, 24, 1) == B.CKV_ENOTSUP
+    assert decode(1 << 23, 8, 8) == decode(1 << 25, 16, 1) == B.CKV_EINVAL
