@@ -14,13 +14,14 @@ WEIGHT_BITS = {          # relative rounding error of a weight in the product wi
     ("cuda", "plain"): 2.0 ** -24, ("cuda", "8-bit"): 2.0 ** -24}
 
 
-def decode(q, values_k, values_v, table, lens, page_size, scale, fmt, dtype, kernel, vscale=None):
+def decode(q, values_k, values_v, table, lens, page_size, scale, fmt, dtype, kernel, vscale=None, moves=1):
     """out, lse in 64 bits and bounds on |kernel - out| and |kernel - lse|; kernel "tensor" (bf16) or "cuda".
 
     With weights w_i and relative errors d_i of theirs, out moves by sum w_i d_i (v_i - out) and lse by sum w_i d_i.
     d_i: the sum of a logit's dh products (dh additions, relative to sum |q||k|; queries of 8-bit pages as halves on the
     tensor cores: 2^-39 of the largest element each), four roundings relative to the logit (row scale, two factors, the
-    difference to the maximum, which is at most twice the largest logit), 2^-22 of exp2.  Then the rounding of the weights in
+    difference to the maximum, which is at most twice the largest logit), 2^-22 of exp2 once and each time the running
+    maximum moves (`moves`: of the order of ln n a warp, and three where warps, CTAs and parts meet).  Then the rounding of the weights in
     the second product, the additions over the rows (a quarter of them one behind the other at most, and 64 more where
     parts are joined) and the result's rounding.  Two halves: a product of weight and row scale loses 2^-40 of the largest
     such product at the least, times the code."""
@@ -43,7 +44,7 @@ def decode(q, values_k, values_v, table, lens, page_size, scale, fmt, dtype, ker
             w = torch.softmax(logit, -1)
             out[s, hs] = w @ V
             lse[s, hs] = torch.logsumexp(logit, -1)
-            d = (dh + 8) * STEP * abs(scale) * (qs.abs() @ K.abs().T) + 4 * STEP * logit.abs() + 2.0 ** -22
+            d = (dh + 8) * STEP * abs(scale) * (qs.abs() @ K.abs().T) + 4 * STEP * logit.abs() + moves * 2.0 ** -22
             d = d + STEP * logit.abs().amax(-1, keepdim=True)
             if kernel == "tensor" and fmt != "plain":
                 d = d + 2.0 ** -39 * abs(scale) * qs.abs().amax(-1, keepdim=True) * K.abs().sum(-1)
