@@ -22,8 +22,8 @@
 // for bf16 pages two bf16 (16 bits); for 8-bit pages, whose codes are exact halves, two halves (22 bits) of weight * scale
 // of the row * 2^15 / the largest such product so far.  What is below 2^-40 of that largest product is lost, so rows of very
 // different norms and long tails of small weights keep theirs.  The queries of
-// 8-bit pages become halves after a scaling by a power of two that puts the largest of a row at 2^14: exact but for
-// elements 2^-29 below it.
+// 8-bit pages become halves after a scaling by a power of two that puts the largest of a row at 2^14 (at most 2^100): exact
+// but for elements 2^-29 below it or below 2^-114, which are rounded to multiples of 2^-38 of it or of 2^-124.
 //
 // Measured: 2 x 131072 bf16 rows a head, 40 query heads on 8, 168 us, 6.4 TB/s (0.98 of the copy bandwidth); 32 x 6553
 // e4m3 rows a head, 32 query heads on 8, 87 us, 5.2 TB/s (0.80; 82 us with weights of 11 bits, whose error is seen where
@@ -81,6 +81,7 @@ template <int FMT> __device__ __forceinline__ void codes_to_halves(uint32_t four
 // The largest product of a weight and a row's scale so far, as a half (8-bit pages): the top of the range, so that a long
 // tail of small weights keeps its part of the sums.
 constexpr float kTopWeight = 32768.f;
+constexpr float kLeastTop = 3.851859888774472e-34f;   // 2^-111: kTopWeight over it and it over kTopWeight are normal floats
 
 template <int FMT, int DH, int NT> struct Shape {
   static constexpr bool kPlain = FMT == CKV_CACHE_PLAIN;
@@ -428,7 +429,9 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               float& z = s[n][u][2 * h + x];
-              z = (S::kPlain ? z : z * ks[u][h]) * to_log2[n][x];
+              // the two scales first: a product of codes and normalised queries, up to 2^31, times a large row scale alone
+              // would overflow where tiny queries make up for it
+              z *= S::kPlain ? to_log2[n][x] : ks[u][h] * to_log2[n][x];
               top[x] = fmaxf(top[x], z);
             }
         float f[2] = {1.f, 1.f};                                     // what the sums so far are multiplied by
@@ -487,7 +490,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
               most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 4));
               most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 8));
               most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 16));
-              const float one = most[x] > 0.f ? __frcp_rn(most[x]) : 0.f;
+              most[x] = fmaxf(most[x], kLeastTop);
+              const float one = __frcp_rn(most[x]);
               f[x] = big[n][x] * one;
               big[n][x] = most[x];
               inv[n][x] = one * kTopWeight;

@@ -19,7 +19,8 @@ def decode(q, values_k, values_v, table, lens, page_size, scale, fmt, dtype, ker
 
     With weights w_i and relative errors d_i of theirs, out moves by sum w_i d_i (v_i - out) and lse by sum w_i d_i.
     d_i: the sum of a logit's dh products (dh additions, relative to sum |q||k|; queries of 8-bit pages as halves on the
-    tensor cores: 2^-39 of the largest element each), four roundings relative to the logit (row scale, two factors, the
+    tensor cores: halves are multiples of 2^-24, so half a step is 2^-25; the largest element stands at 2^14 or above, which
+    makes it 2^-39 of that each, but the scaling is by 2^100 at most, which makes it 2^-125 for tinier rows), four roundings relative to the logit (row scale, two factors, the
     difference to the maximum, which is at most twice the largest logit), 2^-22 of exp2 once and each time the running
     maximum moves (`moves`: of the order of ln n a warp, and three where warps, CTAs and parts meet).  Then the rounding of the weights in
     the second product, the additions over the rows (a quarter of them one behind the other at most, and 64 more where
@@ -47,7 +48,7 @@ def decode(q, values_k, values_v, table, lens, page_size, scale, fmt, dtype, ker
             d = (dh + 8) * STEP * abs(scale) * (qs.abs() @ K.abs().T) + 4 * STEP * logit.abs() + moves * 2.0 ** -22
             d = d + STEP * logit.abs().amax(-1, keepdim=True)
             if kernel == "tensor" and fmt != "plain":
-                d = d + 2.0 ** -39 * abs(scale) * qs.abs().amax(-1, keepdim=True) * K.abs().sum(-1)
+                d = d + abs(scale) * (2.0 ** -39 * qs.abs().amax(-1, keepdim=True) + 2.0 ** -125) * K.abs().sum(-1)
             adds = (n / 4 + 64) * STEP
             for h in range(G):
                 far = (V - out[s, g * G + h]).abs()
