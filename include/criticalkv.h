@@ -348,8 +348,7 @@ CKV_API int criticalkv_rope(criticalkv_handle h, const criticalkv_rope_desc* d, 
  *   idx != NULL   rows idx[s, offsets[s,g] .. offsets[s,g+1]), the result of criticalkv_select (idx [nseq, idx_rows],
  *                 offsets [nseq, Hkv+1]); counts must be NULL.
  * lens_out[s, g] (may be NULL, may be `start` itself, and must not overlap anything else that the call reads) = start +
- * rows written, at most max_pages * page_size.  Other
- * rows of the pages keep their contents.  No page may be listed twice among the rows that one call writes.
+ * rows written, at most max_pages * page_size.  K and V share their strides.  Other rows of the pages keep their contents.  No page may be listed twice among the rows that one call writes.
  */
 CKV_API int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* c, const void* K, const void* V,
                                    int32_t n, const int64_t* stride, const int32_t* idx, const int32_t* offsets,
@@ -369,7 +368,7 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
  * rows of that KV head, out[s, h, :] = sum_i softmax_i(scale * q . k_i) v_i and lse[s, h] = log sum_i exp(scale * q .
  * k_i) (lse may be NULL; it is what merging with attention over other keys needs).  A head without rows gives zeros and
  * -infinity; one that has rows but none in an existing page, or only logits of -infinity, gives NaN; rows with infinite or
- * NaN values give results that are not finite.  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
+ * NaN values give results that are not finite (a key that makes a logit -infinity has no weight).  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
  * bf16 queries run on tensor cores: stored 8-bit values enter exactly, sums and the softmax are float32, and a weight
  * enters its product with the values rounded to 16 bits (plain pages) or, times the row's scale, to 22 bits and no finer than
  * 2^-40 of the head's largest such product (8-bit pages).  float32 queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores,

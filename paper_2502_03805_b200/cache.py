@@ -326,7 +326,8 @@ class PagedCache(_Owner):
     def store(self, K, V, start, lens_out=None, *, idx=None, offsets=None, counts=None, stream=None):
         """Writes rows of K, V [nseq, Hkv, n, dh] behind row start[s, g] of every head and returns lens_out, which may
         be `start` (allocated when None).  All n rows, the first counts[s] of them, or with idx [nseq, idx_rows] and
-        offsets [nseq, Hkv+1] the rows that CompressionSession.select chose."""
+        offsets [nseq, Hkv+1] the rows that CompressionSession.select chose.  K and V have the same strides: parts of one
+        projection keep them when Rotary.rotate turns k in place (k_out=k)."""
         if lens_out is None:
             with self._allocating(stream):
                 lens_out = torch.empty((self.nseq, self.Hkv), dtype=torch.int32, device=self.device)
@@ -404,8 +405,9 @@ class PagedCache(_Owner):
 
     def workspace(self, stream=None):
         """The decode workspace of a stream (None: the current one): allocated there on first use and kept.  Calls on
-        different streams have different ones, and while a stream is captured every call gets a new one from the graph's
-        memory, so that neither two graphs nor a graph and other calls share any."""
+        different streams have different ones, and while torch.cuda.graph captures a stream every call gets a new one from
+        the graph's memory, so that neither two graphs nor a graph and other calls share any.  A capture that torch's
+        allocator does not know of needs a `ws` argument that outlives the graph."""
         if stream is None:
             return self._workspace(_raw_stream(self._index))
         with self._allocating(stream):

@@ -472,8 +472,9 @@ struct LaunchSetup {
 //   1 sequence  x  400 rows:   -    9.6   7.6   6.7   7.6, 8.1      18 x 200:  8.7  10.0 ...      , 11.6
 //   1 sequence  x  819 rows:   -   13.9  10.2   8.6   8.1, 8.1      37 x 200: 10.5  18.6 ...      , 14.1
 //   6 sequences x  400 rows:   -   10.3   8.5   8.6  22.3, 9.9      128 x 60: 16.4  33.1 ...      , 19.0
-// In between the choice is up to 15 % off on the device (14 sequences of 400 e4m3 rows 11.7, split 10.2), which is what the
-// second launch costs a call.
+// In between the choice is up to 17 % off on the device (14 sequences of 400 e4m3 rows 12.4, split 10.6), which is what the
+// second launch costs a call.  A cache whose table has room for much more than its heads hold takes the split, too (1
+// sequence x 819 bf16 rows in a table for 16384: 8.6 us instead of 8.0 on the device, 12.2 instead of 9.7 a call).
 inline int decode_team(const DecodeArgs& p, const LaunchSetup::Fit& fit, int sm_count, int tile) {
   const long long tiles = (p.c.capacity + tile - 1) / tile, resident = (long long)fit.per_sm.load() * sm_count;
   auto fit_at_once = [&](int i) { return p.allow_cluster && p.items <= fit.clusters[i].load(std::memory_order_relaxed); };

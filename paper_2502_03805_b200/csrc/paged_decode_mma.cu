@@ -4,8 +4,8 @@
 // of K and V from HBM, and CUDA cores cannot keep up with that stream (at G = 4 and 8-bit pages the CUDA-core kernel
 // reached a quarter of it).  The matrix instruction is mma.sync with the CACHE ROWS on its 16-row side and 8 queries on
 // the other: a query tile of tcgen05.mma would be 64 or 128 rows of which G are used, its operands would have to lie in
-// shared memory in the format of the instruction (8-bit pages converted and written back), and this kernel needs about
-// a tenth of the mma.sync rate.
+// shared memory in the format of the instruction (8-bit pages converted and written back), and this kernel keeps the tensor
+// pipe busy for 13 to 31 % of its time.
 //
 //   S^T = K Q^T   A = 16 rows of K.  Lane (r, c) = (lane / 4, lane % 4) reads 16 bytes of two rows; which of a row's
 //                 elements those are is free, as long as the query fragments are loaded in the same order.
@@ -13,21 +13,24 @@
 //                 and interleaves them with byte permutes; which elements form a 16-row tile is free again.  P^T is
 //                 the accumulator of the first product with rows and columns exchanged (movmatrix).
 //
-// Every warp streams on its own: it works through 16 or 32 rows at a time, which one lane fetches with TMA (16 rows of
-// a page are contiguous) into the warp's own slots, K of the next step as soon as K Q^T of this one is done, V likewise
-// after V^T P^T, also across the end of an item: 8 KB a warp and 12 warps an SM are on their way.  The 128-byte swizzle
-// and the order of the rows (row_of) keep both reads free of bank conflicts.
+// Every warp streams on its own: it works through 16 to 64 rows at a time (Shape::kSub), which one lane fetches with TMA
+// (16 rows of a page are contiguous) into the warp's own slots, K of the next step as soon as K Q^T of this one is done, V
+// likewise after V^T P^T, also across the end of an item: 8 KB a warp are on their way (16 with two query tiles on 128-byte
+// rows), on 12 warps an SM with one query tile and 8 with two.  The 128-byte swizzle and the order of the rows (row_of)
+// keep both reads free of bank conflicts.
 // Softmax statistics are float32; the running maximum is only reduced over the warp (and the sums only rescaled) in
 // steps in which some lane sees a larger logit.  The weights enter the second product as the sum of two 16-bit numbers:
 // for bf16 pages two bf16 (16 bits); for 8-bit pages, whose codes are exact halves, two halves (22 bits) of weight * scale
 // of the row * 2^15 / the largest such product so far.  What is below 2^-40 of that largest product is lost, so rows of very
-// different norms and long tails of small weights keep theirs.  The queries of
-// 8-bit pages become halves after a scaling by a power of two that puts the largest of a row at 2^14 (at most 2^100): exact
-// but for elements 2^-29 below it or below 2^-114, which are rounded to multiples of 2^-38 of it or of 2^-124.
+// different norms and long tails of small weights keep theirs.  The queries of 8-bit pages become halves after a scaling
+// by a power of two (at most 2^100) that puts the largest of a row at 2^14: exact but for elements 2^-29 below it or below
+// 2^-114, which are rounded to multiples of 2^-38 of it or of 2^-124.  The factor of a logit, scale * log2(e), is one float
+// and the exponential is ex2.approx (2^-22); the CUDA-core kernel keeps the rest of the factor as well.
 //
 // Measured: 2 x 131072 bf16 rows a head, 40 query heads on 8, 168 us, 6.4 TB/s (0.98 of the copy bandwidth); 32 x 6553
-// e4m3 rows a head, 32 query heads on 8, 87 us, 5.2 TB/s (0.80; 82 us with weights of 11 bits, whose error is seen where
-// values cancel), bound by instruction latency: 168 registers leave three CTAs an SM, and with 128 the sums spill (122 us).  1 x 819 bf16 rows: 7.9 us, a chain of latencies.
+// e4m3 rows a head, 32 query heads on 8, 86 us, 5.2 TB/s (0.81; 82 us with weights of 11 bits, whose error is seen where
+// values cancel), bound by instruction latency: 168 registers (60 bytes spilled) leave three CTAs an SM; four, with 128 and
+// 400 bytes spilled, take 99 us.  1 x 819 bf16 rows: 8.0 us, a chain of latencies.
 #include "paged_decode.cuh"
 #include "sm100_ptx.cuh"
 #include "tma_host.h"
@@ -87,8 +90,8 @@ template <int FMT, int DH, int NT> struct Shape {
   static constexpr bool kPlain = FMT == CKV_CACHE_PLAIN;
   static constexpr int kRowBytes = kPlain ? DH * 2 : DH;
   // 16-row groups a warp takes at a time.  4 KB of K and of V; 8 KB for two query tiles on 128-byte rows, where the work
-  // per step that does not depend on the rows weighs more (16 queries on e4m3 rows of 128: 143 -> 120 us; with one
-  // query tile 88.7 and 88.6 us).
+  // per step that does not depend on the rows weighs more (16 queries on e4m3 rows of 128: 144 -> 123 us; with one
+  // query tile 86.0 and 85.3 us, int8 95 and 101 us).
   static constexpr int kSub = kRowBytes >= 256 ? 1 : kRowBytes == 128 ? 2 * NT : 4;
   static constexpr int kTile = kDecodeWarps * 16 * kSub;           // cache rows a CTA takes at a time
   static constexpr int kChunks = kRowBytes / 64;                   // 16-byte pieces of a K row per lane

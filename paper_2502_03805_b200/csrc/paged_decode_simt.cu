@@ -8,9 +8,10 @@
 // scale enters with the rest of its rounding, and only the difference of a logit to the maximum is rounded.
 // Half of the values and the page of the next rows are loaded before the logits.
 //
-// Measured (8 x 6553 rows a head, 8 KV heads): float32 rows of 128, four queries a head, 80 us, 5.4 TB/s (0.84 of the copy
-// bandwidth; 119 us without the early loads and with items of eight); e4m3 rows 64 us, bound by arithmetic (two products
-// a stored byte and query, and the conversions).
+// Measured (8 x 6553 rows a head, 8 KV heads): float32 rows of 128, four queries a head, 79 us, 5.5 TB/s (0.85 of the copy
+// bandwidth; 119 us without the early loads and with items of eight); e4m3 rows 62 us (floor 17).  That is latency, not
+// products: 2.2 instructions a cycle and SM, and most of a warp's stalls wait for its 4-byte loads and the shared-memory
+// round trips of logits and weights, with 15 warps an SM to hide them.
 #include <cuda_bf16.h>
 
 #include "paged_decode.cuh"

@@ -2,7 +2,8 @@
 // Pair i of a row is turned by pos * freq[i]: (a, b) -> factor * (a cos - b sin, b cos + a sin).
 //
 // The angle is reduced to a fraction of a turn in float64 (pos * freq loses up to pos * 2^-24 radians in float32: 0.008
-// at position 131072) and only then goes to sincospif.  All heads of a token share its rot/2 angles, so a thread owns
+// at position 131072) and only then rounded, to within 2 pi 2^-26 radians, for sincospif; cosine and sine times `factor`
+// and the products are float32.  All heads of a token share its rot/2 angles, so a thread owns
 // one unit of one token's rows (half layout: 16 bytes of a pair's first elements and 16 of its second; interleaved: 16
 // bytes), keeps the unit's cosines and sines in registers and walks over the heads, 64 bytes in flight, 32 warps an SM.
 // Elements that are only copied form units of the same size.  Bound by HBM: every row is read and written once (32768
