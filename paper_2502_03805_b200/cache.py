@@ -3,7 +3,8 @@
 Device-buffer plumbing around the C ABI, like session.py: shapes, types and devices of tensors are checked here, every
 number is computed by the kernels of libcriticalkv.  Work goes to torch's current stream of the tensors' device unless
 a stream is given.  The tensors of a call must be ready on that stream; what an object keeps for itself (pages, tables,
-frequencies, workspaces) may be dropped while calls are in flight.
+frequencies, workspaces) may be dropped while calls are in flight on torch's own streams.  On a stream that torch did not
+make (an address, torch.cuda.ExternalStream) the caller keeps the object until the calls are done.
 """
 from __future__ import annotations
 
@@ -86,12 +87,17 @@ class _Owner:
         it: their memory is not handed out again before the work in flight on it at their end is done."""
         raw = _raw_stream(self._index) if stream is None else self._on(stream)
         if raw not in self._seen:
-            at = self._torch_stream(stream)
-            for t in self._kept():
-                if t is not None:
-                    t.record_stream(at)
+            self._record(self._kept(), stream)
             self._seen.add(raw)
         return raw
+
+    def _record(self, tensors, stream):
+        at = self._torch_stream(stream)
+        if at.cuda_stream and at.stream_id == at.cuda_stream:
+            return       # not torch's: it may be gone when the tensors go, and an event would then be recorded on it
+        for t in tensors:
+            if t is not None:
+                t.record_stream(at)
 
     def _fail(self, rc, where):
         B._check(self.handle, rc, where, True)

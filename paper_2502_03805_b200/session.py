@@ -178,9 +178,8 @@ class ChunkedPrefillCompressor:
             if current != default:
                 current.wait_stream(default)
         for rows in (self.K, self.V):      # the next step drops them, perhaps before they have been read
-            for x in (rows if isinstance(rows, list) else [rows]):
-                if x.is_cuda:
-                    x.record_stream(cache._torch_stream(stream))
+            if rows[0].is_cuda:
+                cache._record(rows if isinstance(rows, list) else [rows], stream)
         with cache._allocating(stream):
             start = cache.new_lengths() if start is None else start
             if self.budget_mode == "uniform":
