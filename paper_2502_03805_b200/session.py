@@ -81,13 +81,15 @@ class CompressionSession:
         """Step 5 into a PagedCache (quantised where its format says so) instead of K_out, V_out: the selected rows of
         K, V go behind row start[b, g] of every head; returns the new lengths.  Without a stream it works on the default
         one, like the other calls of a session; where another stream is current (the one a cache's and a rotary's calls
-        take), each of the two waits for the other."""
+        take), each of the two waits for the other.  While that stream is captured it has to be given."""
         kw = dict(idx=self.idx[:, :self.btot], offsets=self.offsets)
         if stream is not None:
             return cache.store(K, V, start, lens_out, stream=stream, **kw)
+        default, current = torch.cuda.default_stream(self.device), torch.cuda.current_stream(self.device)
+        if current != default and torch.cuda.is_current_stream_capturing():
+            raise ValueError("the current stream is being captured: pass it as `stream` (the default one cannot be captured)")
         if lens_out is None:      # of the current stream, on which the caller goes on
             lens_out = torch.empty((cache.nseq, cache.Hkv), dtype=torch.int32, device=cache.device)
-        default, current = torch.cuda.default_stream(self.device), torch.cuda.current_stream(self.device)
         if current != default:
             default.wait_stream(current)
         cache.store(K, V, start, lens_out, stream=0, **kw)
@@ -170,12 +172,13 @@ class ChunkedPrefillCompressor:
     def to_cache(self, cache, start=None, stream=None):
         """Writes the retained rows into a PagedCache of one sequence (decoding starts from there) and returns the
         lengths of its heads.  All of it is done on `stream`, on which the rows must be ready, or without one on the
-        current stream, which then waits for the default stream, the one step() compresses on."""
+        current stream, which then waits for the default stream, the one step() compresses on (a captured stream does
+        not: the rows must be ready)."""
         if self.K is None:
             raise ValueError("nothing has been compressed yet")
         if stream is None:
             default, current = torch.cuda.default_stream(self.device), torch.cuda.current_stream(self.device)
-            if current != default:
+            if current != default and not torch.cuda.is_current_stream_capturing():
                 current.wait_stream(default)
         for rows in (self.K, self.V):      # the next step drops them, perhaps before they have been read
             if rows[0].is_cuda:

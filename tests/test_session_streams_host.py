@@ -38,6 +38,7 @@ def streams(request, monkeypatch):
     made = {n: Stream(n, log) for n in ("default", "side")}
     monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: made["default"])
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: made[request.param])
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return request.param, log
 
 
@@ -68,4 +69,26 @@ def test_to_cache_waits_for_the_stream_of_the_steps(streams, mode):
     assert log == ([] if current == "default" else [("side", "waits for", "default")]) + [("store on", None)]
     log.clear()
     ch.to_cache(Cache(log), stream=77)
+    assert log == [("store on", 77)]
+
+
+def test_while_the_current_stream_is_captured(streams, monkeypatch):
+    """The default stream cannot be captured: neither waits for the other, and what would run on it is refused."""
+    current, log = streams
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    s = object.__new__(CompressionSession)
+    s.handle, s.device, s.btot = None, "cpu", 4
+    s.idx, s.offsets = torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, 3, dtype=torch.int32)
+    ch = ChunkedPrefillCompressor(Hq=2, Hkv=2, dh=64, dm=64, w=8, pool_k=3, dtype="f32")
+    ch.device = torch.device("cpu")
+    K = ch.K = ch.V = torch.zeros(2, 3, 64)
+    ch.to_cache(Cache(log))
+    assert log == [("store on", None)]
+    log.clear()
+    start = torch.zeros(1, 2, dtype=torch.int32)
+    if current == "side":
+        with pytest.raises(ValueError):
+            s.compact_into(Cache(log), K, K, start)
+        assert log == []
+    s.compact_into(Cache(log), K, K, start, stream=77)
     assert log == [("store on", 77)]

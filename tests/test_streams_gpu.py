@@ -69,3 +69,31 @@ def test_a_chunked_prefill_into_a_cache_on_a_side_stream(mode):
         m = int(lens[0, h])
         assert m == ch.K[h].shape[0]
         assert torch.equal(K[0, h, :m], ch.K[h].cpu()) and torch.equal(V[0, h, :m], ch.V[h].cpu())
+
+
+def test_a_compression_into_a_cache_captured_as_a_graph():
+    """With the captured stream given; each replay selects and stores again."""
+    g = gen(5)
+    Hq, Hkv, dh, dm, n, w = 4, 2, 64, 64, 300, 8
+    Qw, K, V, WO = (torch.randn(*s, generator=g).bfloat16().cuda() for s in ((1, Hq, w, dh), (1, Hkv, n, dh), (1, Hkv, n, dh), (1, Hq, dh, dm)))
+    s = CompressionSession(nb=1, Hq=Hq, Hkv=Hkv, dh=dh, dm=dm, n=n, w=w, pool_k=3, dtype="bf16", budget_mode="uniform", budget=60)
+    cache = PagedCache.allocate(nseq=1, Hq=Hq, Hkv=Hkv, dh=dh, dtype="bf16", rows=n)
+    start, lens = cache.new_lengths(), cache.new_lengths()
+    s.compress(Qw, K, V, WO)
+    s.compact_into(cache, K, V, start, lens)
+    want = [x.clone() for x in cache.load(lens, 60)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(ValueError):
+            s.compact_into(cache, K, V, start, lens)
+        s.compact_into(cache, K, V, start, lens, stream=torch.cuda.current_stream())
+    for _ in range(2):
+        cache.k_pages.zero_()
+        cache.v_pages.zero_()
+        lens.zero_()
+        graph.replay()
+        assert lens.cpu().tolist() == [[60, 60]]
+        for a, b in zip(cache.load(lens, 60), want):
+            assert torch.equal(a, b)
