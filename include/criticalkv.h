@@ -348,7 +348,8 @@ CKV_API int criticalkv_rope(criticalkv_handle h, const criticalkv_rope_desc* d, 
  *   idx != NULL   rows idx[s, offsets[s,g] .. offsets[s,g+1]), the result of criticalkv_select (idx [nseq, idx_rows],
  *                 offsets [nseq, Hkv+1]); counts must be NULL.
  * lens_out[s, g] (may be NULL, may be `start` itself, and must not overlap anything else that the call reads) = start +
- * rows written, at most max_pages * page_size.  K and V share their strides.  Other rows of the pages keep their contents.  No page may be listed twice among the rows that one call writes.
+ * rows written, at most max_pages * page_size.  K and V share their strides.  Other rows of the pages keep their
+ * contents.  No page may be listed twice among the rows that one call writes.
  */
 CKV_API int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* c, const void* K, const void* V,
                                    int32_t n, const int64_t* stride, const int32_t* idx, const int32_t* offsets,
