@@ -290,12 +290,20 @@ CKV_API int criticalkv_diagnose(criticalkv_handle h, const criticalkv_desc* d, c
 typedef enum {
   CKV_CACHE_PLAIN = 0, /* pages hold rows in the model's element type (dtype)                                   */
   CKV_CACHE_E4M3 = 1,  /* 8-bit float codes (4 exponent, 3 fraction bits, largest 448), one float32 scale a row   */
-  CKV_CACHE_INT8 = 2   /* 8-bit integer codes in -127..127, one float32 scale a row                               */
+  CKV_CACHE_INT8 = 2,  /* 8-bit integer codes in -127..127, one float32 scale a row                               */
+  CKV_CACHE_E2M1 = 3   /* 4-bit float codes (2 exponent, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+                          negatives), two a byte, the earlier element in the low half; an e4m3 scale for every 16
+                          elements and a float32 scale a row: dh * 9 / 16 + 4 bytes                               */
 } criticalkv_cache_format;
 /* A quantised row x[0..dh): s = max(max_i |x_i| / top, 2^-100) with top = 448 or 127, r = 1 / s, code_i = x_i * r
    rounded to nearest even; every operation a separately rounded float32 one (where top * s would overflow, s is the
    float below).  It stands for code_i * s.  A row that holds an infinity or a NaN gets an infinite or NaN scale and
-   stands for NaN in every element. */
+   stands for NaN in every element.
+   A 4-bit row: s = max(max_i |x_i| / 2688, 2^-100) (2688 = 448 * 6), r = 1 / s; for each group of 16 elements
+   g = e4m3((max of the group * r) * (1/6 as a float)), code_i = e2m1(x_i * (r / g)), 0 where g is 0; roundings to nearest
+   even, values beyond 448 and 6 become these, every operation a separately rounded float32 one (where 2688 * s would
+   overflow, s is the float below).  It stands for (code_i * g) * s, whose first product is exact.  In a row that holds an
+   infinity or a NaN, s is infinite or NaN, g and the codes are 0: it stands for NaN in every element. */
 
 typedef struct {
   int32_t nseq;          /* sequences, >= 0 (0: the calls do nothing)                                           */
@@ -311,11 +319,14 @@ typedef struct {
   float scale;           /* logit scale; <= 0 selects 1/sqrt(dh)                                                */
   uint32_t reserved;     /* must be 0                                                                           */
   int64_t page_stride;   /* elements of k_pages / v_pages from one page to the next, 0 = page_size * dh         */
-  void* k_pages;         /* [num_pages, page_size, dh] of dtype (plain) or 8-bit codes                          */
+  void* k_pages;         /* [num_pages, page_size, dh] of dtype (plain), 8-bit codes, or 4-bit codes (dh/2 bytes
+                            a row)                                                                              */
   void* v_pages;
   float* k_scale;        /* [num_pages, page_size], quantised formats only                                      */
   float* v_scale;
   const int32_t* page_table; /* [nseq, Hkv, max_pages]; entries behind a head's last page are never read as pages */
+  uint8_t* k_group_scale; /* e4m3 [num_pages, page_size, dh/16]; these two are read for CKV_CACHE_E2M1 only      */
+  uint8_t* v_group_scale;
 } criticalkv_cache;
 
 /* Rotary positions.  The first `rot` elements of every row are rot/2 pairs, (x_i, x_{i+rot/2}) in the half layout and

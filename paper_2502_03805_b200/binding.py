@@ -25,7 +25,7 @@ CKV_FLAG_SELECT_NO_CLUSTER = 256
 CKV_FLAG_DEBUG_CHECKS = 64
 CKV_FLAG_REQUIRE_TENSOR_CORES = 128
 CKV_EBOUNDS = -7
-CKV_CACHE_PLAIN, CKV_CACHE_E4M3, CKV_CACHE_INT8 = 0, 1, 2
+CKV_CACHE_PLAIN, CKV_CACHE_E4M3, CKV_CACHE_INT8, CKV_CACHE_E2M1 = 0, 1, 2, 3
 CKV_ROPE_HALF, CKV_ROPE_INTERLEAVED = 0, 1
 CKV_SELFTEST_MAX_WAIT_NS = 100_000_000
 CKV_STATIC_SCRATCH_BYTES = (8 << 20) + (64 << 10)
@@ -56,7 +56,7 @@ class criticalkv_cache(C.Structure):
                 ("format", C.c_int32), ("page_size", C.c_int32), ("num_pages", C.c_int32), ("max_pages", C.c_int32),
                 ("flags", C.c_uint32), ("scale", C.c_float), ("reserved", C.c_uint32), ("page_stride", C.c_int64),
                 ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
-                ("page_table", C.c_void_p)]
+                ("page_table", C.c_void_p), ("k_group_scale", C.c_void_p), ("v_group_scale", C.c_void_p)]
 
 
 class criticalkv_rope_desc(C.Structure):
@@ -290,16 +290,17 @@ def criticalkv_diagnose(handle, desc, Qw, K, V, WO, vnorm, idx, offsets, stage, 
 
 
 def make_cache(*, nseq, Hq, Hkv, dh, dtype, format, page_size, num_pages, max_pages, k_pages, v_pages, page_table,
-               k_scale=None, v_scale=None, page_stride=0, scale=0.0, flags=0):
+               k_scale=None, v_scale=None, page_stride=0, scale=0.0, flags=0, k_group_scale=None, v_group_scale=None):
     """Cache descriptor; the caller keeps the tensors (or addresses) alive while it is in use."""
     c = criticalkv_cache()
     c.nseq, c.Hq, c.Hkv, c.dh = nseq, Hq, Hkv, dh
     c.dtype = {"f32": CKV_F32, "bf16": CKV_BF16}.get(dtype, dtype)
-    c.format = {"plain": CKV_CACHE_PLAIN, "e4m3": CKV_CACHE_E4M3, "int8": CKV_CACHE_INT8}.get(format, format)
+    c.format = {"plain": CKV_CACHE_PLAIN, "e4m3": CKV_CACHE_E4M3, "int8": CKV_CACHE_INT8,
+                "e2m1": CKV_CACHE_E2M1}.get(format, format)
     c.page_size, c.num_pages, c.max_pages, c.page_stride = page_size, num_pages, max_pages, page_stride
     c.flags, c.scale, c.reserved = flags, scale, 0
     for name, x in (("k_pages", k_pages), ("v_pages", v_pages), ("k_scale", k_scale), ("v_scale", v_scale),
-                    ("page_table", page_table)):
+                    ("page_table", page_table), ("k_group_scale", k_group_scale), ("v_group_scale", v_group_scale)):
         setattr(c, name, x if x is None or isinstance(x, int) else x.data_ptr())
     return c
 

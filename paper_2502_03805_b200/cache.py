@@ -23,7 +23,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (     # ha
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _capturing = torch.cuda.is_current_stream_capturing
-_CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+_CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8, "e2m1": torch.uint8}     # "e2m1": two codes a byte
 
 
 def _sig(t):
@@ -261,19 +261,22 @@ class PagedCache(_Owner):
     """A paged KV cache whose heads have lengths of their own.
 
     k_pages, v_pages [num_pages, page_size, dh] of the model's type ("plain") or of 8-bit codes ("e4m3": float8_e4m3fn,
-    "int8": int8) with k_scale, v_scale float32 [num_pages, page_size]; page_table int32 [nseq, Hkv, max_pages].  The
+    "int8": int8) with k_scale, v_scale float32 [num_pages, page_size]; or of 4-bit codes ("e2m1": uint8 [num_pages,
+    page_size, dh/2], the earlier element in the low half of a byte) with these scales and k_group_scale, v_group_scale
+    float8_e4m3fn [num_pages, page_size, dh/16]; page_table int32 [nseq, Hkv, max_pages].  The
     tensors stay the caller's: lengths are passed to every call, pages are handed out by whoever owns the pool
     (PagedCache.allocate makes a pool in which every head has all its pages)."""
 
     def __init__(self, *, Hq, dtype, k_pages, v_pages, page_table, format="plain", k_scale=None, v_scale=None, scale=0.0,
-                 flags=0, handle=None):
-        if dtype not in _TORCH_DTYPE or format not in ("plain", "e4m3", "int8"):
+                 flags=0, handle=None, k_group_scale=None, v_group_scale=None):
+        if dtype not in _TORCH_DTYPE or format not in ("plain", "e4m3", "int8", "e2m1"):
             raise ValueError(f"unknown dtype {dtype!r} or format {format!r}")
         if k_pages.dim() != 3 or page_table.dim() != 3:
             raise ValueError("k_pages must be [num_pages, page_size, dh], page_table [nseq, Hkv, max_pages]")
         self.dtype, self.format, self.torch_dtype = dtype, format, _TORCH_DTYPE[dtype]
         dev = self.device = _device_of(k_pages, "k_pages")
         num_pages, page_size, dh = k_pages.shape
+        dh *= 2 if format == "e2m1" else 1
         code = _CODE.get(format, self.torch_dtype)
         strides = []
         for t, what in ((k_pages, "k_pages"), (v_pages, "v_pages")):
@@ -286,16 +289,22 @@ class PagedCache(_Owner):
         if k_scale is not None:
             _need(k_scale, "k_scale", (num_pages, page_size), torch.float32, dev)
             _need(v_scale, "v_scale", (num_pages, page_size), torch.float32, dev)
+        if (k_group_scale is None) != (format != "e2m1") or (v_group_scale is None) != (format != "e2m1"):
+            raise ValueError('k_group_scale and v_group_scale go with the format "e2m1"')
+        if k_group_scale is not None:
+            for t, what in ((k_group_scale, "k_group_scale"), (v_group_scale, "v_group_scale")):
+                _need(t, what, (num_pages, page_size, dh // 16), torch.float8_e4m3fn, dev)
         nseq, Hkv, max_pages = page_table.shape
         _need(page_table, "page_table", page_table.shape, torch.int32, dev)
         self.nseq, self.Hq, self.Hkv, self.dh = nseq, Hq, Hkv, dh
         self.page_size, self.num_pages, self.max_pages = page_size, num_pages, max_pages
         self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.k_group_scale, self.v_group_scale = k_group_scale, v_group_scale
         self.page_table = page_table
         self.desc = B.make_cache(nseq=nseq, Hq=Hq, Hkv=Hkv, dh=dh, dtype=dtype, format=format, page_size=page_size,
                                  num_pages=num_pages, max_pages=max_pages, k_pages=k_pages, v_pages=v_pages,
-                                 page_table=page_table, k_scale=k_scale, v_scale=v_scale, page_stride=strides[0],
-                                 scale=scale, flags=flags)
+                                 page_table=page_table, k_scale=k_scale, v_scale=v_scale, page_stride=strides[0] * (2 if format == "e2m1" else 1),
+                                 scale=scale, flags=flags, k_group_scale=k_group_scale, v_group_scale=v_group_scale)
         self._ws_bytes = B.criticalkv_decode_workspace_bytes(self.desc)   # also refuses a bad description
         self._ws = {}                    # workspaces by stream
         self._out_shape = (nseq, Hq, dh)
@@ -313,17 +322,20 @@ class PagedCache(_Owner):
         dev = torch.device("cuda", device)
         cols = max(1, -(-rows // page_size))
         n = max(1, nseq * Hkv * cols)
-        code = _CODE.get(format, _TORCH_DTYPE[dtype])
-        pages = [torch.zeros((n, page_size, dh), dtype=torch.uint8 if code in _CODE.values() else code,
+        code, four = _CODE.get(format, _TORCH_DTYPE[dtype]), format == "e2m1"
+        pages = [torch.zeros((n, page_size, dh // 2 if four else dh), dtype=torch.uint8 if code in _CODE.values() else code,
                              device=dev).view(code) for _ in range(2)]
         scales = [torch.zeros((n, page_size), dtype=torch.float32, device=dev) if format != "plain" else None
                   for _ in range(2)]
+        groups = [torch.zeros((n, page_size, dh // 16), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn) if four else None
+                  for _ in range(2)]
         table = torch.arange(nseq * Hkv * cols, dtype=torch.int32, device=dev).view(nseq, Hkv, cols)
         return cls(Hq=Hq, dtype=dtype, format=format, k_pages=pages[0], v_pages=pages[1], k_scale=scales[0],
-                   v_scale=scales[1], page_table=table, **kw)
+                   v_scale=scales[1], page_table=table, k_group_scale=groups[0], v_group_scale=groups[1], **kw)
 
     def _kept(self):
-        return self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.page_table
+        return (self.k_pages, self.v_pages, self.k_scale, self.v_scale, self.k_group_scale, self.v_group_scale,
+                self.page_table)
 
     def new_lengths(self):
         """Lengths of an empty cache."""

@@ -10,6 +10,7 @@ using ckv::CacheDims;
 using ckv::DeviceGuard;
 using ckv::aligned16;
 using ckv::record_cuda;
+using ckv::stored_bytes;
 
 inline bool aligned_to(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -26,7 +27,7 @@ int resolve_cache(const criticalkv_cache* c, CacheDims* o) {
   if (c->Hq > 65536) return CKV_ENOTSUP;
   if (c->dh != 64 && c->dh != 128) return CKV_ENOTSUP;
   if (c->dtype != CKV_F32 && c->dtype != CKV_BF16) return CKV_EINVAL;
-  if (c->format != CKV_CACHE_PLAIN && c->format != CKV_CACHE_E4M3 && c->format != CKV_CACHE_INT8) return CKV_EINVAL;
+  if (c->format < CKV_CACHE_PLAIN || c->format > CKV_CACHE_E2M1) return CKV_EINVAL;
   int shift = 0;
   switch (c->page_size) {
     case 16: shift = 4; break;
@@ -42,16 +43,22 @@ int resolve_cache(const criticalkv_cache* c, CacheDims* o) {
   const long long capacity = (long long)c->max_pages << shift;
   // row numbers are 32-bit, and so is the number of a call's (sequence, query head) pairs
   if (capacity > 0x7fffffffLL - 256 || (long long)c->nseq * c->Hq > 0x7fffffffLL) return CKV_ENOTSUP;
-  const int es = c->format != CKV_CACHE_PLAIN ? 1 : (c->dtype == CKV_F32 ? 4 : 2);
   const long long dense = (long long)c->page_size * c->dh;
   o->page_stride = c->page_stride ? c->page_stride : dense;
   if (o->page_stride < dense) return CKV_EINVAL;
   if (o->page_stride >= (1LL << 38)) return CKV_ENOTSUP;   // a tensor map holds strides below 2^40 bytes
-  if (o->page_stride * es % 16) return CKV_EALIGN;
+  if (o->page_stride % 2 || stored_bytes(c->format, c->dtype, o->page_stride) % 16) return CKV_EALIGN;
   if (!c->k_pages || !c->v_pages || (c->nseq && !c->page_table)) return CKV_EINVAL;
   if (c->format != CKV_CACHE_PLAIN && (!c->k_scale || !c->v_scale)) return CKV_EINVAL;
   if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || !aligned_to(c->page_table, 4)) return CKV_EALIGN;
   if (c->format != CKV_CACHE_PLAIN && (!aligned16(c->k_scale) || !aligned16(c->v_scale))) return CKV_EALIGN;
+  if (c->format == CKV_CACHE_E2M1) {
+    if (!c->k_group_scale || !c->v_group_scale) return CKV_EINVAL;
+    if (!aligned16(c->k_group_scale) || !aligned16(c->v_group_scale)) return CKV_EALIGN;
+    o->k_group = c->k_group_scale; o->v_group = c->v_group_scale;
+  } else {
+    o->k_group = o->v_group = nullptr;
+  }
   o->nseq = c->nseq; o->Hq = c->Hq; o->Hkv = c->Hkv; o->dh = c->dh; o->dtype = c->dtype; o->format = c->format;
   o->page_shift = shift; o->num_pages = c->num_pages; o->max_pages = c->max_pages;
   o->capacity = capacity;

@@ -136,8 +136,14 @@ struct CacheDims {
   void* v_pages;
   float* k_scale;
   float* v_scale;
+  uint8_t* k_group;                         // e2m1 only: e4m3 scales of 16 elements
+  uint8_t* v_group;
   const int32_t* page_table;
 };
+// Bytes that n elements of stored rows take.
+inline long long stored_bytes(int format, int dtype, long long n) {
+  return format == CKV_CACHE_PLAIN ? n * (dtype == CKV_F32 ? 4 : 2) : format == CKV_CACHE_E2M1 ? n / 2 : n;
+}
 struct DecodeCall {
   const void* q;
   long long q_stride[2];                    // elements: sequence, head

@@ -24,12 +24,17 @@ constexpr int kTile = 64, kWarpRows = kTile / kDecodeWarps;   // cache rows a ti
 // Four consecutive elements of a stored row, at element offset e.
 template <typename T, int FMT> struct Four {
   uint32_t w[FMT == CKV_CACHE_PLAIN ? sizeof(T) : 1];
+  uint32_t g;                                   // e2m1: scale of the group
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (unsigned i = 0; i < sizeof(w) / 4; ++i) w[i] = 0;
+    g = 0;
   }
-  __device__ __forceinline__ void load(const char* row, int e) {
-    if constexpr (FMT != CKV_CACHE_PLAIN) {
+  __device__ __forceinline__ void load(const char* row, const uint8_t* groups, int e) {
+    if constexpr (FMT == CKV_CACHE_E2M1) {
+      w[0] = *reinterpret_cast<const uint16_t*>(row + e / 2);
+      g = groups[e / 16];
+    } else if constexpr (FMT != CKV_CACHE_PLAIN) {
       w[0] = *reinterpret_cast<const uint32_t*>(row + e);
     } else if constexpr (sizeof(T) == 2) {
       const uint2 v = *reinterpret_cast<const uint2*>(row + e * 2);
@@ -42,6 +47,11 @@ template <typename T, int FMT> struct Four {
   __device__ __forceinline__ void get(float (&x)[4]) const {
     if constexpr (FMT != CKV_CACHE_PLAIN) {
       decode4<FMT>(w[0], x);
+      if constexpr (FMT == CKV_CACHE_E2M1) {
+        const float s = e4m3_to_float(g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] *= s;
+      }
     } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -68,7 +78,7 @@ template <int DH, int kQ> struct Shared {   // kQ: query rows an item
 // CTAs an SM: four where the sums of four query rows leave the registers for it, three with eight (two to four measured)
 template <typename T, int FMT, int DH, int kQ>
 __global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_kernel(DecodeArgs p) {
-  constexpr int ROW_BYTES = DH * (FMT == CKV_CACHE_PLAIN ? (int)sizeof(T) : 1);
+  constexpr int ROW_BYTES = FMT == CKV_CACHE_PLAIN ? DH * (int)sizeof(T) : FMT == CKV_CACHE_E2M1 ? DH / 2 : DH;
   constexpr int PIECES = DH / 16;               // pieces of four elements a quad lane has of a row
   constexpr int LPR = DH / 4, KPI = 32 / LPR;   // values: lanes a row, rows at a time
   constexpr int WL = 32 / kQ, WR = kWarpRows / WL;   // weights: lanes a query row, cache rows a lane
@@ -125,6 +135,8 @@ __global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_k
       const long long slot = ((long long)at_page << p.c.page_shift) + in_page;
       const char* K = p.c.page[0] + off;
       const char* V = p.c.page[1] + off;
+      const uint8_t* gk = FMT == CKV_CACHE_E2M1 ? p.c.group[0] + slot * (DH / 16) : nullptr;
+      const uint8_t* gv = FMT == CKV_CACHE_E2M1 ? p.c.group[1] + slot * (DH / 16) : nullptr;
 
       // ---- logits
       Four<T, FMT> k[2][PIECES];
@@ -135,7 +147,7 @@ __global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_k
         ks[h] = (FMT != CKV_CACHE_PLAIN && i < here) ? p.c.scale[0][slot + i] : 1.f;
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
-          if (i < here) k[h][j].load(K + i * ROW_BYTES, 4 * c + 16 * j);
+          if (i < here) k[h][j].load(K + i * ROW_BYTES, gk + i * (DH / 16), 4 * c + 16 * j);
           else k[h][j].clear();
         }
       }
@@ -144,7 +156,7 @@ __global__ void __launch_bounds__(kDecodeThreads, kQ == 4 ? 4 : 3) decode_simt_k
 #pragma unroll
         for (int j = 0; j < 8 / KPI; ++j) {
           const int i = b + j * KPI + lane / LPR;
-          if (i < here) v[j].load(V + i * ROW_BYTES, 4 * (lane % LPR));
+          if (i < here) v[j].load(V + i * ROW_BYTES, gv + i * (DH / 16), 4 * (lane % LPR));
           else v[j].clear();
         }
       };
@@ -280,6 +292,8 @@ template <typename T> cudaError_t by_format(const DecodeArgs& p, int format, int
     return dh == 64 ? launch<T, CKV_CACHE_PLAIN, 64>(p, device, sm_count, st, launches) : launch<T, CKV_CACHE_PLAIN, 128>(p, device, sm_count, st, launches);
   if (format == CKV_CACHE_E4M3)
     return dh == 64 ? launch<T, CKV_CACHE_E4M3, 64>(p, device, sm_count, st, launches) : launch<T, CKV_CACHE_E4M3, 128>(p, device, sm_count, st, launches);
+  if (format == CKV_CACHE_E2M1)
+    return dh == 64 ? launch<T, CKV_CACHE_E2M1, 64>(p, device, sm_count, st, launches) : launch<T, CKV_CACHE_E2M1, 128>(p, device, sm_count, st, launches);
   return dh == 64 ? launch<T, CKV_CACHE_INT8, 64>(p, device, sm_count, st, launches) : launch<T, CKV_CACHE_INT8, 128>(p, device, sm_count, st, launches);
 }
 

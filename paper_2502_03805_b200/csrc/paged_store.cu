@@ -6,10 +6,8 @@
 // 6553 of 32768 rows of 128 bf16 each to e4m3: 58 us, 5.6 TB/s (101 us with 16 bytes a lane, 87 us with 16 warps an SM).
 // Load: 16 bytes of output a lane, four rows of K and V in flight.  8 x 8 heads of 6553 e4m3 rows of 128 to bf16: 55 us,
 // 6.0 TB/s.
-#include <cuda_bf16.h>
-
 #include "launch_early.cuh"
-#include "paged_common.cuh"
+#include "paged_codes.cuh"
 
 namespace ckv {
 namespace {
@@ -19,71 +17,40 @@ constexpr int kStoreThreads = 128, kStoreCtas = 8;
 constexpr int kRows = 4;          // load: rows of K and V in flight per thread
 constexpr int kPieces = 4;        // store: 16-byte pieces of a row per lane
 
-// (a, b) rounded to two e4m3 codes, a in the low byte.
-__device__ __forceinline__ uint32_t e4m3x2(float a, float b) {
-  uint16_t v;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(b), "f"(a));
-  return v;
-}
-
-// 16 bytes of a source row as floats.
-template <typename T> struct Piece;
-template <> struct Piece<float> {
-  static constexpr int V = 4;
-  static __device__ __forceinline__ void get(const uint4& r, float (&x)[4]) {
-    x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
-  }
-  static __device__ __forceinline__ uint4 put(const float (&x)[4]) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-  }
-};
-__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-template <> struct Piece<__nv_bfloat16> {
-  static constexpr int V = 8;
-  static __device__ __forceinline__ void get(const uint4& r, float (&x)[8]) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ uint4 put(const float (&x)[8]) {
-    return make_uint4(bf16x2(x[0], x[1]), bf16x2(x[2], x[3]), bf16x2(x[4], x[5]), bf16x2(x[6], x[7]));
-  }
-};
-
-// Scale and codes of a row piece (criticalkv.h states the rule).  The row's largest magnitude is found on the bit
-// patterns, whose order puts NaN above infinity, so a row with a NaN gets a NaN scale.
+// Scale and codes of a row piece; LANES lanes share the row.
 template <int FMT, int LANES, int N>
 __device__ __forceinline__ float quantise(const float (&x)[N], uint32_t (&code)[N / 4]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  uint32_t top = top_bits(x);
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  constexpr float kTop = FMT == CKV_CACHE_E4M3 ? 448.f : 127.f;
-  float scale = __fdiv_rn(__uint_as_float(top), kTop);
-  if (scale < kLeastScale) scale = kLeastScale;
-  // a row that reaches the largest float must not read back as infinity because the quotient was rounded up
-  if (top < 0x7f800000u && __fmul_rn(scale, kTop) == INFINITY) scale = __uint_as_float(__float_as_uint(scale) - 1);
+  const float scale = row_scale<FMT>(top);
   const float r = __frcp_rn(scale);
 #pragma unroll
-  for (int i = 0; i < N / 4; ++i) {
-    float y[4];
+  for (int i = 0; i < N / 4; ++i) code[i] = encode4<FMT>(x + 4 * i, r);
+  return scale;
+}
+
+// The same for a 4-bit row, of which a lane has N / 16 whole groups: codes of eight elements a word, a scale a byte.
+template <int LANES, int N>
+__device__ __forceinline__ float quantise_e2m1(const float (&x)[N], uint32_t (&code)[N / 8], uint32_t& groups) {
+  uint32_t of_group[N / 16], top = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = __fmul_rn(x[4 * i + j], r);
-    if (FMT == CKV_CACHE_E4M3) {
-      code[i] = e4m3x2(y[0], y[1]) | (e4m3x2(y[2], y[3]) << 16);
-    } else {
-      code[i] = 0;
+  for (int g = 0; g < N / 16; ++g) {
+    of_group[g] = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        code[i] |= ((uint32_t)min(max(__float2int_rn(y[j]), -127), 127) & 0xffu) << (8 * j);   // NaN becomes 0
-    }
+    for (int i = 0; i < 16; ++i) of_group[g] = max(of_group[g], __float_as_uint(x[16 * g + i]) & 0x7fffffffu);
+    top = max(top, of_group[g]);
+  }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float scale = row_scale<CKV_CACHE_E2M1>(top), r = __frcp_rn(scale);
+  groups = 0;
+#pragma unroll
+  for (int g = 0; g < N / 16; ++g) {
+    float factor;
+    groups |= group_scale(__uint_as_float(of_group[g]), r, top < 0x7f800000u, factor) << (8 * g);
+    code[2 * g] = encode8_e2m1(x + 16 * g, factor);
+    code[2 * g + 1] = encode8_e2m1(x + 16 * g + 8, factor);
   }
   return scale;
 }
@@ -131,6 +98,9 @@ template <typename T, int FMT, int DH>
 __global__ void __launch_bounds__(kStoreThreads, kStoreCtas) store_kernel(StoreArgs p) {
   wait_for_previous_kernel();
   constexpr int V = Piece<T>::V, LANES = store_lanes(DH * (int)sizeof(T)), ROWS = kStoreThreads / LANES;   // rows a pass
+  // A lane's pieces of a row: LANES apart, so that the lanes of a row read it side by side; one behind the other for
+  // 4-bit codes, so that a lane has whole groups and writes 8 or 16 bytes of codes at once.
+  constexpr int FIRST = FMT == CKV_CACHE_E2M1 ? kPieces * 16 : 16, STEP = FMT == CKV_CACHE_E2M1 ? 16 : LANES * 16;
   const int item = blockIdx.x / p.chunks, chunk = blockIdx.x % p.chunks;
   const int s = item / p.c.Hkv, g = item % p.c.Hkv;
   const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
@@ -165,11 +135,11 @@ __global__ void __launch_bounds__(kStoreThreads, kStoreCtas) store_kernel(StoreA
     uint4 raw[2][kPieces];
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const char* src = p.src[w] + s * p.ss[0] + g * p.ss[1] + from * p.ss[2] + lane * 16;
+      const char* src = p.src[w] + s * p.ss[0] + g * p.ss[1] + from * p.ss[2] + lane * FIRST;
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) {
         raw[w][j] = make_uint4(0, 0, 0, 0);
-        if (slot >= 0) raw[w][j] = *reinterpret_cast<const uint4*>(src + j * LANES * 16);
+        if (slot >= 0) raw[w][j] = *reinterpret_cast<const uint4*>(src + j * STEP);
       }
     }
     base += step;
@@ -187,7 +157,6 @@ __global__ void __launch_bounds__(kStoreThreads, kStoreCtas) store_kernel(StoreA
           if (slot >= 0) *reinterpret_cast<uint4*>(to + j * LANES * 16) = raw[w][j];
       } else {
         float x[kPieces * V];
-        uint32_t code[kPieces * V / 4];
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
           float piece[V];
@@ -195,6 +164,24 @@ __global__ void __launch_bounds__(kStoreThreads, kStoreCtas) store_kernel(StoreA
 #pragma unroll
           for (int i = 0; i < V; ++i) x[V * j + i] = piece[i];
         }
+        if constexpr (FMT == CKV_CACHE_E2M1) {
+          uint32_t code[kPieces * V / 8], groups;
+          const float scale = quantise_e2m1<LANES>(x, code, groups);
+          char* to = p.c.page[w] + page_at + in_page * (DH / 2) + lane * (kPieces * V / 2);
+          uint8_t* group = p.c.group[w] + slot * (DH / 16) + lane * (kPieces * V / 16);
+          if (slot >= 0) {
+            if constexpr (V == 8) {
+              *reinterpret_cast<uint4*>(to) = make_uint4(code[0], code[1], code[2 % (kPieces * V / 8)], code[3 % (kPieces * V / 8)]);
+              *reinterpret_cast<uint16_t*>(group) = (uint16_t)groups;
+            } else {
+              *reinterpret_cast<uint2*>(to) = make_uint2(code[0], code[1]);
+              *group = (uint8_t)groups;
+            }
+            if (lane == 0) p.c.scale[w][slot] = scale;
+          }
+          continue;
+        }
+        uint32_t code[kPieces * V / 4];
         const float scale = quantise<FMT, LANES>(x, code);
         char* to = p.c.page[w] + page_at + in_page * DH + lane * V;
         if (slot >= 0) {
@@ -284,16 +271,22 @@ __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
             *reinterpret_cast<uint4*>(p.dst[w] + s * p.ds[0] + g * p.ds[1] + (at + base + u * RPP + sub) * p.ds[2] +
                                       lane * 16) = raw[u][w];
     } else {
-      uint32_t code[kRows][2][V / 4];
+      uint32_t code[kRows][2][V / 4];     // e2m1: all V codes in the first
       float scale[kRows][2];
+      uint32_t group[kRows][2];
 #pragma unroll
       for (int u = 0; u < kRows; ++u)
 #pragma unroll
         for (int w = 0; w < 2; ++w)
           if (slot[u] >= 0) {
+            constexpr int PART = FMT == CKV_CACHE_E2M1 ? 2 : 1;     // codes a byte
             const char* row = p.c.page[w] + (slot[u] >> p.c.page_shift) * p.c.page_stride +
-                              (slot[u] & ((1 << p.c.page_shift) - 1)) * DH + lane * V;
-            if constexpr (V == 8) {
+                              (slot[u] & ((1 << p.c.page_shift) - 1)) * (DH / PART) + lane * (V / PART);
+            if constexpr (FMT == CKV_CACHE_E2M1) {
+              if constexpr (V == 8) code[u][w][0] = *reinterpret_cast<const uint32_t*>(row);
+              else code[u][w][0] = *reinterpret_cast<const uint16_t*>(row);
+              group[u][w] = p.c.group[w][slot[u] * (DH / 16) + lane * V / 16];
+            } else if constexpr (V == 8) {
               const uint2 v = *reinterpret_cast<const uint2*>(row);
               code[u][w][0] = v.x;
               code[u][w][V / 4 - 1] = v.y;
@@ -311,7 +304,14 @@ __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
 #pragma unroll
             for (int i = 0; i < V / 4; ++i) {
               float y[4];
-              decode4<FMT>(code[u][w][i], y);
+              if constexpr (FMT == CKV_CACHE_E2M1) {
+                decode4<FMT>(code[u][w][0] >> (16 * i), y);
+                const float g = e4m3_to_float(group[u][w]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] *= g;
+              } else {
+                decode4<FMT>(code[u][w][i], y);
+              }
 #pragma unroll
               for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * scale[u][w];
             }
@@ -332,6 +332,7 @@ template <typename F> void by_type(const CacheDims& d, F&& f) {
   auto formats = [&](auto t) {
     if (d.format == CKV_CACHE_PLAIN) dims(t, std::integral_constant<int, CKV_CACHE_PLAIN>());
     else if (d.format == CKV_CACHE_E4M3) dims(t, std::integral_constant<int, CKV_CACHE_E4M3>());
+    else if (d.format == CKV_CACHE_E2M1) dims(t, std::integral_constant<int, CKV_CACHE_E2M1>());
     else dims(t, std::integral_constant<int, CKV_CACHE_INT8>());
   };
   if (d.dtype == CKV_F32) formats(float());
