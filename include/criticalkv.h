@@ -279,8 +279,12 @@ CKV_API int criticalkv_diagnose(criticalkv_handle h, const criticalkv_desc* d, c
  *
  *   criticalkv_rope         rotary positions of new queries and keys (a new token's position is not its row number)
  *   criticalkv_cache_store  writes rows into the pages: new tokens, or the rows a selection kept; quantises them
+ *   criticalkv_cache_append the two above in one launch: new tokens' queries and keys rotated, keys and values written
  *   criticalkv_cache_load   reads rows back into a dense tensor, for another compression step
  *   criticalkv_decode       attention of one new token per sequence over the pages
+ *   criticalkv_summarise_pages, criticalkv_select_pages
+ *                           the pages that score best against the new token's queries, as a page table of their own that
+ *                           criticalkv_decode reads: attention over a part of a long cache
  *
  * Page ids outside [0, num_pages), row numbers outside the table and lengths outside [0, max_pages * page_size] never
  * cause an access outside a buffer: such rows are skipped (store, load), treated as absent (decode), lengths are
@@ -368,6 +372,19 @@ CKV_API int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* 
                                    void* stream);
 
 /*
+ * New tokens into the cache: criticalkv_rope on q and k, then criticalkv_cache_store of the rotated k (rounded to dtype in
+ * between) and of v, in one launch.  r describes q, k and q_out as for criticalkv_rope (nseq, Hq, Hk = Hkv, dh and dtype
+ * those of the cache, k_out_stride 0); v [nseq, Hkv, T, dh] has strides of its own (v_stride[3], NULL or 0 entries = dense).
+ * Tokens 0..counts[s]-1 of a sequence (device int32 [nseq]; NULL: all T) go behind row start[s, g] of every head; the others
+ * are ignored, their rows of q_out keep their contents.  q_out may be q (same strides); start and lens_out as for
+ * criticalkv_cache_store.
+ */
+CKV_API int criticalkv_cache_append(criticalkv_handle h, const criticalkv_cache* c, const criticalkv_rope_desc* r,
+                                    const void* q, const void* k, const void* v, const int64_t* v_stride, const int32_t* pos,
+                                    const double* freq, const int32_t* counts, const int32_t* start, void* q_out,
+                                    int32_t* lens_out, void* stream);
+
+/*
  * Rows out of the cache.  K_out, V_out [nseq, Hkv, n, dh] (strides as above).  With align_right == 0 row i of head
  * (s, g) goes to row i for i < min(lens[s,g], n); with align_right == 1 the last min(lens, n) rows end at row n-1,
  * the layout that criticalkv_desc.valid_from = n - lens describes.  Other rows of the outputs keep their contents.
@@ -391,6 +408,35 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
 CKV_API int criticalkv_decode_workspace_bytes(const criticalkv_cache* c, size_t* bytes);
 CKV_API int criticalkv_decode(criticalkv_handle h, const criticalkv_cache* c, const void* q, const int64_t* q_stride,
                               const int32_t* lens, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over a part of a long cache.  A page is summarised by the largest and the smallest value of every channel over
+ * its keys (as the pages stand for them, float32); a query is at most as large against any of its keys as the sum over the
+ * channels of the larger of query * largest and query * smallest.
+ *
+ * criticalkv_summarise_pages writes the summaries of the pages that hold rows start[s, g] .. lens[s, g]-1 of every head
+ * (start NULL: 0), over all rows that a page holds up to lens: codes int8 [num_pages, 2, dh] (largest, smallest), scales
+ * float32 [num_pages], by page id; others keep their contents.  With top the largest magnitude in the page: scale = max(top /
+ * 127, 2^-100), r = 1 / scale, largest code = ceil(largest * r), smallest = floor(smallest * r), within -127..127, every
+ * operation a float32 one.  A page with an infinity or a NaN gets that scale and codes 0.  A page that several heads or
+ * sequences share must hold equally many rows for all of them.
+ *
+ * criticalkv_select_pages scores the pages of a head and chooses `count` of them: the first `first` and the last `last` ones
+ * (first + last <= count), then those with the largest score, the lower page where two are equal.  Score: the group's
+ * queries as codes, scale_q = max(max |q| / 127, 2^-100), code = q * (1 / scale_q) rounded to nearest even; sum (exact, of
+ * whole numbers) over the channels of max(code * largest, code * smallest), as a float32 times scale_q, times the page's
+ * scale; the largest over the query heads of the group.  A score that is NaN counts as the largest, a page id outside the
+ * pool as the smallest.  table_out int32 [nseq, Hkv, count]: the ids of the chosen pages in the order of their rows, -1
+ * behind them; lens_out [nseq, Hkv]: the rows they hold; chosen (may be NULL) [nseq, Hkv, count]: which pages of the head
+ * they are.  criticalkv_decode with page_table = table_out, max_pages = count and lens = lens_out attends to them.  The
+ * outputs must not overlap each other or what is read.  CKV_ENOTSUP for Hq/Hkv > 128, max_pages > 32768, nseq * Hkv > 2^26.
+ */
+CKV_API int criticalkv_summarise_pages(criticalkv_handle h, const criticalkv_cache* c, const int32_t* start,
+                                       const int32_t* lens, int8_t* codes, float* scales, void* stream);
+CKV_API int criticalkv_select_pages(criticalkv_handle h, const criticalkv_cache* c, const void* q, const int64_t* q_stride,
+                                    const int32_t* lens, const int8_t* codes, const float* scales, int32_t count,
+                                    int32_t first, int32_t last, int32_t* table_out, int32_t* lens_out, int32_t* chosen,
+                                    void* stream);
 
 /*
  * Self-test of the bounded device-side wait every tensor-core kernel uses: launches one CTA that waits, for at most

@@ -35,7 +35,8 @@ EXPORTS = ("criticalkv_create", "criticalkv_destroy", "criticalkv_workspace_byte
            "criticalkv_select_static", "criticalkv_compact", "criticalkv_gather_positions", "criticalkv_compress",
            "criticalkv_host_staging_bytes", "criticalkv_compress_host", "criticalkv_selftest_bounded_wait",
            "criticalkv_diagnose_workspace_bytes", "criticalkv_diagnose", "criticalkv_rope",
-           "criticalkv_cache_store", "criticalkv_cache_load", "criticalkv_decode_workspace_bytes",
+           "criticalkv_cache_store", "criticalkv_cache_append", "criticalkv_cache_load", "criticalkv_summarise_pages",
+           "criticalkv_select_pages", "criticalkv_decode_workspace_bytes",
            "criticalkv_decode", "criticalkv_device_status",
            "criticalkv_status_string", "criticalkv_last_cuda_error", "criticalkv_last_path",
            "criticalkv_launch_count")
@@ -106,6 +107,9 @@ def load():
     lib.criticalkv_rope.argtypes = [vp, rp, vp, vp, vp, vp, vp, vp, vp]
     lib.criticalkv_cache_store.argtypes = [vp, cp, vp, vp, C.c_int32, i64p, vp, vp, C.c_int64, vp, vp, vp, vp]
     lib.criticalkv_cache_load.argtypes = [vp, cp, vp, C.c_int32, i64p, C.c_int32, vp, vp, vp]
+    lib.criticalkv_cache_append.argtypes = [vp, cp, rp, vp, vp, vp, i64p, vp, vp, vp, vp, vp, vp, vp]
+    lib.criticalkv_summarise_pages.argtypes = [vp, cp, vp, vp, vp, vp, vp]
+    lib.criticalkv_select_pages.argtypes = [vp, cp, vp, i64p, vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp]
     lib.criticalkv_decode_workspace_bytes.argtypes = [cp, C.POINTER(sz)]
     lib.criticalkv_decode.argtypes = [vp, cp, vp, i64p, vp, vp, vp, vp, sz, vp]
     lib.criticalkv_selftest_bounded_wait.argtypes = [vp, C.c_uint64, vp, vp]
@@ -339,6 +343,28 @@ def criticalkv_cache_load(handle, cache, lens, n, stride, align_right, K_out, V_
     rc = load().criticalkv_cache_load(handle, C.byref(cache), _ptr(lens), n, _strides(stride), int(align_right),
                                       _ptr(K_out), _ptr(V_out), _stream(stream))
     return _check(handle, rc, "criticalkv_cache_load", check)
+
+
+def criticalkv_cache_append(handle, cache, rope, q, k, v, v_stride, pos, freq, counts, start, q_out, lens_out, stream=None,
+                            check=True):
+    rc = load().criticalkv_cache_append(handle, C.byref(cache), C.byref(rope), _ptr(q), _ptr(k), _ptr(v), _strides(v_stride),
+                                        _ptr(pos), _ptr(freq), _ptr(counts), _ptr(start), _ptr(q_out), _ptr(lens_out),
+                                        _stream(stream))
+    return _check(handle, rc, "criticalkv_cache_append", check)
+
+
+def criticalkv_summarise_pages(handle, cache, start, lens, codes, scales, stream=None, check=True):
+    rc = load().criticalkv_summarise_pages(handle, C.byref(cache), _ptr(start), _ptr(lens), _ptr(codes), _ptr(scales),
+                                           _stream(stream))
+    return _check(handle, rc, "criticalkv_summarise_pages", check)
+
+
+def criticalkv_select_pages(handle, cache, q, q_stride, lens, codes, scales, count, first, last, table_out, lens_out, chosen,
+                            stream=None, check=True):
+    rc = load().criticalkv_select_pages(handle, C.byref(cache), _ptr(q), _strides(q_stride), _ptr(lens), _ptr(codes),
+                                        _ptr(scales), count, first, last, _ptr(table_out), _ptr(lens_out), _ptr(chosen),
+                                        _stream(stream))
+    return _check(handle, rc, "criticalkv_select_pages", check)
 
 
 def criticalkv_decode_workspace_bytes(cache):

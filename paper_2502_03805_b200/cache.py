@@ -257,6 +257,14 @@ class Rotary(_Owner):
                                 k_out_stride=kos or zero)
 
 
+class PageSummary:
+    """The largest and smallest key of every page of a PagedCache: codes int8 [num_pages, 2, dh], scale float32 [num_pages]
+    (PagedCache.new_summary makes one, PagedCache.summarise fills it)."""
+
+    def __init__(self, codes, scale):
+        self.codes, self.scale = codes, scale
+
+
 class PagedCache(_Owner):
     """A paged KV cache whose heads have lengths of their own.
 
@@ -315,6 +323,9 @@ class PagedCache(_Owner):
         self._take_handle(handle, dev)
         self._decode, self._store = self._lib.criticalkv_decode, self._lib.criticalkv_cache_store
         self._load = self._lib.criticalkv_cache_load
+        self._append, self._select = self._lib.criticalkv_cache_append, self._lib.criticalkv_select_pages
+        self._parts = {}                 # descriptions of the cache with chosen pages, by their number
+        self._chosen = {}                # tables of chosen pages, by stream and number
 
     @classmethod
     def allocate(cls, *, nseq, Hq, Hkv, dh, dtype, rows, format="plain", page_size=64, device=0, **kw):
@@ -389,6 +400,139 @@ class PagedCache(_Owner):
             _need(counts, "counts", (self.nseq,), torch.int32, dev)
         return (0 if idx is not None and idx_rows == 0 else n), idx_rows, B._strides(strides)
 
+    def append(self, q, k, v, positions, rotary, start, lens_out=None, *, q_out=None, counts=None, stream=None):
+        """New tokens: rotary.rotate of q [nseq, Hq, T, dh] and k [nseq, Hkv, T, dh], then store of the rotated k and of v
+        [nseq, Hkv, T, dh] behind row start[s, g] of every head, in one launch and with the same bits.  The three may be
+        parts of one projection, each with strides of its own; q_out may be q.  With counts only the first counts[s] tokens
+        of a sequence are taken (the other rows of q_out keep their contents).  Returns (q_out, lens_out); lens_out may be
+        `start`, both are allocated when None."""
+        if q_out is None or lens_out is None:
+            with self._allocating(stream):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device) if q_out is None else q_out
+                lens_out = torch.empty((self.nseq, self.Hkv), dtype=torch.int32, device=self.device) if lens_out is None else lens_out
+        key = (rotary.dh, rotary.rot, rotary.layout, rotary.factor, rotary.device, q.dtype, q.shape, q.stride(), q.get_device(),
+               k.dtype, k.shape, k.stride(), k.get_device(), v.dtype, v.shape, v.stride(), v.get_device(), positions.dtype,
+               positions.shape, positions.stride(), positions.get_device(), start.dtype, start.shape, start.stride(),
+               start.get_device(), lens_out.dtype, lens_out.shape, lens_out.stride(), lens_out.get_device(), q_out.dtype,
+               q_out.shape, q_out.stride(), q_out.get_device(), _sig(counts))
+        desc, strides = self._plans.get(key) or self._keep(
+            key, self._describe_append(q, k, v, positions, rotary, start, lens_out, q_out, counts))
+        raw = self._where(stream)
+        rotary._where(stream)                    # its frequencies are read there
+        rc = self._append(
+            self.handle, self._ref, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), strides, positions.data_ptr(),
+            rotary._freq_at, None if counts is None else counts.data_ptr(), start.data_ptr(), q_out.data_ptr(),
+            lens_out.data_ptr(), raw)
+        if rc:
+            self._fail(rc, "criticalkv_cache_append")
+        return q_out, lens_out
+
+    def _describe_append(self, q, k, v, positions, rotary, start, lens_out, q_out, counts):
+        dev = self.device
+        if rotary.device != dev or rotary.dh != self.dh:
+            raise ValueError(f"rotary: need one for heads of {self.dh} on {dev}, got {rotary.dh} on {rotary.device}")
+        if q.dim() != 4:
+            raise ValueError("q must be [nseq, Hq, T, dh]")
+        T = q.shape[2]
+        _need(q, "q", (self.nseq, self.Hq, T, self.dh), self.torch_dtype, dev, dense=False)
+        for t, what in ((k, "k"), (v, "v")):
+            _need(t, what, (self.nseq, self.Hkv, T, self.dh), self.torch_dtype, dev, dense=False)
+        _need(q_out, "q_out", q.shape, self.torch_dtype, dev, dense=False)
+        _need(positions, "positions", (self.nseq, T), torch.int32, dev)
+        _need(start, "start", (self.nseq, self.Hkv), torch.int32, dev)
+        _need(lens_out, "lens_out", (self.nseq, self.Hkv), torch.int32, dev)
+        if counts is not None:
+            _need(counts, "counts", (self.nseq,), torch.int32, dev)
+        zero = (0, 0, 0)
+        desc = B.make_rope_desc(nseq=self.nseq, T=T, Hq=self.Hq, Hk=self.Hkv, dh=self.dh, rot=rotary.rot, dtype=self.dtype,
+                                layout=rotary.layout, factor=rotary.factor, q_stride=_row_strides(q, "q") or zero,
+                                k_stride=_row_strides(k, "k") or zero, q_out_stride=_row_strides(q_out, "q_out") or zero)
+        return desc, B._strides(_row_strides(v, "v"))
+
+    def new_summary(self):
+        """A summary of no pages."""
+        return PageSummary(torch.zeros((self.num_pages, 2, self.dh), dtype=torch.int8, device=self.device),
+                           torch.zeros((self.num_pages,), dtype=torch.float32, device=self.device))
+
+    def _check_summary(self, summary):
+        _need(summary.codes, "summary.codes", (self.num_pages, 2, self.dh), torch.int8, self.device)
+        _need(summary.scale, "summary.scale", (self.num_pages,), torch.float32, self.device)
+
+    def summarise(self, summary, lens, start=None, stream=None):
+        """Brings the summary of the pages that hold rows start[s, g] .. lens[s, g]-1 of every head (all rows without
+        `start`) in line with the keys in them: after a prompt has been stored, and with the lengths before it after each
+        store or append.  Pages that heads share must be full, or hold equally many rows for all."""
+        key = ("summarise", lens.dtype, lens.shape, lens.stride(), lens.get_device(), _sig(start), _sig(summary.codes),
+               _sig(summary.scale))
+        if key not in self._plans:
+            for t, what in ((lens, "lens"), (start, "start")):
+                if t is not None:
+                    _need(t, what, (self.nseq, self.Hkv), torch.int32, self.device)
+            self._check_summary(summary)
+            self._keep(key, True)
+        rc = self._lib.criticalkv_summarise_pages(
+            self.handle, self._ref, None if start is None else start.data_ptr(), lens.data_ptr(), summary.codes.data_ptr(),
+            summary.scale.data_ptr(), self._where(stream))
+        if rc:
+            self._fail(rc, "criticalkv_summarise_pages")
+        return summary
+
+    def select_pages(self, q, lens, summary, pages, *, first=1, last=1, table=None, rows=None, chosen=None, stream=None):
+        """The `pages` pages of every head that score best against q [nseq, Hq, dh], the first `first` and the last `last`
+        ones among them.  Returns (table int32 [nseq, Hkv, pages], -1 behind the last chosen page; rows int32 [nseq, Hkv],
+        how many rows those pages hold): attend(q, rows, table=table) looks at them.  chosen int32 [nseq, Hkv, pages], when
+        given, receives which pages of a head they are."""
+        if table is None or rows is None:
+            with self._allocating(stream):
+                shape = (self.nseq, self.Hkv)
+                table = torch.empty((*shape, pages), dtype=torch.int32, device=self.device) if table is None else table
+                rows = torch.empty(shape, dtype=torch.int32, device=self.device) if rows is None else rows
+        key = ("select", pages, q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(), lens.get_device(),
+               table.dtype, table.shape, table.stride(), table.get_device(), rows.dtype, rows.shape, rows.stride(),
+               rows.get_device(), _sig(chosen), _sig(summary.codes), _sig(summary.scale))
+        strides = self._plans.get(key) or self._keep(key, self._describe_select(q, lens, summary, pages, table, rows, chosen))
+        rc = self._select(self.handle, self._ref, q.data_ptr(), strides[0], lens.data_ptr(), summary.codes.data_ptr(),
+                          summary.scale.data_ptr(), pages, first, last, table.data_ptr(), rows.data_ptr(),
+                          None if chosen is None else chosen.data_ptr(), self._where(stream))
+        if rc:
+            self._fail(rc, "criticalkv_select_pages")
+        return table, rows
+
+    def _describe_select(self, q, lens, summary, pages, table, rows, chosen):
+        dev, shape = self.device, (self.nseq, self.Hkv)
+        _need(q, "q", self._out_shape, self.torch_dtype, dev, dense=False)
+        _need(lens, "lens", shape, torch.int32, dev)
+        _need(rows, "rows", shape, torch.int32, dev)
+        _need(table, "table", (*shape, pages), torch.int32, dev)
+        if chosen is not None:
+            _need(chosen, "chosen", (*shape, pages), torch.int32, dev)
+        self._check_summary(summary)
+        return (B._strides(_row_strides(q, "q")),)
+
+    def attend_selected(self, q, lens, summary, pages, out=None, lse=None, *, first=1, last=1, ws=None, stream=None):
+        """attend over the `pages` pages that select_pages chooses: (out, lse) of one new token per sequence."""
+        if stream is None:
+            table, rows = self._selection(_raw_stream(self._index), pages)
+        else:
+            with self._allocating(stream):
+                table, rows = self._selection(self._on(stream), pages)
+        self.select_pages(q, lens, summary, pages, first=first, last=last, table=table, rows=rows, stream=stream)
+        return self.attend(q, rows, out, lse, ws=ws, table=table, stream=stream)
+
+    def _selection(self, raw, pages):
+        """Table and lengths of the chosen pages, kept like the workspaces.  raw: the current stream."""
+        captured = self._captured()
+        both = None if captured else self._chosen.get((raw, pages))
+        if both is None:
+            n = self.nseq * self.Hkv
+            whole = torch.empty(n * (pages + 1), dtype=torch.int32, device=self.device)
+            both = whole[:n * pages].view(self.nseq, self.Hkv, pages), whole[n * pages:].view(self.nseq, self.Hkv)
+            if not captured:
+                if len(self._chosen) >= 64:
+                    self._chosen.clear()
+                self._chosen[raw, pages] = both
+        return both
+
     def load(self, lens, n=None, K_out=None, V_out=None, *, align_right=False, stream=None):
         """Rows 0..min(lens, n)-1 of every head as K_out, V_out [nseq, Hkv, n, dh] (zeros where there is no row, when
         allocated here; left as they were in a caller's tensor).  align_right puts the last rows of a head at the end,
@@ -431,14 +575,16 @@ class PagedCache(_Owner):
         with self._allocating(stream):
             return self._workspace(self._on(stream))
 
+    def _captured(self):
+        """Whether the current stream of the cache's device is being captured."""
+        if _current_device() == self._index:
+            return _capturing()
+        with torch.cuda.device(self._index):
+            return _capturing()
+
     def _workspace(self, raw):
         """raw: the current stream."""
-        if _current_device() == self._index:
-            captured = _capturing()
-        else:
-            with torch.cuda.device(self._index):
-                captured = _capturing()
-        if captured:
+        if self._captured():
             return torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
         ws = self._ws.get(raw)
         if ws is None:
@@ -447,12 +593,14 @@ class PagedCache(_Owner):
             ws = self._ws[raw] = torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
         return ws
 
-    def attend(self, q, lens, out=None, lse=None, *, ws=None, stream=None):
+    def attend(self, q, lens, out=None, lse=None, *, ws=None, table=None, stream=None):
         """Attention of one new token per sequence: q [nseq, Hq, dh] over the lens[s, g] rows of every head.  Returns
-        (out [nseq, Hq, dh], lse float32 [nseq, Hq])."""
+        (out [nseq, Hq, dh], lse float32 [nseq, Hq]).  table: int32 [nseq, Hkv, columns], another page table in place of
+        the cache's own (select_pages makes them)."""
         key = (q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(), lens.get_device(),
-               _sig(out), _sig(lse), _sig(ws))
-        strides, size = self._plans.get(key) or self._keep(key, self._describe_attend(q, lens, out, lse, ws))
+               _sig(out), _sig(lse), _sig(ws), _sig(table))
+        strides, size = self._plans.get(key) or self._keep(key, self._describe_attend(q, lens, out, lse, ws, table))
+        ref = self._ref if table is None else self._part(table)
         raw = self._where(stream)
         if stream is None:
             out = torch.empty_like(self._out_like) if out is None else out
@@ -463,13 +611,26 @@ class PagedCache(_Owner):
                 out = torch.empty_like(self._out_like) if out is None else out
                 lse = torch.empty_like(self._lse_like) if lse is None else lse
                 ws = self._workspace(raw) if ws is None else ws
-        rc = self._decode(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(), lse.data_ptr(),
+        rc = self._decode(self.handle, ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(), lse.data_ptr(),
                           ws.data_ptr(), size, raw)
         if rc:
             self._fail(rc, "criticalkv_decode")
         return out, lse
 
-    def _describe_attend(self, q, lens, out, lse, ws):
+    def _part(self, table):
+        """The cache's description with another page table (used at once: descriptions are shared by their columns)."""
+        columns = table.shape[2]
+        part = self._parts.get(columns)
+        if part is None:
+            desc = type(self.desc).from_buffer_copy(self.desc)
+            desc.max_pages = columns
+            if len(self._parts) >= 64:
+                self._parts.clear()
+            part = self._parts[columns] = desc, C.byref(desc)
+        part[0].page_table = table.data_ptr()
+        return part[1]
+
+    def _describe_attend(self, q, lens, out, lse, ws, table):
         dev, shape = self.device, self._out_shape
         _need(q, "q", shape, self.torch_dtype, dev, dense=False)
         _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, dev)
@@ -477,6 +638,10 @@ class PagedCache(_Owner):
             _need(out, "out", shape, self.torch_dtype, dev)
         if lse is not None:
             _need(lse, "lse", shape[:2], torch.float32, dev)
+        if table is not None:
+            if table.dim() != 3 or table.shape[2] < 1:
+                raise ValueError("table must be [nseq, Hkv, columns]")
+            _need(table, "table", (self.nseq, self.Hkv, table.shape[2]), torch.int32, dev)
         if ws is not None and (ws.device != dev or not ws.is_contiguous()):
             raise ValueError(f"ws must be contiguous on {dev}")
         return B._strides(_row_strides(q, "q")), self._ws_bytes if ws is None else ws.numel() * ws.element_size()

@@ -153,6 +153,48 @@ int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* c, const
   return record_cuda(h, e);
 }
 
+int criticalkv_cache_append(criticalkv_handle h, const criticalkv_cache* c, const criticalkv_rope_desc* r, const void* q,
+                            const void* k, const void* v, const int64_t* v_stride, const int32_t* pos, const double* freq,
+                            const int32_t* counts, const int32_t* start, void* q_out, int32_t* lens_out, void* stream) {
+  if (!h || !r) return CKV_EINVAL;
+  CacheDims d;
+  int rc = resolve_cache(c, &d);
+  if (rc != CKV_OK) return rc;
+  if (r->T < 0 || r->nseq != d.nseq || r->Hq != d.Hq || r->Hk != d.Hkv || r->dh != d.dh || r->dtype != d.dtype || r->reserved != 0)
+    return CKV_EINVAL;
+  if (r->rot < 2 || r->rot % 2 || r->rot > r->dh) return CKV_EINVAL;
+  if (r->layout != CKV_ROPE_HALF && r->layout != CKV_ROPE_INTERLEAVED) return CKV_EINVAL;
+  if (!isfinite(r->factor)) return CKV_EINVAL;
+  if (r->k_out_stride[0] || r->k_out_stride[1] || r->k_out_stride[2]) return CKV_EINVAL;
+  ckv::AppendCall a;
+  if ((rc = resolve_stride(r->q_stride, d.Hq, r->T, d.dh, d.dtype, a.qs)) != CKV_OK ||
+      (rc = resolve_stride(r->k_stride, d.Hkv, r->T, d.dh, d.dtype, a.ks)) != CKV_OK ||
+      (rc = resolve_stride(v_stride, d.Hkv, r->T, d.dh, d.dtype, a.vs)) != CKV_OK ||
+      (rc = resolve_stride(r->q_out_stride, d.Hq, r->T, d.dh, d.dtype, a.qos)) != CKV_OK)
+    return rc;
+  // tokens are numbered in 32 bits, up to a whole tile of them behind the last
+  if ((long long)d.nseq * r->T > 0x7fffffffLL - 256) return CKV_ENOTSUP;
+  if (d.nseq == 0) return CKV_OK;
+  if (!start || (r->T && (!q || !k || !v || !q_out || !pos || !freq))) return CKV_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned_to(pos, 4) || !aligned_to(freq, 8) ||
+      !aligned_to(counts, 4) || !aligned_to(start, 4) || !aligned_to(lens_out, 4))
+    return CKV_EALIGN;
+  const long long heads = (long long)d.nseq * d.Hkv;
+  if (lens_out && ((lens_out != start && overlap(lens_out, heads, start, heads)) || overlap(lens_out, heads, counts, d.nseq) ||
+                   overlap(lens_out, heads, pos, (long long)d.nseq * r->T) ||
+                   overlap(lens_out, heads, (const int32_t*)freq, r->rot) ||
+                   overlap(lens_out, heads, d.page_table, heads * d.max_pages)))
+    return CKV_EINVAL;
+  a.q = q; a.k = k; a.v = v; a.T = r->T; a.rot = r->rot; a.layout = r->layout; a.factor = r->factor;
+  a.pos = pos; a.freq = freq; a.counts = counts; a.start = start; a.q_out = q_out; a.lens_out = lens_out;
+  DeviceGuard guard(h->device);
+  if (!guard.ok) return CKV_ECUDA;
+  int launches = 0;
+  const cudaError_t e = ckv::launch_append(d, a, h->sm_count, h->status_word, (cudaStream_t)stream, &launches);
+  h->launches += launches;
+  return record_cuda(h, e);
+}
+
 int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c, const int32_t* lens, int32_t n,
                           const int64_t* stride, int32_t align_right, void* K_out, void* V_out, void* stream) {
   if (!h) return CKV_EINVAL;
@@ -170,6 +212,64 @@ int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c, const 
   int launches = 0;
   const cudaError_t e = ckv::launch_cache_load(d, lens, n, ds, align_right, K_out, V_out, h->status_word,
                                                (cudaStream_t)stream, &launches);
+  h->launches += launches;
+  return record_cuda(h, e);
+}
+
+int criticalkv_summarise_pages(criticalkv_handle h, const criticalkv_cache* c, const int32_t* start, const int32_t* lens,
+                               int8_t* codes, float* scales, void* stream) {
+  if (!h) return CKV_EINVAL;
+  CacheDims d;
+  const int rc = resolve_cache(c, &d);
+  if (rc != CKV_OK) return rc;
+  if (d.nseq == 0) return CKV_OK;
+  if (!lens || !codes || !scales) return CKV_EINVAL;
+  if (!aligned16(codes) || !aligned_to(scales, 4) || !aligned_to(lens, 4) || !aligned_to(start, 4)) return CKV_EALIGN;
+  DeviceGuard guard(h->device);
+  if (!guard.ok) return CKV_ECUDA;
+  int launches = 0;
+  const cudaError_t e = ckv::launch_summarise(d, start, lens, codes, scales, h->sm_count, h->status_word, (cudaStream_t)stream, &launches);
+  h->launches += launches;
+  return record_cuda(h, e);
+}
+
+int criticalkv_select_pages(criticalkv_handle h, const criticalkv_cache* c, const void* q, const int64_t* q_stride,
+                            const int32_t* lens, const int8_t* codes, const float* scales, int32_t count, int32_t first,
+                            int32_t last, int32_t* table_out, int32_t* lens_out, int32_t* chosen, void* stream) {
+  if (!h) return CKV_EINVAL;
+  CacheDims d;
+  const int rc = resolve_cache(c, &d);
+  if (rc != CKV_OK) return rc;
+  if (count < 1 || first < 0 || last < 0 || first > count || last > count - first) return CKV_EINVAL;
+  ckv::SelectPagesCall a;
+  const int vec = d.dtype == CKV_F32 ? 4 : 8;
+  const long long dense[2] = {(long long)d.Hq * d.dh, d.dh};
+  for (int i = 0; i < 2; ++i) {
+    a.q_stride[i] = q_stride && q_stride[i] ? q_stride[i] : dense[i];
+    if (a.q_stride[i] < 0) return CKV_EINVAL;
+    if (a.q_stride[i] % vec) return CKV_EALIGN;
+  }
+  const long long heads = (long long)d.nseq * d.Hkv;
+  if (d.Hq / d.Hkv > 128 || d.max_pages > 32768 || heads > (1LL << 26)) return CKV_ENOTSUP;
+  // rows are numbered in 32 bits in the chosen table too
+  if ((long long)count << d.page_shift > 0x7fffffffLL - 256) return CKV_ENOTSUP;
+  if (d.nseq == 0) return CKV_OK;
+  if (!q || !lens || !codes || !scales || !table_out || !lens_out) return CKV_EINVAL;
+  if (!aligned16(q) || !aligned16(codes) || !aligned_to(scales, 4) || !aligned_to(lens, 4) || !aligned_to(table_out, 4) ||
+      !aligned_to(lens_out, 4) || !aligned_to(chosen, 4))
+    return CKV_EALIGN;
+  // the outputs lie apart from what is read and from each other
+  const long long in = heads * d.max_pages, out = heads * count;
+  if (overlap(table_out, out, d.page_table, in) || overlap(table_out, out, lens, heads) || overlap(lens_out, heads, lens, heads) ||
+      overlap(lens_out, heads, d.page_table, in) || overlap(table_out, out, lens_out, heads) || overlap(chosen, out, d.page_table, in) ||
+      overlap(chosen, out, lens, heads) || overlap(chosen, out, lens_out, heads) || overlap(chosen, out, table_out, out))
+    return CKV_EINVAL;
+  a.q = q; a.lens = lens; a.codes = codes; a.scales = scales; a.count = count; a.first = first; a.last = last;
+  a.table_out = table_out; a.lens_out = lens_out; a.chosen = chosen;
+  DeviceGuard guard(h->device);
+  if (!guard.ok) return CKV_ECUDA;
+  int launches = 0;
+  const cudaError_t e = ckv::launch_select_pages(d, a, h->sm_count, h->status_word, (cudaStream_t)stream, &launches);
   h->launches += launches;
   return record_cuda(h, e);
 }

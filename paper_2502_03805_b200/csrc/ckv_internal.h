@@ -152,6 +152,29 @@ struct DecodeCall {
   float* lse;
   void* ws;
 };
+struct AppendCall {
+  const void *q, *k, *v;
+  long long qs[3], ks[3], vs[3], qos[3];    // element strides: sequence, head, token
+  int T, rot, layout;
+  float factor;
+  const int32_t* pos;
+  const double* freq;
+  const int32_t* counts;
+  const int32_t* start;
+  void* q_out;
+  int32_t* lens_out;
+};
+struct SelectPagesCall {
+  const void* q;
+  long long q_stride[2];                    // elements: sequence, head
+  const int32_t* lens;
+  const int8_t* codes;
+  const float* scales;
+  int count, first, last;
+  int32_t* table_out;
+  int32_t* lens_out;
+  int32_t* chosen;
+};
 cudaError_t launch_rope(const RopeDims& d, const void* q, const void* k, const int32_t* pos, const double* freq,
                         void* q_out, void* k_out, int sm_count, cudaStream_t st, int* launches);
 cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V, int n, const long long* stride,
@@ -160,6 +183,13 @@ cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V,
                                cudaStream_t st, int* launches);
 cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right,
                               void* K_out, void* V_out, int* status_word, cudaStream_t st, int* launches);
+cudaError_t launch_append(const CacheDims& d, const AppendCall& call, int sm_count, int* status_word, cudaStream_t st,
+                          int* launches);
+cudaError_t launch_summarise(const CacheDims& d, const int32_t* start, const int32_t* lens, int8_t* codes, float* scales,
+                             int sm_count, int* status_word, cudaStream_t st, int* launches);
+size_t select_pages_smem(const CacheDims& d);      // dynamic shared memory of a CTA
+cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call, int sm_count, int* status_word,
+                                cudaStream_t st, int* launches);
 size_t decode_workspace_bytes(const CacheDims& d);
 cudaError_t launch_decode_mma(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word,
                               cudaStream_t st, int* launches);
