@@ -309,9 +309,10 @@ int criticalkv_decode(criticalkv_handle h, const criticalkv_cache* c, const void
   DeviceGuard guard(h->device);
   if (!guard.ok) return CKV_ECUDA;
   int launches = 0;
-  // tensor cores would round float32 queries; CKV_FLAG_FORCE_SIMT asks for the CUDA-core kernel
-  const bool mma = d.dtype == CKV_BF16 && !(c->flags & CKV_FLAG_FORCE_SIMT);
-  const cudaError_t e = (mma ? ckv::launch_decode_mma : ckv::launch_decode_simt)(d, call, h->device, h->sm_count, h->status_word,
+  // tensor cores would round float32 queries (on 4-bit pages they enter as two halves); CKV_FLAG_FORCE_SIMT asks for the
+  // CUDA-core kernel
+  const bool four = d.format == CKV_CACHE_E2M1, mma = (d.dtype == CKV_BF16 || four) && !(c->flags & CKV_FLAG_FORCE_SIMT);
+  const cudaError_t e = (!mma ? ckv::launch_decode_simt : four ? ckv::launch_decode_four : ckv::launch_decode_mma)(d, call, h->device, h->sm_count, h->status_word,
                                                                                  (cudaStream_t)stream, &launches);
   h->last_decode = mma ? 1 : 2;
   h->launches += launches;

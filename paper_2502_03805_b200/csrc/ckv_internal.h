@@ -193,6 +193,9 @@ cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call,
 size_t decode_workspace_bytes(const CacheDims& d);
 cudaError_t launch_decode_mma(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word,
                               cudaStream_t st, int* launches);
+// 4-bit pages, queries of either type.
+cudaError_t launch_decode_four(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word,
+                               cudaStream_t st, int* launches);
 cudaError_t launch_decode_simt(const CacheDims& d, const DecodeCall& call, int device, int sm_count, int* status_word,
                                cudaStream_t st, int* launches);
 

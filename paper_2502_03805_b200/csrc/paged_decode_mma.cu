@@ -87,38 +87,32 @@ constexpr float kTopWeight = 32768.f;
 constexpr float kLeastTop = 3.851859888774472e-34f;   // 2^-111: kTopWeight over it and it over kTopWeight are normal floats
 
 template <int FMT, int DH, int NT> struct Shape {
-  static constexpr bool kPlain = FMT == CKV_CACHE_PLAIN, kFour = FMT == CKV_CACHE_E2M1;
-  static constexpr int kRowBytes = kPlain ? DH * 2 : kFour ? DH / 2 : DH;
-  static constexpr int kGroups = kFour ? DH / 16 : 0;              // scales of groups a row
+  static constexpr bool kPlain = FMT == CKV_CACHE_PLAIN;
+  static constexpr int kRowBytes = kPlain ? DH * 2 : DH;
   // 16-row groups a warp takes at a time.  4 KB of K and of V; 8 KB for two query tiles on 128-byte rows, where the work
   // per step that does not depend on the rows weighs more (16 queries on e4m3 rows of 128: 144 -> 123 us; with one
   // query tile 86.0 and 85.3 us, int8 95 and 101 us).
   static constexpr int kSub = kRowBytes >= 256 ? 1 : kRowBytes == 128 ? 2 * NT : 4;
   static constexpr int kTile = kDecodeWarps * 16 * kSub;           // cache rows a CTA takes at a time
-  static constexpr int kChunks = kRowBytes >= 64 ? kRowBytes / 64 : 1;   // pieces of a K row per lane, 16 bytes each (or 8)
-  static constexpr int kQWords = kPlain ? 4 : kFour ? DH / 8 : 8;  // registers of query elements per piece
-  static constexpr int kVBytes = kRowBytes >= 128 ? 16 : kRowBytes / 8;  // piece of a V row per lane
+  static constexpr int kChunks = kRowBytes / 64;                   // 16-byte pieces of a K row per lane
+  static constexpr int kQWords = kPlain ? 4 : 8;                   // registers of query elements per piece
+  static constexpr int kVBytes = kRowBytes >= 128 ? 16 : 8;        // piece of a V row per lane
   static constexpr int kVPieces = kRowBytes / (8 * kVBytes);
   static constexpr int kElems = DH / 8;                            // V elements a lane has of a row
   static constexpr int kVWords = kVPieces * kVBytes / 4;           // registers they take
   static constexpr int kMTiles = kElems / 2;                       // 16-row tiles of V^T
   static constexpr int kGroupBytes = 16 * kRowBytes;               // a 16-row group of K or V in shared memory
-  static constexpr int kSpan = kRowBytes >= 128 ? 128 : kRowBytes; // bytes of a row that the swizzle keeps together
+  static constexpr int kSpan = kRowBytes >= 128 ? 128 : 64;        // bytes of a row that the swizzle keeps together
   // 16-byte chunk `chunk` of a row (half = which span of it) in a group as TMA writes it
   static __device__ __forceinline__ int at(int half, int row, int chunk) {
-    return half * 16 * kSpan + row * kSpan + ((chunk ^ (kSpan == 128 ? row & 7 : kSpan == 64 ? (row >> 1) & 3 : 0)) * 16);
-  }
-  // Cache row that row i of the matrix instruction stands for (i + 8: 8 further).  In the K read the eight lanes that are
-  // served together hold two neighbouring i and all c: their rows must differ in bit 2; in the V read they hold rows
-  // row_of(0, 2, 4, 6) or (1, 3, 5, 7): those must differ in bits 1-2.  4-bit rows of 64 bytes: neighbours must differ in
-  // bit 0 and the rows of a V read in bits 0 and 2; of 32 bytes: four neighbours, and those rows, in bits 0 and 1.
-  static __device__ __forceinline__ int row_of(int i) {
-    constexpr uint32_t order = !kFour ? 0x37156240u         // 0 4 2 6 5 1 7 3
-                               : DH == 128 ? 0x65742130u    // 0 3 1 2 4 7 5 6
-                                           : 0x67453210u;   // 0 1 2 3 5 4 7 6
-    return (order >> (4 * i)) & 7;
+    return half * 16 * kSpan + row * kSpan + ((chunk ^ (kSpan == 128 ? row & 7 : (row >> 1) & 3)) * 16);
   }
 };
+
+// Cache row that row i of the matrix instruction stands for (i + 8: 8 further).  In the K read the eight lanes that
+// are served together hold two neighbouring i and all c: their rows must differ in bit 2; in the V read they hold rows
+// row_of(0, 2, 4, 6) or (1, 3, 5, 7): those must differ in bits 1-2.
+__device__ __forceinline__ int row_of(int i) { return (0x37156240 >> (4 * i)) & 7; }   // 0 4 2 6 5 1 7 3
 
 template <int FMT, int DH, int NT> struct alignas(1024) Slots {   // of a warp
   using S = Shape<FMT, DH, NT>;
@@ -128,14 +122,9 @@ template <int FMT, int DH, int NT> struct alignas(1024) Slots {   // of a warp
 template <int FMT, int DH, int NT> struct Scales {   // of a warp; quantised pages only
   float k[Shape<FMT, DH, NT>::kSub][16], v[Shape<FMT, DH, NT>::kSub][16];
 };
-template <int FMT, int DH, int NT> struct Groups {   // of a warp; 4-bit pages only
-  static constexpr int N = Shape<FMT, DH, NT>::kFour ? DH / 16 : 1, U = N > 1 ? Shape<FMT, DH, NT>::kSub : 1;
-  alignas(16) uint8_t k[U][16][N], v[U][16][N];
-};
 template <int FMT, int DH, int NT> struct Shared {
   Slots<FMT, DH, NT> slots[kDecodeWarps];
   Scales<FMT, DH, NT> scales[kDecodeWarps];
-  Groups<FMT, DH, NT> groups[kDecodeWarps];
   float o[kDecodeWarps][4][DH];                            // four queries at a time
   float m[kDecodeWarps][16], l[kDecodeWarps][16], top[16];
   alignas(8) float parts[8 * NT][DH + 2];                  // of a CTA of a team
@@ -232,7 +221,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
     if (lane == 0 && ok) {
       const uint32_t full = is_k ? k_full : v_full;
       const uint32_t slot = ptx::smem_addr(is_k ? sh.slots[warp].k[0] : sh.slots[warp].v[0]);
-      const int count = 16 * together, bytes = count * (S::kRowBytes + S::kGroups + (is_k && !S::kPlain ? 8 : 0));
+      const int count = 16 * together, bytes = count * (S::kRowBytes + (is_k && !S::kPlain ? 8 : 0));
       int n = w.page[0] >= 0;
       if (together < SUB) {
 #pragma unroll
@@ -249,11 +238,6 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
             ptx::bulk_load(ptx::smem_addr(sh.scales[warp].k[u]), p.c.scale[0] + at, count * 4, full);
             ptx::bulk_load(ptx::smem_addr(sh.scales[warp].v[u]), p.c.scale[1] + at, count * 4, full);
           }
-          if (S::kFour) {
-            const long long at = (((long long)w.page[u] << p.c.page_shift) + in_page) * S::kGroups;
-            ptx::bulk_load(ptx::smem_addr(is_k ? sh.groups[warp].k[u] : sh.groups[warp].v[u]), p.c.group[is_k ? 0 : 1] + at,
-                           count * S::kGroups, full);
-          }
         }
       }
     }
@@ -264,7 +248,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
       *(volatile uint32_t*)&sh.late = 1;
     }
   };
-  const int k_row = S::row_of(r);
+  const int k_row = row_of(r);
   // The queries of an item as they are stored, in the element order of the K pieces.
   uint32_t q[NT][S::kChunks][S::kQWords];
   auto load_queries = [&](const Segment& g) {
@@ -383,12 +367,12 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
 #pragma unroll
       for (int u = 0; u < SUB; ++u)
 #pragma unroll
-        for (int j = 0; j < (S::kFour ? 0 : S::kChunks); ++j) {
+        for (int j = 0; j < S::kChunks; ++j) {
           const unsigned char* src = sh.slots[warp].k[u] + S::at(j / 2, k_row, c + 4 * (j % 2));
           const uint4 k0 = *reinterpret_cast<const uint4*>(src), k1 = *reinterpret_cast<const uint4*>(src + 8 * S::kSpan);
           const uint32_t a[4] = {k0.x, k0.y, k0.z, k0.w};
           const uint32_t b[4] = {k1.x, k1.y, k1.z, k1.w};
-          if constexpr (S::kPlain) {
+          if (S::kPlain) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -406,53 +390,6 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
             }
           }
         }
-      if constexpr (S::kFour) {
-        // Lane c of a quad has elements DH/4 * c ... of rows k_row and k_row + 8: one group of 16, or two.  Code times group
-        // scale is exact in a half (2 and 4 significant bits).
-#pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-          constexpr int W = DH / 32;                       // words of eight codes a lane
-          uint32_t x[2][W];
-          __half2 g[2][DH / 64];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int row = k_row + 8 * h;
-            const uint8_t* group = sh.groups[warp].k[u][row] + c * (DH / 64);
-            if constexpr (W == 4) {
-              const uint4 v = *reinterpret_cast<const uint4*>(sh.slots[warp].k[u] + S::at(0, row, c));
-              x[h][0] = v.x; x[h][1] = v.y; x[h][2] = v.z; x[h][3] = v.w;
-              const uint32_t both = e4m3x2_to_half2(*reinterpret_cast<const uint16_t*>(group));
-              const __half2 pair = *reinterpret_cast<const __half2*>(&both);
-              g[h][0] = __low2half2(pair);
-              g[h][DH / 64 - 1] = __high2half2(pair);
-            } else {
-              const uint2 v = *reinterpret_cast<const uint2*>(sh.slots[warp].k[u] + S::at(0, row, c / 2) + 8 * (c % 2));
-              x[h][0] = v.x; x[h][1] = v.y;
-              const uint32_t one = e4m3x2_to_half2(*group * 0x101u);
-              g[h][0] = *reinterpret_cast<const __half2*>(&one);
-            }
-          }
-#pragma unroll
-          for (int w = 0; w < W; ++w) {
-            uint32_t a[2][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              e2m1x8_to_half2(x[h][w], a[h]);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&a[h][i]), g[h][w / 2]);
-                a[h][i] = *reinterpret_cast<const uint32_t*>(&y);
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; i += 2)
-#pragma unroll
-              for (int n = 0; n < NT; ++n)
-                mma_f16(s[n][u], a[0][i], a[1][i], a[0][i + 1], a[1][i + 1], q[n][0][(4 * w + i) % S::kQWords],
-                        q[n][0][(4 * w + i + 1) % S::kQWords]);
-          }
-        }
-      }
       float ks[SUB][2], vs[SUB][2];
       if constexpr (!S::kPlain) {
 #pragma unroll
@@ -589,59 +526,25 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2)
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         uint32_t v[4][S::kVWords];             // of cache rows row_of(2c), row_of(2c + 1) and 8 further
-        uint32_t vg[4];                        // 4-bit pages: scales of the groups they are in
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-          const int row = S::row_of(2 * c + (h & 1)) + 8 * (h >> 1);
+          const int row = row_of(2 * c + (h & 1)) + 8 * (h >> 1);
 #pragma unroll
           for (int j = 0; j < S::kVPieces; ++j) {
             if constexpr (S::kVBytes == 16) {
               const uint4 x = *reinterpret_cast<const uint4*>(sh.slots[warp].v[u] + S::at(j, row, r));
               v[h][4 * j] = x.x; v[h][4 * j + 1] = x.y; v[h][4 * j + 2] = x.z; v[h][4 * j + 3] = x.w;
-            } else if constexpr (S::kVBytes == 8) {
+            } else {
               const uint2 x = *reinterpret_cast<const uint2*>(sh.slots[warp].v[u] + S::at(0, row, r / 2) + 8 * (r % 2));
               v[h][2 * j] = x.x; v[h][2 * j + 1] = x.y;
-            } else {
-              v[h][0] = *reinterpret_cast<const uint32_t*>(sh.slots[warp].v[u] + S::at(0, row, r / 4) + 4 * (r % 4));
             }
           }
-          if constexpr (S::kFour) vg[h] = sh.groups[warp].v[u][row][r * (DH / 64) / 2];
           if (!whole_step && row >= rows(cur, u)) {
 #pragma unroll
             for (int w = 0; w < S::kVWords; ++w) v[h][w] = 0;
-            vg[h] = 0;
           }
         }
-        if constexpr (S::kFour) {
-          // two rows' codes of an element make a byte, which becomes a pair of halves times the two rows' group scales
-          uint32_t y[2][DH / 8];                           // rows 0, 1 and 2, 3 of v: element e of the lane's piece
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const uint32_t both = e4m3x2_to_half2(vg[2 * g] | (vg[2 * g + 1] << 8));
-            const __half2 scale = *reinterpret_cast<const __half2*>(&both);
-#pragma unroll
-            for (int w = 0; w < S::kVWords; ++w) {
-              const uint32_t a = v[2 * g][w], b = v[2 * g + 1][w];
-              uint32_t even[4], odd[4];
-              e2m1x8_to_half2((a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u), even);
-              e2m1x8_to_half2(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), odd);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const __half2 e = __hmul2(*reinterpret_cast<const __half2*>(&even[i]), scale);
-                const __half2 o = __hmul2(*reinterpret_cast<const __half2*>(&odd[i]), scale);
-                y[g][8 * w + 2 * i] = *reinterpret_cast<const uint32_t*>(&e);
-                y[g][8 * w + 2 * i + 1] = *reinterpret_cast<const uint32_t*>(&o);
-              }
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < S::kMTiles; ++i)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              mma_f16(o[n][i], y[0][i], y[0][i + S::kMTiles], y[1][i], y[1][i + S::kMTiles], w_hi[n][u][0], w_hi[n][u][1]);
-              mma_f16(o[n][i], y[0][i], y[0][i + S::kMTiles], y[1][i], y[1][i + S::kMTiles], w_lo[n][u][0], w_lo[n][u][1]);
-            }
-        } else if constexpr (S::kPlain) {
+        if (S::kPlain) {
 #pragma unroll
           for (int i = 0; i < S::kMTiles; ++i) {
             const int e0 = i, e1 = i + S::kMTiles;
@@ -782,7 +685,7 @@ template <typename S> bool page_map(CUtensorMap* m, const DecodeArgs& p, int whi
   const cuuint64_t strides[3] = {(cuuint64_t)S::kRowBytes, (cuuint64_t)S::kSpan, (cuuint64_t)p.c.page_stride};
   const cuuint32_t box[4] = {(cuuint32_t)S::kSpan, (cuuint32_t)box_rows, (cuuint32_t)(S::kRowBytes / S::kSpan), 1}, ones[4] = {1, 1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, p.c.page[which], dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            S::kSpan == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : S::kSpan == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            S::kSpan == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -819,7 +722,6 @@ cudaError_t launch_decode_mma(const CacheDims& d, const DecodeCall& call, int de
   const DecodeArgs p = decode_args(d, call, d.Hq / d.Hkv <= 8 ? 8 : 16, status_word);
   if (d.format == CKV_CACHE_PLAIN) return by_shape<CKV_CACHE_PLAIN>(p, d.dh, device, sm_count, st, launches);
   if (d.format == CKV_CACHE_E4M3) return by_shape<CKV_CACHE_E4M3>(p, d.dh, device, sm_count, st, launches);
-  if (d.format == CKV_CACHE_E2M1) return by_shape<CKV_CACHE_E2M1>(p, d.dh, device, sm_count, st, launches);
   return by_shape<CKV_CACHE_INT8>(p, d.dh, device, sm_count, st, launches);
 }
 

@@ -8,6 +8,7 @@ import numpy as np
 import torch
 
 import cache_ref as R
+import decode_bounds
 from canary_util import Guarded
 from paper_2502_03805_b200 import PagedCache
 
@@ -136,3 +137,44 @@ def expect_store(cache, before, K, V, rows_of, start):
                 want[3 * j + 1].view(shapes[3 * j + 1])[page, slot] = group.view(torch.uint8)
                 want[3 * j + 2].view(torch.float32).view(shapes[3 * j + 2])[page, slot] = scale
     return want
+
+
+def attention(q, cache, lens, scale, kernel, table=None, moves=16):
+    """out, lse in 64 bits and bounds on |kernel - out| and |kernel - lse|, as decode_bounds.decode has them; kernel "tensor" or
+    "cuda" (whose bounds are those of 8-bit pages).
+
+    Tensor cores: the products of codes and group scales are exact; a query element is one half (bf16: exact but for 2^-39 of the
+    row's largest) or the sum of two (float32: half a step of the second, 2^-24 of the element, besides); a weight is the sum of
+    two halves (2^-22) and loses 2^-36 of the largest product of a weight and a row scale at the least, times code and group
+    scale.  `moves`: how often the references move, each time 2^-22 of exp2."""
+    D, G = decode_bounds, q.shape[1] // cache.Hkv
+    K, V = cache.values()
+    table = cache.table if table is None else table
+    if kernel == "cuda":
+        return D.decode(q, K, V, table, lens, cache.page, scale, "e2m1", cache.dtype, kernel, cache.vs, moves)
+    out = torch.zeros(q.shape, dtype=torch.float64)
+    lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float64)
+    tol, tol_lse = torch.zeros_like(out), torch.zeros_like(lse)
+    vs_all = cache.vs.cpu().double()[..., None]
+    for s in range(q.shape[0]):
+        for g in range(cache.Hkv):
+            n = int(lens[s, g])
+            if n == 0:
+                continue
+            k, v, vs = (R.head_rows(x, table[s, g], n, cache.page) for x in (K, V, vs_all))
+            qs, hs = q[s, g * G:(g + 1) * G].double().cpu(), slice(g * G, (g + 1) * G)
+            logit = qs @ k.T * scale
+            w = torch.softmax(logit, -1)
+            out[s, hs], lse[s, hs] = w @ v, torch.logsumexp(logit, -1)
+            size = abs(scale) * (qs.abs() @ k.abs().T)
+            d = (cache.dh + 8 + (1 if cache.dtype == "f32" else 0)) * D.STEP * size + 4 * D.STEP * logit.abs() + moves * 2.0 ** -22
+            d = d + D.STEP * logit.abs().amax(-1, keepdim=True)
+            d = d + abs(scale) * (2.0 ** -39 * qs.abs().amax(-1, keepdim=True) + 2.0 ** -125) * k.abs().sum(-1)
+            adds = (n / 4 + 64) * D.STEP
+            for h in range(G):
+                far = (v - out[s, g * G + h]).abs()
+                tol[s, g * G + h] = (w[h] * d[h]) @ far * 1.02 + (2.0 ** -22 + adds) * (w[h] @ v.abs())
+            tol[s, hs] += adds * out[s, hs].abs() + out[s, hs].abs() * R.HALF_STEP[cache.dtype] + 1e-37
+            tol[s, hs] += 2.0 ** -36 * (w * vs[:, 0]).amax(-1)[:, None] * (v.abs() / vs).sum(0)
+            tol_lse[s, hs] = (w * d).sum(-1) * 1.02 + adds + (lse[s, hs].abs() + 1.0) * D.STEP
+    return out, lse, tol, tol_lse

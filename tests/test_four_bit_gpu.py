@@ -13,7 +13,6 @@ from paper_2502_03805_b200 import binding as B
 from test_cache_gpu import LENS, gen, same
 
 pytestmark = pytest.mark.gpu
-MOVES = 16        # running maxima of a warp over a few thousand rows in random order: about ln n, and the joins
 
 
 # ---- rows in and out -------------------------------------------------------------------------------------------------
@@ -120,10 +119,9 @@ def test_store_outside_the_table_or_the_pool_is_skipped_and_reported():
 def check(cache, q, lens, c=None, kernel=None, scale=None, given=None):
     c = cache.c if c is None else c
     got = c.attend(q.cuda(), (lens if given is None else given).cuda())
-    kernel = kernel or ("tensor" if cache.dtype == "bf16" else "cuda")
+    kernel = kernel or "tensor"
     assert B.criticalkv_last_path(c.handle) & 384 == (128 if kernel == "tensor" else 256)
-    want = D.decode(q, *cache.values(), cache.table, lens, cache.page, 1.0 / math.sqrt(cache.dh) if scale is None else scale,
-                    "e2m1", cache.dtype, kernel, cache.vs, MOVES)
+    want = F.attention(q, cache, lens, 1.0 / math.sqrt(cache.dh) if scale is None else scale, kernel)
     D.check(got, want, lens, q.shape[1] // cache.Hkv)
     return got
 
@@ -186,13 +184,35 @@ def test_values_of_very_different_size(dtype):
     check(cache, (3 * torch.randn(1, 4, 64, generator=gen(8))).to(R.DT[dtype]), lens)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("size", [2.0 ** 40, 2.0 ** -40, 0.0])
-def test_large_and_tiny_queries(dh, size):
+def test_large_and_tiny_queries(dtype, dh, size):
     lens = torch.full((1, 1), 40, dtype=torch.int32)
     scale = 1.0 / (8 * size) if size else 1.0
-    cache = F.FourBit(nseq=1, Hq=2, Hkv=1, dh=dh, dtype="bf16", page=16, cols=3, scale=scale).fill(lens, 3)
-    check(cache, (size * torch.randn(1, 2, dh, generator=gen(8))).bfloat16(), lens, scale=scale)
+    cache = F.FourBit(nseq=1, Hq=2, Hkv=1, dh=dh, dtype=dtype, page=16, cols=3, scale=scale).fill(lens, 3)
+    check(cache, (size * torch.randn(1, 2, dh, generator=gen(8))).to(R.DT[dtype]), lens, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("order", ["rising", "falling", "one late"])
+def test_logits_that_keep_growing(dtype, order):
+    """References that move: logits that rise by a little, by a lot, and a lone large one behind many small ones; a head
+    whose first rows score -infinity and below any reference."""
+    n, dh = 900, 64
+    lens = torch.full((1, 2), n, dtype=torch.int32)
+    cache = F.FourBit(nseq=1, Hq=4, Hkv=2, dh=dh, dtype=dtype, page=32, cols=29, scale=1.0).fill(lens, 3)
+    g = gen(4)
+    size = {"rising": torch.linspace(-60, 60, n), "falling": torch.linspace(60, -60, n),
+            "one late": torch.where(torch.arange(n) == 871, 90.0, 0.01)}[order]
+    for h in range(2):
+        k = torch.randn(n, dh, generator=g) * 0.02
+        k[:, 0] = size / (1 + h)
+        v = torch.randn(n, dh, generator=g) * torch.exp(4 * torch.randn(n, 1, generator=g))
+        cache.put(0, h, torch.arange(n), (k.to(R.DT[dtype]), v.to(R.DT[dtype])))
+    q = 0.1 * torch.randn(1, 4, dh, generator=g)
+    q[:, :, 0] = torch.tensor([1.0, -1.0, 0.3, 2.0])
+    check(cache, q.to(R.DT[dtype]), lens, scale=1.0)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -204,8 +224,7 @@ def test_absent_pages_wild_lengths_and_empty_heads(dtype):
     assert cache.c.device_status() == B.CKV_EBOUNDS
     cache.table_dev[0, 0, 2], cache.table_dev[0, 1, 2], cache.table_dev[0, 2] = -1, cache.k.shape[0], -7
     got = cache.c.attend(q.cuda(), lens.cuda())
-    want = D.decode(q, *cache.values(), cache.table, torch.tensor([[32, 32, 0]]), 16, 0.125, "e2m1", dtype,
-                    "tensor" if dtype == "bf16" else "cuda", cache.vs, MOVES)
+    want = F.attention(q, cache, torch.tensor([[32, 32, 0]]), 0.125, "tensor")
     assert bool(((got[0].cpu().double() - want[0]).abs() <= want[2])[0, :4].all())
     assert bool(torch.isnan(got[0][0, 4:]).all())                             # rows, but none in an existing page
     assert cache.c.device_status() == B.CKV_EBOUNDS and cache.intact()
@@ -235,7 +254,7 @@ def test_strided_queries_own_page_stride_and_shared_pages():
     cache.table_dev.copy_(cache.table)
     both = torch.randn(2, 12, 64, generator=gen(8)).bfloat16()
     got = cache.c.attend(both.cuda()[:, 2:10], lens.cuda())
-    want = D.decode(both[:, 2:10], *cache.values(), cache.table, lens, 16, 0.31, "e2m1", "bf16", "tensor", cache.vs, MOVES)
+    want = F.attention(both[:, 2:10], cache, lens, 0.31, "tensor")
     D.check(got, want, lens, 4)
 
 

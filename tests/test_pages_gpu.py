@@ -108,8 +108,12 @@ def check_attention(cache, q, want, lens, got, rows, c=None):
     table = torch.zeros((nseq, Hkv, cols), dtype=torch.int32)
     for (s, g), pages in want.items():
         table[s, g, :len(pages)] = cache.table[s, g][torch.tensor(pages, dtype=torch.long)]
-    exact = D.decode(q, *cache.values(), table, rows.cpu(), cache.page, 1.0 / math.sqrt(cache.dh), cache.fmt, cache.dtype,
-                     "tensor" if cache.dtype == "bf16" else "cuda", cache.vs, MOVES)
+    scale = 1.0 / math.sqrt(cache.dh)
+    if cache.fmt == "e2m1":
+        exact = F.attention(q, cache, rows.cpu(), scale, "tensor", table)
+    else:
+        exact = D.decode(q, *cache.values(), table, rows.cpu(), cache.page, scale, cache.fmt, cache.dtype,
+                         "tensor" if cache.dtype == "bf16" else "cuda", cache.vs, MOVES)
     D.check(got, exact, rows.cpu(), q.shape[1] // Hkv)
 
 
