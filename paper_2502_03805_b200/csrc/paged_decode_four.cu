@@ -14,11 +14,15 @@
 //              weights (times the row scales) relative to a largest one that is moved only when one is 16 times above it: sums
 //              are rescaled a few times a head instead of in most steps.  A weight enters the second product as two halves
 //              (22 bits, no finer than 2^-36 of the largest such product).  Float pairs go through the packed instructions.
-//   copies     a warp has a ring of steps of 32 rows, filled by TMA: codes, group scales and row scales of K and of V, each
-//              copy issued by a lane of its own, one barrier a step.
+//   queries    up to four of a KV head leave half of the matrix instruction's columns free: they hold the second halves of the
+//              weights, and the lanes of those columns work on the other of two tiles.
+//   copies     a warp has a ring of steps of 32 rows, filled by asynchronous copies of 16 bytes a lane: a step is ten of them.
+//              (Bulk copies take their operands from uniform registers, which made each of six to nine a step some fifteen
+//              instructions.)
+#include <stddef.h>
+
 #include "paged_decode.cuh"
 #include "sm100_ptx.cuh"
-#include "tma_host.h"
 
 namespace ckv {
 namespace {
@@ -54,48 +58,42 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-__device__ __forceinline__ float2 negative(float2 x) { return make_float2(-x.x, -x.y); }
 
 constexpr float kTop = 2048.f;         // where the largest product of a weight and a row scale is put ...
 constexpr float kMost = 32768.f;       // ... and what a later one may reach before it is moved
 constexpr float kAhead = 10.f;         // log2 of what a weight may reach before the maximum is moved
 constexpr float kLeastTop = 3.851859888774472e-34f;   // 2^-111: kTop over it and it over kTop are normal floats
-
 // In place of minus the reference where no logit has been seen: any logit is far above it, and -infinity has weight 0.
 constexpr float kNoReference = 3.4028234e38f;
 
-constexpr int kRows = 32, kTiles = kRows / 16;   // rows of a step, in tiles of the matrix instruction
+constexpr int kWarpRows = 32, kTiles = kWarpRows / 16;          // rows of a step of a warp, in tiles of the matrix instruction
+constexpr int kRows = kDecodeWarps * kWarpRows;                 // rows of a step of all warps
 
 template <int DH> struct Row {
   static constexpr int kBytes = DH / 2, kGroups = DH / 16, kWords = DH / 32;   // of codes; scales; words of codes a quad lane has
-  // 16-byte piece `chunk` of a row as TMA writes it (64-byte rows: 64-byte swizzle, 32-byte rows: none)
-  static __device__ __forceinline__ int at(int row, int chunk) {
-    return row * kBytes + ((DH == 128 ? chunk ^ ((row >> 1) & 3) : chunk) * 16);
-  }
-  // Cache row of a tile that row i of the matrix instruction stands for (i + 8: 8 further), so that neither read has bank
-  // conflicts.  64 bytes: neighbours differ in bit 0, rows 0, 2, 4, 6 (and 1, 3, 5, 7) in bits 0 and 2; 32 bytes: four
-  // neighbours, and those rows, in bits 0 and 1.
-  static __device__ __forceinline__ int of(int i) {
-    constexpr uint32_t order = DH == 128 ? 0x65742130u    // 0 3 1 2 4 7 5 6
-                                         : 0x67453210u;   // 0 1 2 3 5 4 7 6
-    return (order >> (4 * i)) & 7;
-  }
+  // V lies in chunks of eight rows that are 32 bytes apart, so that the rows of the four lanes c below are on different banks.
+  static constexpr int kChunk = 8 * kBytes + 32;
 };
 
-template <int DH> struct alignas(1024) Step {      // the rows of a step in shared memory
-  unsigned char k[kRows * Row<DH>::kBytes], v[kRows * Row<DH>::kBytes];
-  uint8_t kg[kRows][Row<DH>::kGroups], vg[kRows][Row<DH>::kGroups];
-  float ks[kRows], vs[kRows];
-  int here[2];                                     // rows that exist in either half (a page may end between them)
+// Row i of tile u of a warp is row 8 * (i / 2 % 4) + 4u + 2 * (i / 8) + i % 2: of the lanes (r, c), c has rows 2c, 2c + 1, 2c + 8 and
+// 2c + 9 of V^T P^T in one chunk, and neighbouring rows of K Q^T are neighbours in memory.
+__device__ __forceinline__ int row_of(int u, int i) { return 8 * (i >> 1 & 3) + 4 * u + 2 * (i >> 3) + (i & 1); }
+
+template <int DH> struct alignas(16) Step {        // the rows of a step of a warp in shared memory
+  unsigned char k[kWarpRows * Row<DH>::kBytes], v[4 * Row<DH>::kChunk];
+  uint8_t kg[kWarpRows][Row<DH>::kGroups], vg[kWarpRows][Row<DH>::kGroups];
+  float ks[kWarpRows], vs[kWarpRows];
 };
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
 
 template <int DH, int NT, int RING> struct Shared {
   Step<DH> ring[kDecodeWarps][RING];
   float o[kDecodeWarps][4][DH];                    // four queries at a time
   float m[kDecodeWarps][8 * NT], l[kDecodeWarps][8 * NT], top[8 * NT];
   alignas(8) float parts[8 * NT][DH + 2];          // of a CTA of a team
-  uint64_t full[kDecodeWarps][RING];
-  uint32_t late;                                   // a copy did not arrive in time: the other waits give up too
 };
 
 // A CTA's part of an item: tiles [t0, t1) of it, a tile being a step of every warp.
@@ -104,29 +102,21 @@ struct Segment {
   int first;                                       // the item's first tile in the list of all tiles
 };
 
-template <typename T, int DH, int NT, int RING, int CTAS>
-__global__ void __launch_bounds__(kDecodeThreads, CTAS)
-    decode_four_kernel(const __grid_constant__ DecodeArgs p, const __grid_constant__ CUtensorMap k_map,
-                       const __grid_constant__ CUtensorMap v_map) {
+// QUAD: no KV head has more than four queries (NT is 1).
+template <typename T, int DH, int NT, bool QUAD, int RING, int CTAS>
+__global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const __grid_constant__ DecodeArgs p) {
   using R = Row<DH>;
-  constexpr int kTile = kDecodeWarps * kRows;
   constexpr int kParts = sizeof(T) == 4 ? 2 : 1;   // halves a query element is the sum of
   constexpr int kQ = DH / 8;                       // registers of a query's elements
   constexpr int kM = DH / 16;                      // 16-row tiles of V^T
-  extern __shared__ unsigned char smem_raw[];
-  Shared<DH, NT, RING>& sh = *reinterpret_cast<Shared<DH, NT, RING>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  constexpr int kUnits = QUAD ? 1 : kTiles;        // tiles whose weights a lane works on
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  Shared<DH, NT, RING>& sh = *reinterpret_cast<Shared<DH, NT, RING>*>(smem_raw);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, r = lane >> 2, c = lane & 3;
-  if (threadIdx.x < kDecodeWarps * RING) ptx::mbar_init(ptx::smem_addr(&sh.full[0][0] + threadIdx.x), 1);
-  if (threadIdx.x == 0) {
-    sh.late = 0;
-    ptx::prefetch_tensormap(&k_map);
-    ptx::prefetch_tensormap(&v_map);
-  }
-  ptx::fence_barrier_init();
+  const int cc = QUAD ? c & 1 : c;                 // the lane's pair of query columns
   wait_for_previous_kernel();
-  const Walk walk = p.team ? team_walk<T, DH, kTile>(p) : plan<T, DH, kTile>(p);
+  const Walk walk = p.team ? team_walk<T, DH, kRows>(p) : plan<T, DH, kRows>(p);
   if (threadIdx.x < 8 * NT) *reinterpret_cast<float2*>(&sh.parts[threadIdx.x][DH]) = make_float2(-INFINITY, 0.f);
-  __syncthreads();                                 // the mbarriers are visible
 
   // The segment behind `g` (its item, first and tiles), or one with t0 == t1.
   auto following = [&](Segment g) {
@@ -137,74 +127,89 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
       if (g.first >= walk.end) return g;
       g.kv = kv_of(p, g.item);
       g.len = item_len(p, g.kv);
-      g.tiles = (g.len + kTile - 1) / kTile;
+      g.tiles = (g.len + kRows - 1) / kRows;
       g.t0 = max(walk.begin - g.first, 0);
       g.t1 = min(g.tiles, walk.end - g.first);
       if (g.t1 > g.t0) return g;
     }
   };
-
-  // ---- copies.  Lane 8h + kind of a warp fetches one of the six arrays, of all rows of a step (h = 0) or, where a page has
-  // 16 rows, of its half h.
-  const bool halved = p.c.page_shift == 4;
-  const int kind = lane & 7, half = lane >> 3 & 1;
-  const bool copies = kind < 6 && lane < (halved ? 16 : 8);
-  const int count = halved ? 16 : 32;              // rows of a copy
-  Segment front;                                   // what is looked up next
-  int front_left, front_base;                      // steps of `front` left, first row of the next one
-  int page = -1, here = 0, in_page = 0;            // of this lane's copy in the step that is fetched next
+  // ---- copies.  A step is two halves of 16 rows, each of one page.
+  Segment front;                                   // the step that is looked up next: front_left of this segment are left
+  int front_left, front_row;
+  int page[2], here = 0, in_page = 0;              // of the step that is fetched next: its pages, rows, first row in its page
+  uint32_t present = 0;                            // four bits a step of the ring: whether rows 8i ... 8i + 7 are there
+  const uint32_t ring = ptx::smem_addr(&sh.ring[warp][0]);
+  auto enter = [&]() {
+    front_left = front.t1 - front.t0;
+    front_row = (front.t0 * kDecodeWarps + warp) * kWarpRows;
+  };
   auto look_up = [&]() {
-    here = 0;
-    page = -1;
     if (front_left == 0) {
       if (front.t0 < front.t1) front = following(front);
-      front_left = front.t1 - front.t0;
-      front_base = (front.t0 * kDecodeWarps + warp) * kRows;
+      enter();
     }
-    if (front_left > 0) {
-      const int base = front_base + (halved ? 16 * half : 0);
-      here = max(0, min(front.len - base, count));
-      in_page = base & ((1 << p.c.page_shift) - 1);
-      if (here > 0) page = p.c.table[(long long)front.kv * p.c.max_pages + (base >> p.c.page_shift)];
-      front_left -= 1;
-      front_base += kTile;
-    }
+    here = front_left > 0 ? front.len - front_row : 0;
+    in_page = front_row & ((1 << p.c.page_shift) - 1);
+    const int32_t* pages = p.c.table + (long long)front.kv * p.c.max_pages + (front_row >> p.c.page_shift);
+    if (here > 0) page[0] = pages[0];
+    page[1] = page[0];
+    if (p.c.page_shift == 4 && here > 16) page[1] = pages[1];
+    front_left -= front_left > 0;
+    front_row += kRows;
   };
+  // scales are copied by lanes 0 to 15 (those of K) and 16 to 31 (of V)
+  const int w = lane >> 4, l = lane & 15;
   auto fetch = [&](int stage) {
-    Step<DH>& to = sh.ring[warp][stage];
-    if (here > 0 && (unsigned)page >= (unsigned)p.c.num_pages) {
-      if (p.status != nullptr && copies) atomicExch(p.status, (int)CKV_EBOUNDS);
-      here = 0;
-    }
-    const uint32_t full = ptx::smem_addr(&sh.full[warp][stage]);
-    const bool go = here > 0;
-    const int n = go + (halved ? (int)__shfl_xor_sync(0xffffffffu, (int)go, 8) : 0);
-    __syncwarp();                                  // every lane has read what the slot held
-    if (kind == 0 && lane < 16) {
-      if (halved) to.here[half] = here;
-      else to.here[half] = max(0, min(here - 16 * half, 16));
-    }
-    if (lane == 0) ptx::mbar_arrive_expect_tx(full, n * count * 2 * (R::kBytes + R::kGroups + 4));
-    __syncwarp();
-    if (copies && go) {
-      const int row = halved ? 16 * half : 0;
-      if (kind < 2) {
-        ptx::tma_load_4d(ptx::smem_addr(kind == 0 ? to.k : to.v) + row * R::kBytes, kind == 0 ? &k_map : &v_map, 0, in_page, 0, page, full);
-      } else {
-        const long long slot = ((long long)page << p.c.page_shift) + in_page;
-        const int w = kind & 1;
-        if (kind < 4)
-          ptx::bulk_load(ptx::smem_addr(w ? to.vg[row] : to.kg[row]), p.c.group[w] + slot * R::kGroups, count * R::kGroups, full);
-        else
-          ptx::bulk_load(ptx::smem_addr(w ? to.vs + row : to.ks + row), p.c.scale[w] + slot, count * 4, full);
+    using S = Step<DH>;
+    constexpr int kCopy = 512 / R::kBytes;         // rows that the lanes copy at once: 8 or 16
+    const uint32_t to = ring + stage * (uint32_t)sizeof(S), to_codes = to + lane * 16;
+    const uint32_t to_v = DH == 128 ? to_codes : to + lane / 16 * R::kChunk + lane % 16 * 16;
+    const uint32_t to_groups = to + l * 16 + (w ? offsetof(S, vg) : offsetof(S, kg));
+    const uint32_t to_scales = to + (l & 7) * 16 + (w ? offsetof(S, vs) : offsetof(S, ks));
+    const bool groups = DH == 128 || l < 8, scales = DH == 128 ? l < 8 : l >= 8;
+    present &= ~(15u << (4 * stage));
+    __syncwarp();                                  // every lane has read what the step held
+    if (here >= kWarpRows && p.c.page_shift > 4 && (unsigned)page[0] < (unsigned)p.c.num_pages) {
+      present |= 15u << (4 * stage);
+      const long long at = page[0] * p.c.page_stride + in_page * R::kBytes + lane * 16;
+      const long long slot = ((long long)page[0] << p.c.page_shift) + in_page;
+      const char *k = p.c.page[0] + at, *v = p.c.page[1] + at;
+#pragma unroll
+      for (int i = 0; i < kWarpRows / kCopy; ++i) {
+        copy16(to_codes + offsetof(S, k) + 512 * i, k + 512 * i);
+        copy16(to_v + offsetof(S, v) + kCopy / 8 * R::kChunk * i, v + 512 * i);
+      }
+      if (groups) copy16(to_groups, p.c.group[w] + slot * R::kGroups + l * 16);
+      if (scales) copy16(to_scales, p.c.scale[w] + slot + (l & 7) * 4);
+    } else {                                       // the same by halves of 16 rows, which are of a page each and may be absent
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        if (here <= 16 * h) break;
+        const int of = h ? page[1] : page[0];
+        if ((unsigned)of >= (unsigned)p.c.num_pages) {
+          if (p.status != nullptr && lane == 0) atomicExch(p.status, (int)CKV_EBOUNDS);
+          continue;
+        }
+        present |= (here > 16 * h + 8 ? 3u : 1u) << (4 * stage + 2 * h);
+        const int first = in_page + (p.c.page_shift == 4 ? 0 : 16 * h);
+        const long long at = of * p.c.page_stride + first * R::kBytes + lane * 16;
+        const long long slot = ((long long)of << p.c.page_shift) + first - 16 * h;
+#pragma unroll
+        for (int i = 0; i < 16 / kCopy; ++i) {
+          copy16(to_codes + offsetof(S, k) + 16 * h * R::kBytes + 512 * i, p.c.page[0] + at + 512 * i);
+          copy16(to_v + offsetof(S, v) + 2 * h * R::kChunk + kCopy / 8 * R::kChunk * i, p.c.page[1] + at + 512 * i);
+        }
+        // the lanes of this half's rows
+        if (groups && (DH == 128 ? l >> 3 : l >> 2) == h) copy16(to_groups, p.c.group[w] + slot * R::kGroups + l * 16);
+        if (scales && (l >> 2 & 1) == h) copy16(to_scales, p.c.scale[w] + slot + (l & 7) * 4);
       }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
-  const int k_row = R::of(r);
   // The queries of an item, in the element order of the K pieces: lane c of a quad has elements DH/4 * c ...
   uint32_t q[NT][kParts][kQ];
-  float2 to_log2[NT];                              // factor of the products for query columns 2c, 2c + 1
+  float2 to_log2[NT];                              // factor of the products for query columns 2cc, 2cc + 1
   auto load_queries = [&](const Segment& g) {
     const ItemRows it = item_rows(p, g.kv, g.item - g.kv * p.chunks);
 #pragma unroll
@@ -249,13 +254,19 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
       }
       float up[2];
 #pragma unroll
-      for (int x2 = 0; x2 < 2; ++x2)
-        up[x2] = p.scale_log2 * __int_as_float((127 + __shfl_sync(0xffffffffu, e, 8 * c + 4 * x2)) << 23);   // of query 8n + 2c + x2
+      for (int y = 0; y < 2; ++y)
+        up[y] = p.scale_log2 * __int_as_float((127 + __shfl_sync(0xffffffffu, e, 8 * cc + 4 * y)) << 23);   // of query 8n + 2cc + y
       to_log2[n] = make_float2(up[0], up[1]);
     }
   };
+  // Largest over the lanes that have the same query columns.
+  auto top_of_columns = [&](float x) {
+    if (QUAD) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+    return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+  };
 
-  bool ok = true;                                  // no wait of this lane has run out
   int2 join = make_int2(-1, 0);
   Segment seg;
   seg.item = walk.item - 1;
@@ -265,10 +276,8 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
   seg.t0 = seg.t1 = 0;
   if (walk.begin < walk.end) seg = following(seg);
   front = seg;
-  front_left = seg.t1 - seg.t0;
-  front_base = (seg.t0 * kDecodeWarps + warp) * kRows;
+  enter();
   int stage = 0;
-  uint32_t phase = 0;
   if (seg.t0 < seg.t1) {
     look_up();
     for (int i = 0; i < RING; ++i) {
@@ -276,10 +285,10 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
       look_up();
     }
   }
-  while (seg.t0 < seg.t1 && ok) {
+  while (seg.t0 < seg.t1) {
     const ItemRows it = item_rows(p, seg.kv, seg.item - seg.kv * p.chunks);
     load_queries(seg);
-    float o[NT][kM][4];                            // [tile of V^T][even, odd element; query columns 2c, 2c + 1]
+    float o[NT][kM][4];                            // [tile of V^T][even, odd element; columns 2c, 2c + 1]
     float2 m[NT], l[NT], big[NT], inv[NT];         // reference of the logits, sums, largest product, kTop over it
     float2 less[NT];                               // minus the reference
 #pragma unroll
@@ -295,14 +304,28 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
 
     for (int tile = seg.t0; tile < seg.t1; ++tile) {
       const Step<DH>& step = sh.ring[warp][stage];
-      if (!ptx::mbar_wait_bounded(ptx::smem_addr(&sh.full[warp][stage]), phase, &sh.late)) {
-        ok = false;
-        *(volatile uint32_t*)&sh.late = 1;
+      asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+      __syncwarp();
+      const int rows = seg.len - (tile * kDecodeWarps + warp) * kWarpRows;      // that exist, where their pages do
+      const uint32_t chunks = present >> (4 * stage) & 15u;
+      const bool whole_step = rows >= kWarpRows && chunks == 15u;
+      const auto absent = [&](int row) { return row >= rows || !(chunks >> (row >> 3) & 1u); };
+      if (!whole_step && chunks) {
+        // what is left in the places of absent rows may be no number
+        if (absent(lane)) {
+          Step<DH>& own = sh.ring[warp][stage];
+#pragma unroll 1
+          for (int i = 0; i < R::kBytes / 16; ++i) {
+            *reinterpret_cast<uint4*>(own.k + lane * R::kBytes + 16 * i) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(own.v + (lane >> 3) * R::kChunk + (lane & 7) * R::kBytes + 16 * i) = make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll 1
+          for (int i = 0; i < R::kGroups; ++i) own.kg[lane][i] = own.vg[lane][i] = 0;
+          own.ks[lane] = own.vs[lane] = 0.f;
+        }
+        __syncwarp();
       }
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-      const int rows0 = step.here[0], rows1 = step.here[1];
-      const bool whole_step = rows0 + rows1 == kRows;
-      if (rows0 + rows1 > 0) {
+      if (chunks) {
         // ---- logits
         float s[NT][kTiles][4];
 #pragma unroll
@@ -315,16 +338,16 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
           __half2 g[2][DH / 64];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int row = 16 * u + 8 * h + k_row;
+            const int row = row_of(u, r) + 2 * h;
             const uint8_t* group = step.kg[row] + c * (DH / 64);
             if constexpr (DH == 128) {
-              const uint4 v = *reinterpret_cast<const uint4*>(step.k + R::at(row, c));
+              const uint4 v = *reinterpret_cast<const uint4*>(step.k + row * R::kBytes + 16 * c);
               x[h][0] = v.x; x[h][1] = v.y; x[h][R::kWords - 2] = v.z; x[h][R::kWords - 1] = v.w;
               const __half2 pair = halves(e4m3x2_to_half2(*reinterpret_cast<const uint16_t*>(group)));
               g[h][0] = __low2half2(pair);
               g[h][DH / 64 - 1] = __high2half2(pair);
             } else {
-              const uint2 v = *reinterpret_cast<const uint2*>(step.k + R::at(row, c / 2) + 8 * (c % 2));
+              const uint2 v = *reinterpret_cast<const uint2*>(step.k + row * R::kBytes + 8 * c);
               x[h][0] = v.x; x[h][1] = v.y;
               g[h][0] = halves(e4m3x2_to_half2(*group * 0x101u));
             }
@@ -347,59 +370,61 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
                   mma_f16(s[n][u], a[0][i], a[1][i], a[0][i + 1], a[1][i + 1], q[n][part][4 * w + i], q[n][part][4 * w + i + 1]);
           }
         }
-        // ---- weights.  Pair h of a tile: row k_row + 8h, query columns 2c and 2c + 1
-        float2 z[NT][kTiles][2];
-        float vs[kTiles][2];
+        // ---- weights.  Pair h of unit u: row `row` of the warp's, query columns 2cc and 2cc + 1
+        float2 z[NT][kUnits][2];
+        float vs[kUnits][2];
 #pragma unroll
-        for (int u = 0; u < kTiles; ++u)
+        for (int u = 0; u < kUnits; ++u)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int row = 16 * u + 8 * h + k_row;
+            const int row = row_of(QUAD ? c >> 1 : u, r) + 2 * h;
             const float ks = step.ks[row];
             vs[u][h] = step.vs[row];
-            // the two scales first: a product of codes and normalised queries times a large row scale alone would overflow
-            // where tiny queries make up for it
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-              z[n][u][h] = mul2(make_float2(s[n][u][2 * h], s[n][u][2 * h + 1]), mul2(both(ks), to_log2[n]));
+            for (int n = 0; n < NT; ++n) {
+              float2 x = make_float2(s[n][u][2 * h], s[n][u][2 * h + 1]);
+              if (QUAD) {                          // the upper lanes take the second tile
+                const float a = __shfl_xor_sync(0xffffffffu, s[n][kTiles - 1][2 * h], 2);
+                const float b = __shfl_xor_sync(0xffffffffu, s[n][kTiles - 1][2 * h + 1], 2);
+                if (c >= 2) x = make_float2(a, b);
+              }
+              // the two scales first: a product of codes and normalised queries times a large row scale alone would overflow
+              // where tiny queries make up for it
+              z[n][u][h] = mul2(x, mul2(both(ks), to_log2[n]));
+            }
           }
         if (!whole_step) {
+#pragma unroll 1
+          for (int i = 0; i < 1; ++i) {            // a branch: as selections it was a tenth of a step
 #pragma unroll
-          for (int u = 0; u < kTiles; ++u)
+            for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (8 * h + k_row >= (u ? rows1 : rows0)) {
-                vs[u][h] = 1.f;
+              for (int h = 0; h < 2; ++h)
+                if (absent(row_of(QUAD ? c >> 1 : u, r) + 2 * h)) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) z[n][u][h] = both(-INFINITY);
-              }
+                  for (int n = 0; n < NT; ++n) z[n][u][h] = both(-INFINITY);
+                }
+          }
         }
-        float2 w[NT][kTiles][2];                   // weights, then times the value's scale
+        float2 wt[NT][kUnits][2];                  // weights, then times the value's scale
         float2 sum[NT];
         bool far = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float ahead = 0.f, most = 0.f;
+          sum[n] = both(0.f);
 #pragma unroll
-          for (int u = 0; u < kTiles; ++u)
+          for (int u = 0; u < kUnits; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const float2 d = add2(z[n][u][h], less[n]);
               ahead = fmaxf(ahead, fmaxf(d.x, d.y));
-              const float2 e = make_float2(ptx::ex2_approx(d.x), ptx::ex2_approx(d.y));
-              w[n][u][h] = e;
+              wt[n][u][h] = make_float2(ptx::ex2_approx(d.x), ptx::ex2_approx(d.y));
+              sum[n] = add2(sum[n], wt[n][u][h]);
+              wt[n][u][h] = mul2(mul2(wt[n][u][h], both(vs[u][h])), inv[n]);
+              most = fmaxf(most, fmaxf(wt[n][u][h].x, wt[n][u][h].y));
             }
-          far = far || ahead > kAhead;
-          sum[n] = both(0.f);
-#pragma unroll
-          for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              sum[n] = add2(sum[n], w[n][u][h]);
-              w[n][u][h] = mul2(mul2(w[n][u][h], both(vs[u][h])), inv[n]);
-              most = fmaxf(most, fmaxf(w[n][u][h].x, w[n][u][h].y));
-            }
-          far = far || most > kMost;
+          far = far || ahead > kAhead || most > kMost;
         }
         if (__any_sync(0xffffffffu, far)) {
           // ---- the references move: sums so far are rescaled, the weights of this step taken again
@@ -407,15 +432,13 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
           for (int n = 0; n < NT; ++n) {
             float top[2] = {m[n].x, m[n].y}, most[2];
 #pragma unroll
-            for (int u = 0; u < kTiles; ++u)
+            for (int u = 0; u < kUnits; ++u)
 #pragma unroll
               for (int h = 0; h < 2; ++h) { top[0] = fmaxf(top[0], z[n][u][h].x); top[1] = fmaxf(top[1], z[n][u][h].y); }
             float f[2], old[2] = {m[n].x, m[n].y}, was[2] = {big[n].x, big[n].y};
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 4));
-              top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 8));
-              top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], 16));
+              top[x] = top_of_columns(top[x]);
               f[x] = old[x] == top[x] ? 1.f : ptx::ex2_approx(old[x] - top[x]);   // equal infinities included
               most[x] = was[x] * f[x];
             }
@@ -424,30 +447,27 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
             l[n] = mul2(l[n], make_float2(f[0], f[1]));
             sum[n] = both(0.f);
 #pragma unroll
-            for (int u = 0; u < kTiles; ++u)
+            for (int u = 0; u < kUnits; ++u)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 const float2 d = add2(z[n][u][h], less[n]);
-                w[n][u][h] = make_float2(ptx::ex2_approx(d.x), ptx::ex2_approx(d.y));
-                sum[n] = add2(sum[n], w[n][u][h]);
-                w[n][u][h] = mul2(w[n][u][h], both(vs[u][h]));
-                most[0] = fmaxf(most[0], w[n][u][h].x);
-                most[1] = fmaxf(most[1], w[n][u][h].y);
+                wt[n][u][h] = make_float2(ptx::ex2_approx(d.x), ptx::ex2_approx(d.y));
+                sum[n] = add2(sum[n], wt[n][u][h]);
+                wt[n][u][h] = mul2(wt[n][u][h], both(vs[u][h]));
+                most[0] = fmaxf(most[0], wt[n][u][h].x);
+                most[1] = fmaxf(most[1], wt[n][u][h].y);
               }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 4));
-              most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 8));
-              most[x] = fmaxf(most[x], __shfl_xor_sync(0xffffffffu, most[x], 16));
-              most[x] = fmaxf(most[x], kLeastTop);
+              most[x] = fmaxf(top_of_columns(most[x]), kLeastTop);
               f[x] *= was[x] * __frcp_rn(most[x]);
             }
             big[n] = make_float2(most[0], most[1]);
             inv[n] = make_float2(kTop * __frcp_rn(most[0]), kTop * __frcp_rn(most[1]));
 #pragma unroll
-            for (int u = 0; u < kTiles; ++u)
+            for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-              for (int h = 0; h < 2; ++h) w[n][u][h] = mul2(w[n][u][h], inv[n]);
+              for (int h = 0; h < 2; ++h) wt[n][u][h] = mul2(wt[n][u][h], inv[n]);
 #pragma unroll
             for (int i = 0; i < kM; ++i) {
               o[n][i][0] *= f[0]; o[n][i][1] *= f[1];
@@ -455,18 +475,28 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
             }
           }
         }
-        uint32_t w_hi[NT][kTiles][2], w_lo[NT][kTiles][2];
+        // P^T: first and second halves of the weights, of a tile in one matrix (QUAD) or in two
+        constexpr int kB = QUAD ? 1 : 2;
+        uint32_t weight[NT][kTiles][kB][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           l[n] = add2(l[n], sum[n]);
 #pragma unroll
-          for (int u = 0; u < kTiles; ++u)
+          for (int u = 0; u < kUnits; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const __half2 hi = __floats2half2_rn(w[n][u][h].x, w[n][u][h].y);
-              const float2 rest = add2(w[n][u][h], negative(__half22float2(hi)));
-              w_hi[n][u][h] = transpose8(bits(hi));
-              w_lo[n][u][h] = transpose8(bits(__floats2half2_rn(rest.x, rest.y)));
+              const __half2 hi = __floats2half2_rn(wt[n][u][h].x, wt[n][u][h].y);
+              const float2 back = __half22float2(hi);
+              const uint32_t first = bits(hi), second = bits(__floats2half2_rn(wt[n][u][h].x - back.x, wt[n][u][h].y - back.y));
+              if (QUAD) {
+                // lower lanes have the first tile and give its second halves, upper lanes the second tile and its first ones
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, c < 2 ? second : first, 2);
+                weight[n][0][0][h] = transpose8(c < 2 ? first : got);
+                weight[n][kTiles - 1][0][h] = transpose8(c < 2 ? got : second);
+              } else {
+                weight[n][u][0][h] = transpose8(first);
+                weight[n][u][kB - 1][h] = transpose8(second);
+              }
             }
         }
         // ---- O^T += V^T P^T.  Lane r has elements DH/8 * r ... of four rows; elements 2i and 2i + 1 are its rows of tile i
@@ -475,19 +505,16 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
           uint32_t x[4][DH / 64], g[4];
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
-            const int in_tile = R::of(2 * c + (h & 1)) + 8 * (h >> 1), row = 16 * u + in_tile;
+            const int in_chunk = 4 * u + 2 * (h >> 1) + (h & 1), row = 8 * c + in_chunk;
+            const unsigned char* at = step.v + c * R::kChunk + in_chunk * R::kBytes + r * (R::kBytes / 8);
             if constexpr (DH == 128) {
-              const uint2 v = *reinterpret_cast<const uint2*>(step.v + R::at(row, r / 2) + 8 * (r % 2));
+              const uint2 v = *reinterpret_cast<const uint2*>(at);
               x[h][0] = v.x;
               x[h][DH / 64 - 1] = v.y;
             } else {
-              x[h][0] = *reinterpret_cast<const uint32_t*>(step.v + R::at(row, r / 4) + 4 * (r % 4));
+              x[h][0] = *reinterpret_cast<const uint32_t*>(at);
             }
             g[h] = step.vg[row][r * (DH / 64) / 2];
-            if (!whole_step && in_tile >= (u ? rows1 : rows0)) {       // what is left there may be no number
-              x[h][0] = x[h][DH / 64 - 1] = 0;
-              g[h] = 0;
-            }
           }
           __half2 scale[2];
 #pragma unroll
@@ -509,23 +536,22 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                mma_f16(o[n][4 * y + i], even[0][i], odd[0][i], even[1][i], odd[1][i], w_hi[n][u][0], w_hi[n][u][1]);
-                mma_f16(o[n][4 * y + i], even[0][i], odd[0][i], even[1][i], odd[1][i], w_lo[n][u][0], w_lo[n][u][1]);
-              }
+              for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int b = 0; b < kB; ++b)
+                  mma_f16(o[n][4 * y + i], even[0][i], odd[0][i], even[1][i], odd[1][i], weight[n][u][b][0], weight[n][u][b][1]);
           }
         }
       }
       fetch(stage);
       look_up();
-      if (++stage == RING) { stage = 0; phase ^= 1; }
+      if (++stage == RING) stage = 0;
     }
     // ---- the warps meet in shared memory: references first, then the sums rescaled to the largest, four queries at a time
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      if (r == 0) *reinterpret_cast<float2*>(&sh.m[warp][8 * n + 2 * c]) = m[n];
-    ok = !__syncthreads_or(!ok);                   // also: everything of the previous item has been read
-    if (!ok) break;
+      if (r == 0 && c == cc) *reinterpret_cast<float2*>(&sh.m[warp][8 * n + 2 * cc]) = m[n];
+    __syncthreads();                               // also: everything of the previous item has been read
     float2 factor[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -533,16 +559,17 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
       float fs[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int row = 8 * n + 2 * c + x;
+        const int row = 8 * n + 2 * cc + x;
         float top = sh.m[0][row];
 #pragma unroll
         for (int w = 1; w < kDecodeWarps; ++w) top = fmaxf(top, sh.m[w][row]);
         const float f = own[x] == -INFINITY ? 0.f : ptx::ex2_approx(own[x] - top);
         float sum = sums[x];
+        if (QUAD) sum += __shfl_xor_sync(0xffffffffu, sum, 2);
         sum += __shfl_xor_sync(0xffffffffu, sum, 4);
         sum += __shfl_xor_sync(0xffffffffu, sum, 8);
         sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-        if (r == 0) {
+        if (r == 0 && c == cc) {
           sh.l[warp][row] = sum * f;
           if (warp == 0) sh.top[row] = top;
         }
@@ -550,9 +577,15 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
       }
       factor[n] = make_float2(fs[0], fs[1]);
     }
+    if (QUAD) {                                    // what the second halves of the weights came to
+#pragma unroll
+      for (int i = 0; i < kM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[0][i][e] += __shfl_xor_sync(0xffffffffu, o[0][i][e], 2);
+    }
     const bool whole = seg.t0 == 0 && seg.t1 == seg.tiles;
 #pragma unroll
-    for (int g = 0; g < 2 * NT; ++g) {
+    for (int g = 0; g < (QUAD ? 1 : 2 * NT); ++g) {
       if (4 * g < it.rows) {
         if (g > 0) __syncthreads();
         if (c / 2 == g % 2) {
@@ -594,56 +627,36 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS)
     if (seg.t0 > 0 && seg.t1 == seg.tiles) join = make_int2(seg.item, cta_of(walk, seg.first));
     seg = following(seg);
   }
-  if (!ok) {
-    // a copy did not arrive in time: report it, and give what is still on its way a last chance before the CTA (and with
-    // it the shared memory the copies write) goes away
-    if (threadIdx.x == 0) atomicExch(p.timeout, (int)CKV_ETIMEOUT);
-    volatile uint32_t zero = 0;
-    for (int i = 0; i < RING; ++i)
-      for (int x = 0; x < 2; ++x) ptx::mbar_wait_bounded(ptx::smem_addr(&sh.full[warp][i]), phase ^ x, &zero, 100000000ull);
-  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   if (p.team) join_team<T, DH>(p, walk, &sh.parts[0][0]);
   else if (threadIdx.x == 0) p.join[blockIdx.x] = join;
 }
 
-// Pages as TMA sees them: bytes of a row x rows of a page x 1 x pages.
-template <int DH> bool page_map(CUtensorMap* m, const DecodeArgs& p, int which) {
-  EncodeTiledFn fn = tma_encode_fn();
-  if (!fn) return false;
-  using R = Row<DH>;
-  const int box_rows = p.c.page_shift == 4 ? 16 : kRows;
-  const cuuint64_t dims[4] = {(cuuint64_t)R::kBytes, (cuuint64_t)1 << p.c.page_shift, 1, (cuuint64_t)p.c.num_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)R::kBytes, (cuuint64_t)p.c.page_stride, (cuuint64_t)p.c.page_stride};
-  const cuuint32_t box[4] = {(cuuint32_t)R::kBytes, (cuuint32_t)box_rows, 1, 1}, ones[4] = {1, 1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, p.c.page[which], dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            DH == 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-template <typename T, int DH, int NT> cudaError_t launch(DecodeArgs p, int device, int sm_count, cudaStream_t st, int* launches) {
+template <typename T, int DH, int NT, bool QUAD> cudaError_t launch(DecodeArgs p, int device, int sm_count, cudaStream_t st, int* launches) {
   constexpr int RING = 3, CTAS = NT == 1 ? 3 : 2;
-  const auto kernel = decode_four_kernel<T, DH, NT, RING, CTAS>;
-  constexpr int smem = (int)sizeof(Shared<DH, NT, RING>) + 1024;   // the steps start on a multiple of 1024
-  constexpr int tile = kDecodeWarps * kRows;
+  const auto kernel = decode_four_kernel<T, DH, NT, QUAD, RING, CTAS>;
+  constexpr int smem = (int)sizeof(Shared<DH, NT, RING>);
   static LaunchSetup setup;
   const LaunchSetup::Fit* fit = setup.of(kernel, device, smem);
   if (!fit) return cudaErrorInvalidDeviceFunction;
-  CUtensorMap maps[2];
-  for (int i = 0; i < 2; ++i)
-    if (!page_map<DH>(&maps[i], p, i)) return cudaErrorInvalidValue;
-  p.team = decode_team(p, *fit, sm_count, tile);
-  const int grid = p.team ? p.items * p.team : decode_grid(p, fit->per_sm * sm_count, tile);
+  p.team = decode_team(p, *fit, sm_count, kRows);
+  const int grid = p.team ? p.items * p.team : decode_grid(p, fit->per_sm * sm_count, kRows);
   *launches += 1;
-  const cudaError_t e = launch_early_in_clusters<DecodeArgs, CUtensorMap, CUtensorMap>(kernel, dim3(grid), kDecodeThreads, smem,
-                                                                                       p.team, st, p, maps[0], maps[1]);
+  const cudaError_t e = launch_early_in_clusters<DecodeArgs>(kernel, dim3(grid), kDecodeThreads, smem, p.team, st, p);
   if (e != cudaSuccess || p.team) return e;
   *launches += 1;
   return launch_decode_join<T, DH>(p, grid, st);
 }
 
+template <typename T, int DH> cudaError_t by_queries(const DecodeArgs& p, int device, int sm_count, cudaStream_t st, int* launches) {
+  if (p.part_rows <= 4) return launch<T, DH, 1, true>(p, device, sm_count, st, launches);
+  if constexpr (sizeof(T) == 2) {
+    if (p.chunk_rows == 16) return launch<T, DH, 2, false>(p, device, sm_count, st, launches);
+  }
+  return launch<T, DH, 1, false>(p, device, sm_count, st, launches);
+}
 template <typename T> cudaError_t by_shape(const DecodeArgs& p, int dh, int device, int sm_count, cudaStream_t st, int* launches) {
-  if (p.chunk_rows == 8) return dh == 64 ? launch<T, 64, 1>(p, device, sm_count, st, launches) : launch<T, 128, 1>(p, device, sm_count, st, launches);
-  return dh == 64 ? launch<T, 64, 2>(p, device, sm_count, st, launches) : launch<T, 128, 2>(p, device, sm_count, st, launches);
+  return dh == 64 ? by_queries<T, 64>(p, device, sm_count, st, launches) : by_queries<T, 128>(p, device, sm_count, st, launches);
 }
 
 }  // namespace
@@ -652,8 +665,7 @@ cudaError_t launch_decode_four(const CacheDims& d, const DecodeCall& call, int d
                                int* launches) {
   // queries of a KV head: 8 or 16 an item, as paged_decode_mma.cu (float32 queries, of two halves, have registers for 8)
   const DecodeArgs p = decode_args(d, call, d.Hq / d.Hkv <= 8 || d.dtype == CKV_F32 ? 8 : 16, status_word);
-  return d.dtype == CKV_F32 ? (d.dh == 64 ? launch<float, 64, 1>(p, device, sm_count, st, launches)
-                                          : launch<float, 128, 1>(p, device, sm_count, st, launches))
+  return d.dtype == CKV_F32 ? by_shape<float>(p, d.dh, device, sm_count, st, launches)
                             : by_shape<__nv_bfloat16>(p, d.dh, device, sm_count, st, launches);
 }
 
