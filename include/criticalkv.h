@@ -387,8 +387,10 @@ CKV_API int criticalkv_cache_append(criticalkv_handle h, const criticalkv_cache*
 /*
  * Rows out of the cache.  K_out, V_out [nseq, Hkv, n, dh] (strides as above).  With align_right == 0 row i of head
  * (s, g) goes to row i for i < min(lens[s,g], n); with align_right == 1 the last min(lens, n) rows end at row n-1,
- * the layout that criticalkv_desc.valid_from = n - lens describes.  Other rows of the outputs keep their contents.
+ * the layout that criticalkv_desc.valid_from = n - lens describes.  Other rows of the outputs keep their contents, or are
+ * zeroed with CKV_LOAD_CLEAR added to align_right.
  */
+#define CKV_LOAD_CLEAR (1 << 8)
 CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c, const int32_t* lens, int32_t n,
                                   const int64_t* stride, int32_t align_right, void* K_out, void* V_out, void* stream);
 

@@ -27,6 +27,7 @@ CKV_FLAG_REQUIRE_TENSOR_CORES = 128
 CKV_EBOUNDS = -7
 CKV_CACHE_PLAIN, CKV_CACHE_E4M3, CKV_CACHE_INT8, CKV_CACHE_E2M1 = 0, 1, 2, 3
 CKV_ROPE_HALF, CKV_ROPE_INTERLEAVED = 0, 1
+CKV_LOAD_CLEAR = 1 << 8
 CKV_SELFTEST_MAX_WAIT_NS = 100_000_000
 CKV_STATIC_SCRATCH_BYTES = (8 << 20) + (64 << 10)
 

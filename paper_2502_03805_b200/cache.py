@@ -537,16 +537,18 @@ class PagedCache(_Owner):
         """Rows 0..min(lens, n)-1 of every head as K_out, V_out [nseq, Hkv, n, dh] (zeros where there is no row, when
         allocated here; left as they were in a caller's tensor).  align_right puts the last rows of a head at the end,
         as the compression step's valid_from = n - lens wants it."""
+        clear = 0
         if K_out is None or V_out is None:
             if n is None or K_out is not None or V_out is not None:
                 raise ValueError("give n, or both K_out and V_out")
             with self._allocating(stream):
-                K_out = torch.zeros((self.nseq, self.Hkv, n, self.dh), dtype=self.torch_dtype, device=self.device)
-                V_out = torch.zeros_like(K_out)
+                K_out = torch.empty((self.nseq, self.Hkv, n, self.dh), dtype=self.torch_dtype, device=self.device)
+                V_out = torch.empty_like(K_out)
+            clear = B.CKV_LOAD_CLEAR
         key = (n, lens.dtype, lens.shape, lens.stride(), lens.get_device(), K_out.dtype, K_out.shape, K_out.stride(),
                K_out.get_device(), V_out.dtype, V_out.shape, V_out.stride(), V_out.get_device())
         n, strides = self._plans.get(key) or self._keep(key, self._describe_load(lens, n, K_out, V_out))
-        rc = self._load(self.handle, self._ref, lens.data_ptr(), n, strides, 1 if align_right else 0, K_out.data_ptr(),
+        rc = self._load(self.handle, self._ref, lens.data_ptr(), n, strides, (1 if align_right else 0) + clear, K_out.data_ptr(),
                         V_out.data_ptr(), self._where(stream))
         if rc:
             self._fail(rc, "criticalkv_cache_load")

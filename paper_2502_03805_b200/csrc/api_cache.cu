@@ -201,6 +201,8 @@ int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c, const 
   CacheDims d;
   int rc = resolve_cache(c, &d);
   if (rc != CKV_OK) return rc;
+  const int clear = align_right & CKV_LOAD_CLEAR;
+  align_right &= ~CKV_LOAD_CLEAR;
   if (n < 0 || (align_right != 0 && align_right != 1)) return CKV_EINVAL;
   long long ds[3];
   if ((rc = resolve_stride(stride, d.Hkv, n, d.dh, d.dtype, ds)) != CKV_OK) return rc;
@@ -210,7 +212,7 @@ int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c, const 
   DeviceGuard guard(h->device);
   if (!guard.ok) return CKV_ECUDA;
   int launches = 0;
-  const cudaError_t e = ckv::launch_cache_load(d, lens, n, ds, align_right, K_out, V_out, h->status_word,
+  const cudaError_t e = ckv::launch_cache_load(d, lens, n, ds, align_right, clear, K_out, V_out, h->status_word,
                                                (cudaStream_t)stream, &launches);
   h->launches += launches;
   return record_cuda(h, e);

@@ -181,7 +181,7 @@ cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V,
                                const int32_t* idx, const int32_t* offsets, long long idx_rows, const int32_t* counts,
                                const int32_t* start, int32_t* lens_out, int sm_count, int* status_word,
                                cudaStream_t st, int* launches);
-cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right,
+cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right, int clear,
                               void* K_out, void* V_out, int* status_word, cudaStream_t st, int* launches);
 cudaError_t launch_append(const CacheDims& d, const AppendCall& call, int sm_count, int* status_word, cudaStream_t st,
                           int* launches);

@@ -633,7 +633,7 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
 }
 
 template <typename T, int DH, int NT, bool QUAD> cudaError_t launch(DecodeArgs p, int device, int sm_count, cudaStream_t st, int* launches) {
-  constexpr int RING = 3, CTAS = NT == 1 ? 3 : 2;
+  constexpr int RING = NT == 1 ? 2 : 3, CTAS = NT == 1 ? 3 : 2;
   const auto kernel = decode_four_kernel<T, DH, NT, QUAD, RING, CTAS>;
   constexpr int smem = (int)sizeof(Shared<DH, NT, RING>);
   static LaunchSetup setup;

@@ -220,6 +220,7 @@ struct LoadArgs {
   long long ds[3];             // destination byte strides: sequence, head, row
   int n;
   int align_right;
+  int clear;                   // rows of the destination that get none are zeroed
   int chunks;
   int* status;
 };
@@ -239,19 +240,30 @@ __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
   const int at = p.align_right ? p.n - rows : 0;         // and where it goes
   const int32_t* pages = p.c.table + (long long)item * p.c.max_pages;
   const int step = RPP * kRows;
-  for (long long base = (long long)chunk * step; base < rows; base += (long long)p.chunks * step) {
+  const int before = p.clear ? at : 0;                   // rows of the destination in front of the first, where they are cleared
+  const int last = p.clear ? p.n - at : rows;            // row behind the last, counted from the first
+  for (long long base = (long long)chunk * step - before; base < last; base += (long long)p.chunks * step) {
     long long slot[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const long long r = base + u * RPP + sub;
       slot[u] = -1;
-      if (r < rows) {
+      if (r >= 0 && r < rows) {
         const int row = from + (int)r;
         const int page = pages[row >> p.c.page_shift];
         if (page >= 0 && page < p.c.num_pages)
           slot[u] = ((long long)page << p.c.page_shift) + (row & ((1 << p.c.page_shift) - 1));
         bad = bad || slot[u] < 0;
       }
+    }
+    if (p.clear) {
+#pragma unroll
+      for (int u = 0; u < kRows; ++u)
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          if (slot[u] < 0 && base + u * RPP + sub < last)
+            *reinterpret_cast<uint4*>(p.dst[w] + s * p.ds[0] + g * p.ds[1] + (at + base + u * RPP + sub) * p.ds[2] + lane * 16) =
+                make_uint4(0, 0, 0, 0);
     }
     if constexpr (FMT == CKV_CACHE_PLAIN) {
       uint4 raw[kRows][2];
@@ -382,7 +394,7 @@ cudaError_t launch_cache_store(const CacheDims& d, const void* K, const void* V,
   return launch_early<StoreArgs, int>(store_lengths_kernel, dim3((unsigned)((items + 127) / 128)), 128, 0, st, p, (int)items);
 }
 
-cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right,
+cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, const long long* stride, int align_right, int clear,
                               void* K_out, void* V_out, int* status_word, cudaStream_t st, int* launches) {
   const int es = d.dtype == CKV_F32 ? 4 : 2;
   const long long items = (long long)d.nseq * d.Hkv;
@@ -391,7 +403,7 @@ cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, co
   p.lens = lens;
   p.dst[0] = (char*)K_out; p.dst[1] = (char*)V_out;
   for (int i = 0; i < 3; ++i) p.ds[i] = stride[i] * es;
-  p.n = n; p.align_right = align_right;
+  p.n = n; p.align_right = align_right; p.clear = clear != 0;
   p.status = d.debug_checks ? status_word : nullptr;
   const int step = kThreads / (d.dh * es / 16) * kRows;
   p.chunks = chunks_for(n, step, items);

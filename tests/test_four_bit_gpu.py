@@ -297,3 +297,31 @@ def test_allocated_pool_and_refusals():
         B.criticalkv_decode_workspace_bytes(B.make_cache(nseq=1, Hq=1, Hkv=1, dh=128, dtype="bf16", format="e2m1", page_size=16,
                                                          num_pages=1, max_pages=1, k_pages=256, v_pages=256, page_table=256,
                                                          k_scale=256, v_scale=256, k_group_scale=256, v_group_scale=264))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("right", [False, True])
+@pytest.mark.parametrize("n", [1, 37, 200])
+def test_load_into_new_tensors_zeroes_what_has_no_row(dtype, right, n):
+    """Rows in front of and behind a head's, and those of pages outside the pool; a caller's tensors keep theirs."""
+    lens = torch.tensor([[100, 0, 3], [37, 200, 64]], dtype=torch.int32)
+    cache = F.FourBit(nseq=2, Hq=3, Hkv=3, dh=64, dtype=dtype, page=16, cols=13).fill(lens, 3)
+    for fmt in ("e2m1", "plain"):
+        if fmt == "plain":
+            c = PagedCache.allocate(nseq=2, Hq=3, Hkv=3, dh=64, dtype=dtype, rows=200, page_size=16)
+            rows = cache.c.load(lens.cuda(), 200)
+            c.store(*rows, c.new_lengths())
+        else:
+            c = cache.c
+        c.page_table[1, 2, 3] = -1                     # rows 48 to 63
+        junk = torch.full((1 << 22,), 7.0, device="cuda")
+        del junk                                       # what new tensors are made of
+        given = [torch.full((2, 3, n, 64), 5.0, dtype=R.DT[dtype], device="cuda") for _ in range(2)]
+        c.load(lens.cuda(), K_out=given[0], V_out=given[1], align_right=right)
+        for new, old in zip(c.load(lens.cuda(), n, align_right=right), given):
+            at = torch.arange(n).expand(2, 3, n) - ((n - lens.clamp(max=n))[..., None] if right else 0)
+            row = at + ((lens - lens.clamp(max=n))[..., None] if right else 0)
+            there = (at >= 0) & (at < lens.clamp(max=n)[..., None])
+            there[1, 2] &= ~((row[1, 2] >= 48) & (row[1, 2] < 64))
+            assert bool((new.cpu()[~there] == 0).all()) and bool((old.cpu()[~there] == 5.0).all())
+            assert torch.equal(new.cpu()[there], old.cpu()[there])

@@ -78,3 +78,10 @@ def test_select():
     assert select(cache(max_pages=32769)) == select(cache(Hq=258)) == select(count=2 ** 26) == B.CKV_ENOTSUP
     assert select(cache(nseq=2 ** 25 + 1, Hq=2)) == B.CKV_ENOTSUP
     assert select(cache(nseq=0), q=None, lens=None, codes=None, scales=None, table=None, rows=None) == B.CKV_OK
+
+
+def test_load_flags():
+    load = lambda right: B.load().criticalkv_cache_load(HANDLE, C.byref(cache()), None, 4, None, right, 256, 256, None)  # noqa: E731
+    assert B.CKV_LOAD_CLEAR == 256
+    for right in (2, 3, 255, 258, 512, -1):
+        assert load(right) == B.CKV_EINVAL
