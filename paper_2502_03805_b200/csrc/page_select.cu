@@ -63,23 +63,69 @@ template <typename T, int FMT> __device__ __forceinline__ void eight_of(const Pa
   }
 }
 
-// Largest and smallest of the rows `sub`, `sub` + step, ... of a page, four in flight.
+// Maximum and minimum that are NaN where either is one: a page with an infinity or a NaN is then seen by its extremes alone.
+__device__ __forceinline__ float nan_max(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float nan_min(float a, float b) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
+// Largest and smallest of the rows `sub`, `sub` + step, ... of a page, several in flight (the last row again behind the end).
 template <typename T, int FMT>
 __device__ __forceinline__ void reduce_rows(const Pages& c, long long page, int rows, int dh, int e, int sub, int step, float (&hi)[8],
-                                            float (&lo)[8], uint32_t& top) {
-  constexpr int FLY = 4;
-  for (int r = sub; r < rows; r += FLY * step) {
-    float x[FLY][8];
+                                            float (&lo)[8]) {
+  if constexpr (FMT == CKV_CACHE_PLAIN && sizeof(T) == 2) {
+    // two elements an instruction, as they are stored
+    constexpr int FLY = 8;
+    const char* base = c.page[0] + page * c.page_stride + e * 2;
+    __nv_bfloat162 up[4], down[4];
 #pragma unroll
-    for (int i = 0; i < FLY; ++i) eight_of<T, FMT>(c, page, min(r + i * step, rows - 1), dh, e, x[i]);   // the last row again
+    for (int j = 0; j < 4; ++j) {
+      up[j] = __floats2bfloat162_rn(-INFINITY, -INFINITY);
+      down[j] = __floats2bfloat162_rn(INFINITY, INFINITY);
+    }
+    for (int r = sub; r < rows; r += FLY * step) {
+      uint4 raw[FLY];
 #pragma unroll
-    for (int i = 0; i < FLY; ++i)
+      for (int i = 0; i < FLY; ++i) raw[i] = *reinterpret_cast<const uint4*>(base + min(r + i * step, rows - 1) * dh * 2);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        hi[j] = fmaxf(hi[j], x[i][j]);
-        lo[j] = fminf(lo[j], x[i][j]);
-        top = max(top, __float_as_uint(x[i][j]) & 0x7fffffffu);   // the order of the bits puts NaN above infinity
+      for (int i = 0; i < FLY; ++i) {
+        const uint32_t x[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const __nv_bfloat162 y = *reinterpret_cast<const __nv_bfloat162*>(&x[j]);
+          up[j] = __hmax2_nan(up[j], y);
+          down[j] = __hmin2_nan(down[j], y);
+        }
       }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 a = __bfloat1622float2(up[j]), b = __bfloat1622float2(down[j]);
+      hi[2 * j] = a.x; hi[2 * j + 1] = a.y;
+      lo[2 * j] = b.x; lo[2 * j + 1] = b.y;
+    }
+  } else {
+    constexpr int FLY = 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { hi[j] = -INFINITY; lo[j] = INFINITY; }
+    for (int r = sub; r < rows; r += FLY * step) {
+      float x[FLY][8];
+#pragma unroll
+      for (int i = 0; i < FLY; ++i) eight_of<T, FMT>(c, page, min(r + i * step, rows - 1), dh, e, x[i]);
+#pragma unroll
+      for (int i = 0; i < FLY; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          hi[j] = nan_max(hi[j], x[i][j]);
+          lo[j] = nan_min(lo[j], x[i][j]);
+        }
+    }
   }
 }
 
@@ -89,7 +135,6 @@ template <typename T, int FMT, int DH, int WARPS> __global__ void __launch_bound
   constexpr int LANES = DH / 8, ROWS = 32 / LANES;        // lanes a row, rows a warp takes at a time
   constexpr int TEAMS = 4 / WARPS;                        // pages a CTA works on
   __shared__ float part[2][4][DH];
-  __shared__ uint32_t tops[4];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int item = blockIdx.x / p.workers, worker = blockIdx.x % p.workers * TEAMS + warp / WARPS;
   const int given = p.lens[item];
@@ -113,38 +158,36 @@ template <typename T, int FMT, int DH, int WARPS> __global__ void __launch_bound
     }
     const int rows = (int)min(len - (n << p.c.page_shift), (long long)size);
     float hi[8], lo[8];
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) { hi[j] = -INFINITY; lo[j] = INFINITY; }
-    reduce_rows<T, FMT>(p.c, page, rows, DH, e, warp % WARPS * ROWS + lane / LANES, WARPS * ROWS, hi, lo, top);
+    reduce_rows<T, FMT>(p.c, page, rows, DH, e, warp % WARPS * ROWS + lane / LANES, WARPS * ROWS, hi, lo);
 #pragma unroll
     for (int o = LANES; o < 32; o <<= 1)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        hi[j] = fmaxf(hi[j], __shfl_xor_sync(0xffffffffu, hi[j], o));
-        lo[j] = fminf(lo[j], __shfl_xor_sync(0xffffffffu, lo[j], o));
+        hi[j] = nan_max(hi[j], __shfl_xor_sync(0xffffffffu, hi[j], o));
+        lo[j] = nan_min(lo[j], __shfl_xor_sync(0xffffffffu, lo[j], o));
       }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     if (WARPS > 1) {
       __syncthreads();                                    // the page before has been joined
       if (lane < LANES) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) { part[0][warp][e + j] = hi[j]; part[1][warp][e + j] = lo[j]; }
       }
-      if (lane == 0) tops[warp] = top;
       __syncthreads();
       if (warp > 0) continue;
 #pragma unroll
       for (int w = 1; w < 4; ++w) {
-        top = max(top, tops[w]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          hi[j] = fmaxf(hi[j], part[0][w][e + j]);
-          lo[j] = fminf(lo[j], part[1][w][e + j]);
+          hi[j] = nan_max(hi[j], part[0][w][e + j]);
+          lo[j] = nan_min(lo[j], part[1][w][e + j]);
         }
       }
     }
+    uint32_t top = 0;                                     // the order of the bits puts NaN above infinity
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, max(__float_as_uint(hi[j]) & 0x7fffffffu, __float_as_uint(lo[j]) & 0x7fffffffu));
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     const bool finite = top < 0x7f800000u;
     float scale = __fdiv_rn(__uint_as_float(top), 127.f);
     if (scale < kLeastScale) scale = kLeastScale;
