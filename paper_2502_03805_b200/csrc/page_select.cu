@@ -8,8 +8,8 @@
 //
 // summarise reads every key once and is bound by HBM.  select reads 2 dh + 4 bytes a page: a (sequence, KV head) is a
 // cluster's of 1 to 16 CTAs whose warps score 16 pages at a time (pages on the 16-row side of mma.sync, 8 queries on the
-// other) and leave the scores in the shared memory of the cluster's first CTA, which looks for the smallest chosen one by
-// bisection and writes the chosen pages in order: one launch, and the table that it writes is one that decode reads.
+// other) and leave the scores in the shared memory of the cluster's first CTA, which looks for the smallest chosen one in a
+// histogram and writes the chosen pages in order: one launch, and the table that it writes is one that decode reads.
 #include "launch_early.cuh"
 #include "paged_codes.cuh"
 
@@ -210,7 +210,8 @@ template <typename T, int FMT, int DH, int WARPS> __global__ void __launch_bound
 }
 
 // ---- choice ----------------------------------------------------------------------------------------------------------
-constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
+constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
+constexpr int kBins = 1024, kShort = 1024;       // of the histogram of keys; pages that share the last bin and are ranked one by one
 constexpr uint32_t kForced = 0xffffffffu;        // key of a page that is always chosen
 
 struct SelectArgs {
@@ -242,197 +243,277 @@ __device__ __forceinline__ uint32_t key_of(float score) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
-// Sum over the CTA; `turn` alternates between calls, so that one barrier is enough.
-__device__ __forceinline__ uint32_t sum_of_cta(uint32_t x, uint32_t (&sums)[2][kSelectWarps], int turn) {
-  x = __reduce_add_sync(0xffffffffu, x);
-  if (threadIdx.x % 32 == 0) sums[turn][threadIdx.x / 32] = x;
-  __syncthreads();
-  uint32_t total = 0;
+// Sum over the threads in front of this one; `total`: over all of them.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t (&sums)[kSelectWarps], uint32_t& total) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  uint32_t incl = x;
 #pragma unroll
-  for (int w = 0; w < kSelectWarps; ++w) total += sums[turn][w];
-  return total;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  __syncthreads();                               // the sums of the call before have been read
+  if (lane == 31) sums[warp] = incl;
+  __syncthreads();
+  total = 0;
+  uint32_t before = incl - x;
+#pragma unroll
+  for (int w = 0; w < kSelectWarps; ++w) {
+    if (w < warp) before += sums[w];
+    total += sums[w];
+  }
+  return before;
 }
 
-template <typename T, int DH> __global__ void __launch_bounds__(kSelectThreads) select_pages_kernel(SelectArgs p) {
+// What the first CTA of a cluster looks for the smallest chosen key with.
+struct Search {
+  uint32_t bins[kBins];
+  uint32_t keys[kShort];                         // of the pages in the last bin
+  uint32_t sums[kSelectWarps], low, high, bin, above, listed, least, ties;
+};
+
+// The smallest chosen key of n and how many of the pages that have it are chosen: `count` in all, n > count.  Every thread
+// gets them.  Keys are spread over bins by their distance from the smallest, the bin that holds the border is listed, and
+// every listed page counts those above it; a bin that is too full (equal scores) is halved until it is not.
+__device__ __forceinline__ void find_least(const uint32_t* keys, int n, uint32_t count, Search& f) {
+  uint32_t low = kForced, high = 0, forced = 0;
+  for (int j = threadIdx.x; j < n; j += kSelectThreads) {
+    const uint32_t k = keys[j];
+    if (k == kForced) { forced += 1; continue; }
+    low = min(low, k);
+    high = max(high, k);
+  }
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
+  forced = __reduce_add_sync(0xffffffffu, forced);
+  if (threadIdx.x % 32 == 0) {                   // set up before the scores
+    atomicMin(&f.low, low);
+    atomicMax(&f.high, high);
+    atomicAdd(&f.above, forced);
+  }
+  __syncthreads();
+  low = f.low;
+  high = f.high;
+  uint32_t above = f.above;                      // keys above `high`
+  if (above >= count) {                          // (equal: the forced ones are all)
+    if (threadIdx.x == 0) { f.least = kForced; f.ties = count; }
+    __syncthreads();
+    return;
+  }
+  while (true) {
+    // the border is among the keys of low ... high, `above` keys are above them
+    const int shift = max(0, 32 - __clz(high - low) - 10);
+    for (int b = threadIdx.x; b < kBins; b += kSelectThreads) f.bins[b] = 0;
+    if (threadIdx.x == 0) f.listed = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < n; j += kSelectThreads) {
+      const uint32_t k = keys[j];
+      if (k >= low && k <= high) atomicAdd(&f.bins[kBins - 1 - ((k - low) >> shift)], 1u);   // the largest first
+    }
+    __syncthreads();
+    static_assert(kBins == 2 * kSelectThreads, "two bins a thread");
+    const uint32_t b0 = f.bins[2 * threadIdx.x], b1 = f.bins[2 * threadIdx.x + 1];
+    uint32_t total, before = above + sum_before(b0 + b1, f.sums, total);
+    if (before < count && before + b0 + b1 >= count) {
+      const bool second = before + b0 < count;
+      f.bin = 2 * threadIdx.x + second;
+      f.above = before + (second ? b0 : 0);
+    }
+    __syncthreads();
+    const uint32_t at = low + ((uint32_t)(kBins - 1 - f.bin) << shift);       // smallest key of the bin
+    const uint32_t held = f.bins[f.bin];
+    above = f.above;
+    if (shift == 0) {                            // one key a bin
+      if (threadIdx.x == 0) { f.least = at; f.ties = count - above; }
+      __syncthreads();
+      return;
+    }
+    low = at;
+    high = min(high, at + ((1u << shift) - 1u));
+    if (held <= kShort) {
+      for (int j = threadIdx.x; j < n; j += kSelectThreads) {
+        const uint32_t k = keys[j];
+        if (k >= low && k <= high) f.keys[atomicAdd(&f.listed, 1u)] = k;
+      }
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < held; i += kSelectThreads) {
+        const uint32_t k = f.keys[i];
+        uint32_t larger = above, equal = 0;
+        for (uint32_t o = 0; o < held; ++o) {
+          larger += f.keys[o] > k;
+          equal += f.keys[o] == k;
+        }
+        if (larger < count && larger + equal >= count) { f.least = k; f.ties = count - larger; }   // the same of equal ones
+      }
+      __syncthreads();
+      return;
+    }
+    __syncthreads();                             // all have read the bin
+  }
+}
+
+template <typename T, int DH> __global__ void __launch_bounds__(kSelectThreads, 2) select_pages_kernel(SelectArgs p) {
   wait_for_previous_kernel();
   constexpr int Q = DH + 64;                     // bytes from query to query: the eight lanes of a read on different banks
   extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ Search found;
   const int heads8 = (p.G + 7) / 8 * 8;
   unsigned char* q_pos = smem;                   // [heads8][Q] positive codes, then negative ones
   unsigned char* q_neg = smem + heads8 * Q;
   float* q_scale = reinterpret_cast<float*>(smem + 2 * heads8 * Q);
   uint32_t* keys = reinterpret_cast<uint32_t*>(q_scale + heads8);   // of all pages, in the cluster's first CTA
-  __shared__ uint32_t sums[2][kSelectWarps];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane >> 2, c = lane & 3;
   const int item = blockIdx.x / p.cluster, rank = blockIdx.x % p.cluster;
   const int s = item / p.c.Hkv, head0 = (item - s * p.c.Hkv) * p.G;
+  if (threadIdx.x == 0) { found.low = kForced; found.high = 0; found.above = 0; }
+  if (p.cluster > 1) cluster_arrive();           // the others may write to this CTA's shared memory
+  // what the first tile needs is on its way before the length is known
   const int given = p.lens[item];
+  const int32_t* pages = p.c.table + (long long)item * p.c.max_pages;
+  int tile = rank * kSelectWarps + warp, page[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) page[h] = tile * 16 + r + 8 * h < p.c.max_pages ? pages[tile * 16 + r + 8 * h] : -1;
+  // ---- queries as 8-bit codes
+  for (int h = warp; h < heads8; h += kSelectWarps) {
+    constexpr int E = DH / 32;
+    float x[E];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      x[i] = h < p.G ? (float)reinterpret_cast<const T*>(p.q + s * p.qs[0] + (head0 + h) * p.qs[1])[E * lane + i] : 0.f;
+      top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    float scale = __fdiv_rn(__uint_as_float(top), 127.f);
+    if (scale < kLeastScale) scale = kLeastScale;
+    const float inv = __frcp_rn(scale);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int code = top < 0x7f800000u ? min(max(__float2int_rn(__fmul_rn(x[i], inv)), -127), 127) : 0;
+      q_pos[h * Q + E * lane + i] = (unsigned char)max(code, 0);
+      q_neg[h * Q + E * lane + i] = (unsigned char)min(code, 0);
+    }
+    if (lane == 0) q_scale[h] = scale;
+  }
   const long long len = min(max((long long)given, 0LL), p.c.capacity);
   if (len != given && rank == 0 && threadIdx.x == 0 && p.status != nullptr) atomicExch(p.status, (int)CKV_EBOUNDS);
   const int size = 1 << p.c.page_shift;
   const int held = (int)((len + size - 1) >> p.c.page_shift);       // pages of the head
-  const int32_t* pages = p.c.table + (long long)item * p.c.max_pages;
   const bool all = held <= p.count;
-
-  if (!all) {
-    // ---- queries as 8-bit codes
-    for (int h = warp; h < heads8; h += kSelectWarps) {
-      constexpr int E = DH / 32;
-      float x[E];
-      uint32_t top = 0;
+  __syncthreads();
+  bool arrived = p.cluster == 1;
+  uint32_t keys_at;                              // of the first CTA
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(keys_at) : "r"((uint32_t)__cvta_generic_to_shared(keys)), "r"(0));
+  // ---- scores of 16 pages at a time
+  const int tiles = all ? 0 : (held + 15) / 16;
+  while (tile < tiles) {
+    const int row[2] = {tile * 16 + r, tile * 16 + r + 8};
+    uint4 a[2][2][DH / 64];                      // [page][largest, smallest][16 bytes of 64]
+    float scale[2];
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        x[i] = h < p.G ? (float)reinterpret_cast<const T*>(p.q + s * p.qs[0] + (head0 + h) * p.qs[1])[E * lane + i] : 0.f;
-        top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-      }
-      top = __reduce_max_sync(0xffffffffu, top);
-      float scale = __fdiv_rn(__uint_as_float(top), 127.f);
-      if (scale < kLeastScale) scale = kLeastScale;
-      const float inv = __frcp_rn(scale);
+    for (int h = 0; h < 2; ++h) {
+      const bool there = row[h] < held && page[h] >= 0 && page[h] < p.c.num_pages;
+      if (!there && row[h] < held && p.status != nullptr && c == 0) atomicExch(p.status, (int)CKV_EBOUNDS);
+      if (!there) page[h] = -1;
+      const int8_t* at = p.codes + (long long)(there ? page[h] : 0) * 2 * DH + c * 16;
+      scale[h] = there ? p.scales[page[h]] : 0.f;
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const int code = top < 0x7f800000u ? min(max(__float2int_rn(__fmul_rn(x[i], inv)), -127), 127) : 0;
-        q_pos[h * Q + E * lane + i] = (unsigned char)max(code, 0);
-        q_neg[h * Q + E * lane + i] = (unsigned char)min(code, 0);
-      }
-      if (lane == 0) q_scale[h] = scale;
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int j = 0; j < DH / 64; ++j)
+          a[h][w][j] = there ? *reinterpret_cast<const uint4*>(at + w * DH + 64 * j) : make_uint4(0, 0, 0, 0);
     }
+    tile += p.cluster * kSelectWarps;
+    int next[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) next[h] = tile * 16 + r + 8 * h < held ? pages[tile * 16 + r + 8 * h] : -1;
+    uint32_t best[2] = {0, 0};
+    for (int h0 = 0; h0 < p.G; h0 += 8) {
+      int d[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int j = 0; j < DH / 64; ++j) {
+          const uint4 b = *reinterpret_cast<const uint4*>((w ? q_neg : q_pos) + (h0 + r) * Q + c * 16 + 64 * j);
+          mma_s8(d, a[0][w][j].x, a[1][w][j].x, a[0][w][j].y, a[1][w][j].y, b.x, b.y);
+          mma_s8(d, a[0][w][j].z, a[1][w][j].z, a[0][w][j].w, a[1][w][j].w, b.z, b.w);
+        }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int h = h0 + 2 * c + x;
+        if (h < p.G) {
+          const float qs = q_scale[h];
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            best[y] = max(best[y], key_of(__fmul_rn(__fmul_rn((float)d[2 * y + x], qs), scale[y])));
+        }
+      }
+    }
+    if (!arrived) {                              // the first CTA is there
+      cluster_wait();
+      arrived = true;
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      best[y] = max(best[y], __shfl_xor_sync(0xffffffffu, best[y], 1));
+      best[y] = max(best[y], __shfl_xor_sync(0xffffffffu, best[y], 2));
+      if (c == 0 && row[y] < held) {
+        uint32_t key = page[y] < 0 ? 0u : best[y];
+        if (row[y] < p.first || row[y] >= held - p.last) key = kForced;
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys_at + 4 * row[y]), "r"(key) : "memory");
+      }
+    }
+    page[0] = next[0];
+    page[1] = next[1];
+  }
+  if (p.cluster > 1) {
+    if (!arrived) cluster_wait();
+    cluster_arrive();
+    cluster_wait();
+  } else {
     __syncthreads();
   }
-  if (p.cluster > 1) cluster_barrier();          // the first CTA is there
-  if (!all) {
-    uint32_t keys_at;                            // of the first CTA
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(keys_at) : "r"((uint32_t)__cvta_generic_to_shared(keys)), "r"(0));
-    // ---- scores of 16 pages at a time
-    const int tiles = (held + 15) / 16;
-    for (int tile = rank * kSelectWarps + warp; tile < tiles; tile += p.cluster * kSelectWarps) {
-      const int row[2] = {tile * 16 + r, tile * 16 + r + 8};
-      int page[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) page[h] = row[h] < held ? pages[row[h]] : -1;
-      uint4 a[2][2][DH / 64];                    // [page][largest, smallest][16 bytes of 64]
-      float scale[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bool there = page[h] >= 0 && page[h] < p.c.num_pages;
-        if (!there && row[h] < held && p.status != nullptr && c == 0) atomicExch(p.status, (int)CKV_EBOUNDS);
-        if (!there) page[h] = -1;
-        const int8_t* at = p.codes + (long long)(there ? page[h] : 0) * 2 * DH + c * 16;
-        scale[h] = there ? p.scales[page[h]] : 0.f;
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int j = 0; j < DH / 64; ++j)
-            a[h][w][j] = there ? *reinterpret_cast<const uint4*>(at + w * DH + 64 * j) : make_uint4(0, 0, 0, 0);
-      }
-      uint32_t best[2] = {0, 0};
-      for (int h0 = 0; h0 < p.G; h0 += 8) {
-        int d[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int j = 0; j < DH / 64; ++j) {
-            const uint4 b = *reinterpret_cast<const uint4*>((w ? q_neg : q_pos) + (h0 + r) * Q + c * 16 + 64 * j);
-            mma_s8(d, a[0][w][j].x, a[1][w][j].x, a[0][w][j].y, a[1][w][j].y, b.x, b.y);
-            mma_s8(d, a[0][w][j].z, a[1][w][j].z, a[0][w][j].w, a[1][w][j].w, b.z, b.w);
-          }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int h = h0 + 2 * c + x;
-          if (h < p.G) {
-            const float qs = q_scale[h];
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-              best[y] = max(best[y], key_of(__fmul_rn(__fmul_rn((float)d[2 * y + x], qs), scale[y])));
-          }
-        }
-      }
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        best[y] = max(best[y], __shfl_xor_sync(0xffffffffu, best[y], 1));
-        best[y] = max(best[y], __shfl_xor_sync(0xffffffffu, best[y], 2));
-        if (c == 0 && row[y] < held) {
-          uint32_t key = page[y] < 0 ? 0u : best[y];
-          if (row[y] < p.first || row[y] >= held - p.last) key = kForced;
-          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys_at + 4 * row[y]), "r"(key) : "memory");
-        }
-      }
-    }
-  }
-  if (p.cluster > 1) cluster_barrier();
-  else __syncthreads();
   if (rank != 0) return;
 
-  // ---- the smallest chosen key, and how many of the pages that have it are chosen
   uint32_t least = 0, ties = 0;
-  int turn = 0;
   if (!all) {
-    uint32_t lo = 0, hi = kForced, above = min(p.first + p.last, held);   // at least `count` keys reach lo, `above` < count hi
-    while (hi - lo > 1) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      uint32_t n = 0;
-      for (int j = threadIdx.x; j < held; j += kSelectThreads) n += keys[j] >= mid;
-      n = sum_of_cta(n, sums, turn);
-      turn ^= 1;
-      if (n >= (uint32_t)p.count) lo = mid;
-      else { hi = mid; above = n; }
-      if (n == (uint32_t)p.count) break;
-    }
-    least = lo;
-    ties = (uint32_t)p.count - (hi == lo + 1 ? above : 0);
-    if (hi != lo + 1) ties = held;               // exactly `count` keys reach `least`
+    find_least(keys, held, (uint32_t)p.count, found);
+    least = found.least;
+    ties = found.ties;
   }
-  // ---- the chosen pages in order: every thread has consecutive ones
+  // ---- the chosen pages in order: every thread has consecutive ones; first their numbers, then their ids
   const int per = (held + kSelectThreads - 1) / kSelectThreads, at = min((int)threadIdx.x * per, held), to = min(at + per, held);
   uint32_t mine = 0;                             // low half: keys above, high half: keys equal to `least`
   for (int j = at; j < to; ++j) mine += all ? 1u : keys[j] > least ? 1u : keys[j] == least ? 0x10000u : 0u;
-  uint32_t before = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t v = __shfl_up_sync(0xffffffffu, before, o);
-    if (lane >= o) before += v;
-  }
-  if (lane == 31) sums[turn][warp] = before;
-  __syncthreads();
-  uint32_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kSelectWarps; ++w) {
-    if (w < warp) before += sums[turn][w];
-    total += sums[turn][w];
-  }
-  before -= mine;
+  uint32_t total;
+  const uint32_t before = sum_before(mine, found.sums, total);
   uint32_t above = before & 0xffffu, equal = before >> 16;
   int32_t* table = p.table_out + (long long)item * p.count;
   int32_t* chosen = p.chosen != nullptr ? p.chosen + (long long)item * p.count : nullptr;
   for (int j = at; j < to; ++j) {
     const uint32_t key = all ? kForced : keys[j];
     const bool is = key > least || all, tie = !is && key == least;
-    if (is || (tie && equal < ties)) {
-      const int place = (int)(above + min(equal, ties));
-      table[place] = pages[j];
-      if (chosen != nullptr) chosen[place] = j;
-    }
+    if (is || (tie && equal < ties)) table[above + min(equal, ties)] = j;
     above += is;
     equal += tie;
   }
   const int n = (int)((total & 0xffffu) + min(total >> 16, ties));
-  for (int j = n + threadIdx.x; j < p.count; j += kSelectThreads) {
-    table[j] = -1;
-    if (chosen != nullptr) chosen[j] = -1;
+  if (at < held && to == held) {
+    // the last page may not be full; it is the last of the chosen ones where it is chosen
+    const uint32_t key = all ? kForced : keys[held - 1];
+    const bool tail = all || key > least || (key == least && equal - 1 < ties);
+    p.lens_out[item] = n * size - (tail ? (int)(((long long)held << p.c.page_shift) - len) : 0);
+  } else if (held == 0 && threadIdx.x == 0) {
+    p.lens_out[item] = 0;
   }
-  if (threadIdx.x == kSelectThreads - 1 || (at < held && to == held)) {
-    if (at < held && to == held) {
-      // the last page may not be full; it is the last of the chosen ones where it is chosen
-      const uint32_t key = all ? kForced : keys[held - 1];
-      const bool tail = all || key > least || (key == least && equal - 1 < ties);
-      p.lens_out[item] = n * size - (tail ? (int)(((long long)held << p.c.page_shift) - len) : 0);
-    } else if (held == 0) {
-      p.lens_out[item] = 0;
-    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.count; i += kSelectThreads) {
+    const int j = i < n ? table[i] : -1;
+    table[i] = j >= 0 ? pages[j] : -1;
+    if (chosen != nullptr) chosen[i] = j;
   }
 }
 
@@ -501,10 +582,10 @@ cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call,
   // a cluster as large as its pages keep busy and as leaves every head one at the same time
   const int tiles = (d.max_pages + 15) / 16;
   p.cluster = 1;
-  while (d.allow_cluster && p.cluster < 8 && p.cluster * kSelectWarps < tiles && 2 * p.cluster * items <= sm_count) p.cluster *= 2;
+  while (d.allow_cluster && p.cluster < 8 && p.cluster * kSelectWarps < tiles && 2 * p.cluster * items <= 2LL * sm_count) p.cluster *= 2;
   const auto kernel = d.dtype == CKV_F32 ? (d.dh == 64 ? select_pages_kernel<float, 64> : select_pages_kernel<float, 128>)
                                          : (d.dh == 64 ? select_pages_kernel<__nv_bfloat16, 64> : select_pages_kernel<__nv_bfloat16, 128>);
-  if (smem > 48 * 1024 - 256) {
+  if (smem > 48 * 1024 - (int)sizeof(Search)) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
   }
