@@ -490,8 +490,8 @@ class PagedCache(_Owner):
         key = ("select", pages, q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(), lens.get_device(),
                table.dtype, table.shape, table.stride(), table.get_device(), rows.dtype, rows.shape, rows.stride(),
                rows.get_device(), _sig(chosen), _sig(summary.codes), _sig(summary.scale))
-        strides = self._plans.get(key) or self._keep(key, self._describe_select(q, lens, summary, pages, table, rows, chosen))
-        rc = self._select(self.handle, self._ref, q.data_ptr(), strides[0], lens.data_ptr(), summary.codes.data_ptr(),
+        strides, = self._plans.get(key) or self._keep(key, self._describe_select(q, lens, summary, pages, table, rows, chosen))
+        rc = self._select(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), summary.codes.data_ptr(),
                           summary.scale.data_ptr(), pages, first, last, table.data_ptr(), rows.data_ptr(),
                           None if chosen is None else chosen.data_ptr(), self._where(stream))
         if rc:
@@ -511,17 +511,35 @@ class PagedCache(_Owner):
 
     def attend_selected(self, q, lens, summary, pages, out=None, lse=None, *, first=1, last=1, ws=None, stream=None):
         """attend over the `pages` pages that select_pages chooses: (out, lse) of one new token per sequence."""
-        if stream is None:
-            table, rows = self._selection(_raw_stream(self._index), pages)
-        else:
-            with self._allocating(stream):
-                table, rows = self._selection(self._on(stream), pages)
-        self.select_pages(q, lens, summary, pages, first=first, last=last, table=table, rows=rows, stream=stream)
-        return self.attend(q, rows, out, lse, ws=ws, table=table, stream=stream)
+        key = ("selected", pages, q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(),
+               lens.get_device(), _sig(summary.codes), _sig(summary.scale), _sig(out), _sig(lse), _sig(ws))
+        strides, size = self._plans.get(key) or self._keep(key, self._describe_selected(q, lens, summary, pages, out, lse, ws))
+        raw = self._where(stream)
+        with self._allocating(stream):
+            captured = self._captured()
+            table, rows = self._selection(raw, pages, captured)
+            out = torch.empty_like(self._out_like) if out is None else out
+            lse = torch.empty_like(self._lse_like) if lse is None else lse
+            ws = self._workspace(raw, captured) if ws is None else ws
+        at, rows_at = table.data_ptr(), rows.data_ptr()
+        rc = self._select(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), summary.codes.data_ptr(),
+                          summary.scale.data_ptr(), pages, first, last, at, rows_at, None, raw)
+        if rc:
+            self._fail(rc, "criticalkv_select_pages")
+        rc = self._decode(self.handle, self._part(pages, at), q.data_ptr(), strides, rows_at, out.data_ptr(), lse.data_ptr(),
+                          ws.data_ptr(), size, raw)
+        if rc:
+            self._fail(rc, "criticalkv_decode")
+        return out, lse
 
-    def _selection(self, raw, pages):
+    def _describe_selected(self, q, lens, summary, pages, out, lse, ws):
+        if pages < 1:
+            raise ValueError("pages must be at least 1")
+        self._check_summary(summary)
+        return self._describe_attend(q, lens, out, lse, ws, None)
+
+    def _selection(self, raw, pages, captured):
         """Table and lengths of the chosen pages, kept like the workspaces.  raw: the current stream."""
-        captured = self._captured()
         both = None if captured else self._chosen.get((raw, pages))
         if both is None:
             n = self.nseq * self.Hkv
@@ -584,9 +602,9 @@ class PagedCache(_Owner):
         with torch.cuda.device(self._index):
             return _capturing()
 
-    def _workspace(self, raw):
-        """raw: the current stream."""
-        if self._captured():
+    def _workspace(self, raw, captured=None):
+        """raw: the current stream, and whether it is being captured (None: not asked yet)."""
+        if self._captured() if captured is None else captured:
             return torch.empty(self._ws_bytes, dtype=torch.uint8, device=self.device)
         ws = self._ws.get(raw)
         if ws is None:
@@ -602,7 +620,7 @@ class PagedCache(_Owner):
         key = (q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(), lens.get_device(),
                _sig(out), _sig(lse), _sig(ws), _sig(table))
         strides, size = self._plans.get(key) or self._keep(key, self._describe_attend(q, lens, out, lse, ws, table))
-        ref = self._ref if table is None else self._part(table)
+        ref = self._ref if table is None else self._part(table.shape[2], table.data_ptr())
         raw = self._where(stream)
         if stream is None:
             out = torch.empty_like(self._out_like) if out is None else out
@@ -619,9 +637,8 @@ class PagedCache(_Owner):
             self._fail(rc, "criticalkv_decode")
         return out, lse
 
-    def _part(self, table):
+    def _part(self, columns, at):
         """The cache's description with another page table (used at once: descriptions are shared by their columns)."""
-        columns = table.shape[2]
         part = self._parts.get(columns)
         if part is None:
             desc = type(self.desc).from_buffer_copy(self.desc)
@@ -629,7 +646,7 @@ class PagedCache(_Owner):
             if len(self._parts) >= 64:
                 self._parts.clear()
             part = self._parts[columns] = desc, C.byref(desc)
-        part[0].page_table = table.data_ptr()
+        part[0].page_table = at
         return part[1]
 
     def _describe_attend(self, q, lens, out, lse, ws, table):

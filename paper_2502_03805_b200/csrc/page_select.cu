@@ -332,7 +332,7 @@ __device__ __forceinline__ void find_least(const uint32_t* keys, int n, uint32_t
       return;
     }
     low = at;
-    high = min(high, at + ((1u << shift) - 1u));
+    high = at + min(high - at, (1u << shift) - 1u);
     if (held <= kShort) {
       for (int j = threadIdx.x; j < n; j += kSelectThreads) {
         const uint32_t k = keys[j];
@@ -496,7 +496,8 @@ template <typename T, int DH> __global__ void __launch_bounds__(kSelectThreads, 
   for (int j = at; j < to; ++j) {
     const uint32_t key = all ? kForced : keys[j];
     const bool is = key > least || all, tie = !is && key == least;
-    if (is || (tie && equal < ties)) table[above + min(equal, ties)] = j;
+    const uint32_t place = above + min(equal, ties);
+    if ((is || (tie && equal < ties)) && place < (uint32_t)p.count) table[place] = j;
     above += is;
     equal += tie;
   }

@@ -248,6 +248,29 @@ def test_many_pages_with_equal_and_special_scores(cols):
     check_choice(told, q, torch.tensor([[16 * cols, 500]], dtype=torch.int32), summary, 20, 2, 1)
 
 
+@pytest.mark.parametrize("n", [2, 3, 40, 1500])
+def test_borders_at_both_ends_of_the_order_of_scores(n):
+    """Few pages, of which some score NaN, infinity, zero or minus infinity: the border is in the first or last of the bins that
+    the scores are spread over."""
+    dh = 64
+    pages = torch.zeros(8, 16, dh, dtype=torch.bfloat16, device="cuda")
+    codes, scale = torch.zeros(8, 2, dh, dtype=torch.int8), torch.ones(8)
+    codes[0], codes[1], codes[2], codes[3] = 5, -5, 1, 2
+    codes[4], codes[5] = 127, -127
+    scale[4], scale[5], scale[7] = 3e38, 3e38, math.nan
+    summary = PageSummary(codes.cuda(), scale.cuda())
+    q = torch.full((1, 1, dh), 2.0, dtype=torch.bfloat16)
+
+    class Told:
+        page = 16
+    told = Told()
+    for seed in range(6):
+        told.table_dev = torch.randint(-1 if seed % 2 else 0, 8, (1, 1, n), generator=gen(seed), dtype=torch.int32)
+        told.c = PagedCache(Hq=1, dtype="bf16", k_pages=pages, v_pages=pages.clone(), page_table=told.table_dev.cuda())
+        for count in sorted({1, n // 2 or 1, n - 1}):
+            check_choice(told, q, torch.tensor([[16 * n - 3]], dtype=torch.int32), summary, count, 0, 0)
+
+
 def test_scores_bound_the_logits():
     """The page with the largest logit of a single query is chosen when its bound stands out; and no page's best logit is
     above its score by more than the codes round."""
