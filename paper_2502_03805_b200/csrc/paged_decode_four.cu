@@ -394,17 +394,15 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
             }
           }
         if (!whole_step) {
-#pragma unroll 1
-          for (int i = 0; i < 1; ++i) {            // a branch: as selections it was a tenth of a step
+          asm volatile("" ::: "memory");           // a branch: as selections it was a tenth of a step
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u)
+          for (int u = 0; u < kUnits; ++u)
 #pragma unroll
-              for (int h = 0; h < 2; ++h)
-                if (absent(row_of(QUAD ? c >> 1 : u, r) + 2 * h)) {
+            for (int h = 0; h < 2; ++h)
+              if (absent(row_of(QUAD ? c >> 1 : u, r) + 2 * h)) {
 #pragma unroll
-                  for (int n = 0; n < NT; ++n) z[n][u][h] = both(-INFINITY);
-                }
-          }
+                for (int n = 0; n < NT; ++n) z[n][u][h] = both(-INFINITY);
+              }
         }
         float2 wt[NT][kUnits][2];                  // weights, then times the value's scale
         float2 sum[NT];
