@@ -29,41 +29,64 @@ struct SummaryArgs {
   int* status;
 };
 
-// Eight consecutive elements of a stored row as floats.
-template <typename T, int FMT> __device__ __forceinline__ void eight_of(const Pages& c, long long page, int in_page, int dh,
-                                                                        int e, float (&x)[8]) {
-  const char* base = c.page[0] + page * c.page_stride;
-  if constexpr (FMT == CKV_CACHE_PLAIN) {
-    constexpr int V = Piece<T>::V;
+// Eight consecutive elements of a stored row: as they lie in memory, and as floats.
+template <typename T, int FMT> struct Eight {
+  static constexpr int V = Piece<T>::V;
+  uint4 raw[FMT == CKV_CACHE_PLAIN ? 8 / V : 1];       // 8-bit and 4-bit codes: x, y
+  float scale;
+  uint32_t group;
+  __device__ __forceinline__ void load(const Pages& c, long long page, int in_page, int dh, int e) {
+    const char* base = c.page[0] + page * c.page_stride;
+    if constexpr (FMT == CKV_CACHE_PLAIN) {
 #pragma unroll
-    for (int i = 0; i < 8 / V; ++i) {
-      float y[V];
-      Piece<T>::get(*reinterpret_cast<const uint4*>(base + ((long long)in_page * dh + e + V * i) * (int)sizeof(T)), y);
-#pragma unroll
-      for (int j = 0; j < V; ++j) x[V * i + j] = y[j];
-    }
-  } else {
-    const long long slot = (page << c.page_shift) + in_page;
-    const float scale = c.scale[0][slot];
-    float y[2][4];
-    if constexpr (FMT == CKV_CACHE_E2M1) {
-      const uint32_t code = *reinterpret_cast<const uint32_t*>(base + (in_page * dh + e) / 2);
-      const float g = e4m3_to_float(c.group[0][slot * (dh / 16) + e / 16]);
-      decode4<FMT>(code, y[0]);
-      decode4<FMT>(code >> 16, y[1]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i / 4][i % 4] *= g;
+      for (int i = 0; i < 8 / V; ++i) raw[i] = *reinterpret_cast<const uint4*>(base + (in_page * dh + e + V * i) * (int)sizeof(T));
     } else {
-      const uint2 code = *reinterpret_cast<const uint2*>(base + in_page * dh + e);
-      decode4<FMT>(code.x, y[0]);
-      decode4<FMT>(code.y, y[1]);
+      const long long slot = (page << c.page_shift) + in_page;
+      if constexpr (FMT == CKV_CACHE_E2M1) {
+        raw[0].x = *reinterpret_cast<const uint32_t*>(base + (in_page * dh + e) / 2);
+        group = c.group[0][slot * (dh / 16) + e / 16];
+      } else {
+        const uint2 code = *reinterpret_cast<const uint2*>(base + in_page * dh + e);
+        raw[0].x = code.x;
+        raw[0].y = code.y;
+      }
+      scale = c.scale[0][slot];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = y[i / 4][i % 4] * scale;
   }
-}
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    if constexpr (FMT == CKV_CACHE_PLAIN) {
+#pragma unroll
+      for (int i = 0; i < 8 / V; ++i) {
+        float y[V];
+        Piece<T>::get(raw[i], y);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[V * i + j] = y[j];
+      }
+    } else if constexpr (FMT == CKV_CACHE_E2M1) {
+      decode8_e2m1(raw[0].x, group, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= scale;
+    } else {
+      float y[2][4];
+      decode4<FMT>(raw[0].x, y[0]);
+      decode4<FMT>(raw[0].y, y[1]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = y[i / 4][i % 4] * scale;
+    }
+  }
+};
 
 // Maximum and minimum that are NaN where either is one: a page with an infinity or a NaN is then seen by its extremes alone.
+__device__ __forceinline__ float nan_max(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float nan_min(float a, float b, float c) {
+  float d;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ float nan_max(float a, float b) {
   float d;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
@@ -111,20 +134,24 @@ __device__ __forceinline__ void reduce_rows(const Pages& c, long long page, int 
       lo[2 * j] = b.x; lo[2 * j + 1] = b.y;
     }
   } else {
-    constexpr int FLY = 4;
+    constexpr int FLY = FMT == CKV_CACHE_PLAIN ? 4 : 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) { hi[j] = -INFINITY; lo[j] = INFINITY; }
     for (int r = sub; r < rows; r += FLY * step) {
-      float x[FLY][8];
+      Eight<T, FMT> row[FLY];
 #pragma unroll
-      for (int i = 0; i < FLY; ++i) eight_of<T, FMT>(c, page, min(r + i * step, rows - 1), dh, e, x[i]);
+      for (int i = 0; i < FLY; ++i) row[i].load(c, page, min(r + i * step, rows - 1), dh, e);
 #pragma unroll
-      for (int i = 0; i < FLY; ++i)
+      for (int i = 0; i < FLY; i += 2) {
+        float x[2][8];
+        row[i].get(x[0]);
+        row[i + 1].get(x[1]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          hi[j] = nan_max(hi[j], x[i][j]);
-          lo[j] = nan_min(lo[j], x[i][j]);
+          hi[j] = nan_max(hi[j], x[0][j], x[1][j]);
+          lo[j] = nan_min(lo[j], x[0][j], x[1][j]);
         }
+      }
     }
   }
 }

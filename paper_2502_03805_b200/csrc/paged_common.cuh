@@ -63,6 +63,20 @@ __device__ __forceinline__ float e4m3_to_float(uint32_t one) {
   return __half2float(__ushort_as_half((unsigned short)h));
 }
 
+// Eight e2m1 codes of a group with the e4m3 scale `group` as floats: code times group scale, exact in a half.
+__device__ __forceinline__ void decode8_e2m1(uint32_t eight, uint32_t group, float (&x)[8]) {
+  uint32_t h[4];
+  e2m1x8_to_half2(eight, h);
+  const uint32_t two = e4m3x2_to_half2(group * 0x101u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h[i]), *reinterpret_cast<const __half2*>(&two));
+    const float2 f = __half22float2(y);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+
 // Four codes as floats, exact: bytes, or for e2m1 the low four half bytes.
 template <int FMT> __device__ __forceinline__ void decode4(uint32_t code, float (&x)[4]) {
   if (FMT == CKV_CACHE_E2M1) {

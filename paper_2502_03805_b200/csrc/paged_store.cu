@@ -313,19 +313,23 @@ __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
         for (int w = 0; w < 2; ++w)
           if (slot[u] >= 0) {
             float x[V];
+            if constexpr (FMT == CKV_CACHE_E2M1 && V == 8) {
+              decode8_e2m1(code[u][w][0], group[u][w], x);
 #pragma unroll
-            for (int i = 0; i < V / 4; ++i) {
-              float y[4];
-              if constexpr (FMT == CKV_CACHE_E2M1) {
-                decode4<FMT>(code[u][w][0] >> (16 * i), y);
-                const float g = e4m3_to_float(group[u][w]);
+              for (int j = 0; j < V; ++j) x[j] *= scale[u][w];
+            } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] *= g;
-              } else {
+              for (int i = 0; i < V / 4; ++i) {
+                float y[4];
                 decode4<FMT>(code[u][w][i], y);
-              }
+                if constexpr (FMT == CKV_CACHE_E2M1) {
+                  const float g = e4m3_to_float(group[u][w]);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * scale[u][w];
+                  for (int j = 0; j < 4; ++j) y[j] *= g;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[4 * i + j] = y[j] * scale[u][w];
+              }
             }
             *reinterpret_cast<uint4*>(p.dst[w] + s * p.ds[0] + g * p.ds[1] + (at + base + u * RPP + sub) * p.ds[2] +
                                       lane * 16) = Piece<T>::put(x);
