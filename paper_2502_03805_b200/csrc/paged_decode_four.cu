@@ -136,30 +136,32 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
   // ---- copies.  A step is two halves of 16 rows, each of one page.
   Segment front;                                   // the step that is looked up next: front_left of this segment are left
   int front_left, front_row;
-  int page[2], here = 0, in_page = 0;              // of the step that is fetched next: its pages, rows, first row in its page
+  struct Next {                                    // a step to be fetched: its pages, rows, first row in its page
+    int page[2], here, in_page;
+  };
   uint32_t present = 0;                            // four bits a step of the ring: whether rows 8i ... 8i + 7 are there
   const uint32_t ring = ptx::smem_addr(&sh.ring[warp][0]);
   auto enter = [&]() {
     front_left = front.t1 - front.t0;
     front_row = (front.t0 * kDecodeWarps + warp) * kWarpRows;
   };
-  auto look_up = [&]() {
+  auto look_up = [&](Next& n) {
     if (front_left == 0) {
       if (front.t0 < front.t1) front = following(front);
       enter();
     }
-    here = front_left > 0 ? front.len - front_row : 0;
-    in_page = front_row & ((1 << p.c.page_shift) - 1);
+    n.here = front_left > 0 ? front.len - front_row : 0;
+    n.in_page = front_row & ((1 << p.c.page_shift) - 1);
     const int32_t* pages = p.c.table + (long long)front.kv * p.c.max_pages + (front_row >> p.c.page_shift);
-    if (here > 0) page[0] = pages[0];
-    page[1] = page[0];
-    if (p.c.page_shift == 4 && here > 16) page[1] = pages[1];
+    n.page[0] = n.here > 0 ? pages[0] : 0;
+    n.page[1] = n.page[0];
+    if (p.c.page_shift == 4 && n.here > 16) n.page[1] = pages[1];
     front_left -= front_left > 0;
     front_row += kRows;
   };
   // scales are copied by lanes 0 to 15 (those of K) and 16 to 31 (of V)
   const int w = lane >> 4, l = lane & 15;
-  auto fetch = [&](int stage) {
+  auto fetch = [&](int stage, const Next& n) {
     using S = Step<DH>;
     constexpr int kCopy = 512 / R::kBytes;         // rows that the lanes copy at once: 8 or 16
     const uint32_t to = ring + stage * (uint32_t)sizeof(S), to_codes = to + lane * 16;
@@ -169,10 +171,10 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
     const bool groups = DH == 128 || l < 8, scales = DH == 128 ? l < 8 : l >= 8;
     present &= ~(15u << (4 * stage));
     __syncwarp();                                  // every lane has read what the step held
-    if (here >= kWarpRows && p.c.page_shift > 4 && (unsigned)page[0] < (unsigned)p.c.num_pages) {
+    if (n.here >= kWarpRows && p.c.page_shift > 4 && (unsigned)n.page[0] < (unsigned)p.c.num_pages) {
       present |= 15u << (4 * stage);
-      const long long at = page[0] * p.c.page_stride + in_page * R::kBytes + lane * 16;
-      const long long slot = ((long long)page[0] << p.c.page_shift) + in_page;
+      const long long at = n.page[0] * p.c.page_stride + n.in_page * R::kBytes + lane * 16;
+      const long long slot = ((long long)n.page[0] << p.c.page_shift) + n.in_page;
       const char *k = p.c.page[0] + at, *v = p.c.page[1] + at;
 #pragma unroll
       for (int i = 0; i < kWarpRows / kCopy; ++i) {
@@ -184,14 +186,14 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
     } else {                                       // the same by halves of 16 rows, which are of a page each and may be absent
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
-        if (here <= 16 * h) break;
-        const int of = h ? page[1] : page[0];
+        if (n.here <= 16 * h) break;
+        const int of = h ? n.page[1] : n.page[0];
         if ((unsigned)of >= (unsigned)p.c.num_pages) {
           if (p.status != nullptr && lane == 0) atomicExch(p.status, (int)CKV_EBOUNDS);
           continue;
         }
-        present |= (here > 16 * h + 8 ? 3u : 1u) << (4 * stage + 2 * h);
-        const int first = in_page + (p.c.page_shift == 4 ? 0 : 16 * h);
+        present |= (n.here > 16 * h + 8 ? 3u : 1u) << (4 * stage + 2 * h);
+        const int first = n.in_page + (p.c.page_shift == 4 ? 0 : 16 * h);
         const long long at = of * p.c.page_stride + first * R::kBytes + lane * 16;
         const long long slot = ((long long)of << p.c.page_shift) + first - 16 * h;
 #pragma unroll
@@ -278,12 +280,14 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
   front = seg;
   enter();
   int stage = 0;
+  Next next = {};
   if (seg.t0 < seg.t1) {
-    look_up();
-    for (int i = 0; i < RING; ++i) {
-      fetch(i);
-      look_up();
-    }
+    Next first[RING];                              // the pages of all of them before the first is needed
+#pragma unroll
+    for (int i = 0; i < RING; ++i) look_up(first[i]);
+    look_up(next);
+#pragma unroll
+    for (int i = 0; i < RING; ++i) fetch(i, first[i]);
   }
   while (seg.t0 < seg.t1) {
     const ItemRows it = item_rows(p, seg.kv, seg.item - seg.kv * p.chunks);
@@ -541,8 +545,8 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
           }
         }
       }
-      fetch(stage);
-      look_up();
+      fetch(stage, next);
+      look_up(next);
       if (++stage == RING) stage = 0;
     }
     // ---- the warps meet in shared memory: references first, then the sums rescaled to the largest, four queries at a time
