@@ -70,7 +70,8 @@ typedef enum { CKV_NORM_L1 = 0, CKV_NORM_L2 = 1 } criticalkv_norm;
 
 enum {
   CKV_FLAG_WO_SHARED = 1u << 0,   /* WO has no nb dimension (one projection for the whole call)             */
-  CKV_FLAG_FORCE_SIMT = 1u << 1,  /* bf16 only: use the CUDA-core kernels instead of the tensor-core ones   */
+  CKV_FLAG_FORCE_SIMT = 1u << 1,  /* use the CUDA-core kernels instead of the tensor-core ones (bf16, and
+                                     criticalkv_decode of float32 queries on 4-bit pages)                   */
   CKV_FLAG_PROTECT_WINDOW = 1u << 3, /* always keep the last w entries (the observation window): their scores are
                                      raised to the largest float32 in both stages, so they fill stage 1 first and
                                      count against the budget                                                   */
@@ -90,8 +91,9 @@ enum {
                                      layer at a time that is about twice as fast.  Same results bit for bit      */
   CKV_FLAG_SELECT_NO_CLUSTER = 1u << 8, /* criticalkv_select: no thread-block clusters in steps 3-4 (the separate
                                      kernels then give every head one CTA), for contexts where cluster launches are
-                                     not wanted.  Same results bit for bit.  criticalkv_decode: none either, some small
-                                     calls take two launches then; the sums are added in another order         */
+                                     not wanted.  Same results bit for bit.  criticalkv_select_pages: likewise.
+                                     criticalkv_decode: none either, some small calls take two launches then; the sums are
+                                     added in another order                                                    */
   CKV_FLAG_DEBUG_CHECKS = 1u << 6, /* device-side checks in criticalkv_select, criticalkv_compact and
                                      criticalkv_gather_positions: every index read from idx / offsets / budgets and
                                      every output position is tested against the bounds the descriptor implies
@@ -318,8 +320,8 @@ typedef struct {
   int32_t page_size;     /* rows a page: 16, 32, 64, 128 or 256                                                 */
   int32_t num_pages;     /* pages in the pool, >= 1                                                             */
   int32_t max_pages;     /* columns of the page table, >= 1; a head holds at most max_pages * page_size rows    */
-  uint32_t flags;        /* CKV_FLAG_FORCE_SIMT and CKV_FLAG_SELECT_NO_CLUSTER (criticalkv_decode),
-                            CKV_FLAG_DEBUG_CHECKS                                                               */
+  uint32_t flags;        /* CKV_FLAG_FORCE_SIMT (criticalkv_decode), CKV_FLAG_SELECT_NO_CLUSTER
+                            (criticalkv_decode, criticalkv_select_pages), CKV_FLAG_DEBUG_CHECKS                 */
   float scale;           /* logit scale; <= 0 selects 1/sqrt(dh)                                                */
   uint32_t reserved;     /* must be 0                                                                           */
   int64_t page_stride;   /* elements of k_pages / v_pages from one page to the next, 0 = page_size * dh         */
@@ -402,8 +404,10 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
  * NaN values give results that are not finite (a key that makes a logit -infinity has no weight).  q [nseq, Hq, dh] with element strides q_stride[2] for sequence and head (NULL or 0 = dense); out dense.
  * bf16 queries run on tensor cores: stored 8-bit values enter exactly, sums and the softmax are float32, and a weight
  * enters its product with the values rounded to 16 bits (plain pages) or, times the row's scale, to 22 bits and no finer than
- * 2^-40 of the head's largest such product (8-bit pages).  float32 queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores,
- * in float32 throughout.  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) exceeds 2^26 or, times ceil(max_pages *
+ * 2^-40 of the head's largest such product (8-bit pages; 2^-36 on 4-bit pages, whose code times group scale enters exactly).
+ * float32 queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores, in float32 throughout; on 4-bit pages float32 queries run on
+ * tensor cores too, an element as the sum of two halves (its error 2^-24 of it, or 2^-39 of the query's largest element where
+ * that is more).  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) exceeds 2^26 or, times ceil(max_pages *
  * page_size / 64), 2^31 - 1.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
  * needs no initialisation; calls that may overlap on the GPU need workspaces of their own.
  */

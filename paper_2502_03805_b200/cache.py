@@ -1,4 +1,5 @@
-"""Decoding on a compressed cache: rotary positions, the paged cache, and attention of a new token over it.
+"""Decoding on a compressed cache: rotary positions, the paged cache, and attention of a new token over all of it or over the
+pages that score best.
 
 Device-buffer plumbing around the C ABI, like session.py: shapes, types and devices of tensors are checked here, every
 number is computed by the kernels of libcriticalkv.  Work goes to torch's current stream of the tensors' device unless

@@ -511,7 +511,8 @@ template <typename T, int DH> __global__ void __launch_bounds__(kSelectThreads, 
     least = found.least;
     ties = found.ties;
   }
-  // ---- the chosen pages in order: every thread has consecutive ones; first their numbers, then their ids
+  // ---- the chosen pages in order: every thread has consecutive ones; first their numbers (where the bins were, if there is
+  // room), then their ids
   const int per = (held + kSelectThreads - 1) / kSelectThreads, at = min((int)threadIdx.x * per, held), to = min(at + per, held);
   uint32_t mine = 0;                             // low half: keys above, high half: keys equal to `least`
   for (int j = at; j < to; ++j) mine += all ? 1u : keys[j] > least ? 1u : keys[j] == least ? 0x10000u : 0u;
@@ -520,11 +521,12 @@ template <typename T, int DH> __global__ void __launch_bounds__(kSelectThreads, 
   uint32_t above = before & 0xffffu, equal = before >> 16;
   int32_t* table = p.table_out + (long long)item * p.count;
   int32_t* chosen = p.chosen != nullptr ? p.chosen + (long long)item * p.count : nullptr;
+  int32_t* numbers = p.count <= kBins ? reinterpret_cast<int32_t*>(found.bins) : table;
   for (int j = at; j < to; ++j) {
     const uint32_t key = all ? kForced : keys[j];
     const bool is = key > least || all, tie = !is && key == least;
     const uint32_t place = above + min(equal, ties);
-    if ((is || (tie && equal < ties)) && place < (uint32_t)p.count) table[place] = j;
+    if ((is || (tie && equal < ties)) && place < (uint32_t)p.count) numbers[place] = j;
     above += is;
     equal += tie;
   }
@@ -539,7 +541,7 @@ template <typename T, int DH> __global__ void __launch_bounds__(kSelectThreads, 
   }
   __syncthreads();
   for (int i = threadIdx.x; i < p.count; i += kSelectThreads) {
-    const int j = i < n ? table[i] : -1;
+    const int j = i < n ? numbers[i] : -1;
     table[i] = j >= 0 ? pages[j] : -1;
     if (chosen != nullptr) chosen[i] = j;
   }
