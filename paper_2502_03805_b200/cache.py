@@ -210,6 +210,7 @@ class Rotary(_Owner):
             torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)).contiguous()
         self.device = _device_of(self.freq, "frequencies")
         self.dh, self.rot, self.layout, self.factor = dh, 2 * self.freq.numel(), layout, float(factor)
+        self._kind = (dh, self.rot, layout, self.factor, self.device)
         self._take_handle(handle, self.device)
         self._rope, self._freq_at = self._lib.criticalkv_rope, self.freq.data_ptr()
 
@@ -407,19 +408,18 @@ class PagedCache(_Owner):
         parts of one projection, each with strides of its own; q_out may be q.  With counts only the first counts[s] tokens
         of a sequence are taken (the other rows of q_out keep their contents).  Returns (q_out, lens_out); lens_out may be
         `start`, both are allocated when None."""
-        if q_out is None or lens_out is None:
-            with self._allocating(stream):
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device) if q_out is None else q_out
-                lens_out = torch.empty((self.nseq, self.Hkv), dtype=torch.int32, device=self.device) if lens_out is None else lens_out
-        key = (rotary.dh, rotary.rot, rotary.layout, rotary.factor, rotary.device, q.dtype, q.shape, q.stride(), q.get_device(),
-               k.dtype, k.shape, k.stride(), k.get_device(), v.dtype, v.shape, v.stride(), v.get_device(), positions.dtype,
-               positions.shape, positions.stride(), positions.get_device(), start.dtype, start.shape, start.stride(),
-               start.get_device(), lens_out.dtype, lens_out.shape, lens_out.stride(), lens_out.get_device(), q_out.dtype,
-               q_out.shape, q_out.stride(), q_out.get_device(), _sig(counts))
-        desc, strides = self._plans.get(key) or self._keep(
+        key = (rotary._kind, q.dtype, q.shape, q.stride(), q.get_device(), k.dtype, k.shape, k.stride(), k.get_device(), v.dtype,
+               v.shape, v.stride(), v.get_device(), positions.dtype, positions.shape, positions.stride(), positions.get_device(),
+               start.dtype, start.shape, start.stride(), start.get_device(), _sig(lens_out), _sig(q_out), _sig(counts))
+        desc, strides, like = self._plans.get(key) or self._keep(
             key, self._describe_append(q, k, v, positions, rotary, start, lens_out, q_out, counts))
         raw = self._where(stream)
-        rotary._where(stream)                    # its frequencies are read there
+        if raw not in rotary._seen:              # its frequencies are read there
+            rotary._where(stream)
+        if q_out is None or lens_out is None:
+            with self._allocating(stream):
+                q_out = torch.empty_like(like, memory_format=torch.contiguous_format) if q_out is None else q_out
+                lens_out = torch.empty_like(start) if lens_out is None else lens_out
         rc = self._append(
             self.handle, self._ref, desc, q.data_ptr(), k.data_ptr(), v.data_ptr(), strides, positions.data_ptr(),
             rotary._freq_at, None if counts is None else counts.data_ptr(), start.data_ptr(), q_out.data_ptr(),
@@ -438,17 +438,25 @@ class PagedCache(_Owner):
         _need(q, "q", (self.nseq, self.Hq, T, self.dh), self.torch_dtype, dev, dense=False)
         for t, what in ((k, "k"), (v, "v")):
             _need(t, what, (self.nseq, self.Hkv, T, self.dh), self.torch_dtype, dev, dense=False)
-        _need(q_out, "q_out", q.shape, self.torch_dtype, dev, dense=False)
+        if q_out is not None:
+            _need(q_out, "q_out", q.shape, self.torch_dtype, dev, dense=False)
         _need(positions, "positions", (self.nseq, T), torch.int32, dev)
         _need(start, "start", (self.nseq, self.Hkv), torch.int32, dev)
-        _need(lens_out, "lens_out", (self.nseq, self.Hkv), torch.int32, dev)
+        if lens_out is not None:
+            _need(lens_out, "lens_out", (self.nseq, self.Hkv), torch.int32, dev)
         if counts is not None:
             _need(counts, "counts", (self.nseq,), torch.int32, dev)
         zero = (0, 0, 0)
         desc = B.make_rope_desc(nseq=self.nseq, T=T, Hq=self.Hq, Hk=self.Hkv, dh=self.dh, rot=rotary.rot, dtype=self.dtype,
                                 layout=rotary.layout, factor=rotary.factor, q_stride=_row_strides(q, "q") or zero,
-                                k_stride=_row_strides(k, "k") or zero, q_out_stride=_row_strides(q_out, "q_out") or zero)
-        return desc, B._strides(_row_strides(v, "v"))
+                                k_stride=_row_strides(k, "k") or zero,
+                                q_out_stride=zero if q_out is None else _row_strides(q_out, "q_out") or zero)
+        return desc, B._strides(_row_strides(v, "v")), self._like(q.shape)
+
+    def _like(self, shape):
+        """What torch.empty_like makes a dense tensor of the model's type from (half as long as torch.empty with a shape, a
+        type and a device takes); one element, whatever the shape."""
+        return torch.empty((1,) * len(shape), dtype=self.torch_dtype, device=self.device).expand(shape)
 
     def new_summary(self):
         """A summary of no pages."""
@@ -556,19 +564,31 @@ class PagedCache(_Owner):
         """Rows 0..min(lens, n)-1 of every head as K_out, V_out [nseq, Hkv, n, dh] (zeros where there is no row, when
         allocated here; left as they were in a caller's tensor).  align_right puts the last rows of a head at the end,
         as the compression step's valid_from = n - lens wants it."""
-        clear = 0
         if K_out is None or V_out is None:
             if n is None or K_out is not None or V_out is not None:
                 raise ValueError("give n, or both K_out and V_out")
-            with self._allocating(stream):
-                K_out = torch.empty((self.nseq, self.Hkv, n, self.dh), dtype=self.torch_dtype, device=self.device)
-                V_out = torch.empty_like(K_out)
-            clear = B.CKV_LOAD_CLEAR
+            return self._load_new(lens, n, align_right, stream)
         key = (n, lens.dtype, lens.shape, lens.stride(), lens.get_device(), K_out.dtype, K_out.shape, K_out.stride(),
                K_out.get_device(), V_out.dtype, V_out.shape, V_out.stride(), V_out.get_device())
         n, strides = self._plans.get(key) or self._keep(key, self._describe_load(lens, n, K_out, V_out))
-        rc = self._load(self.handle, self._ref, lens.data_ptr(), n, strides, (1 if align_right else 0) + clear, K_out.data_ptr(),
+        rc = self._load(self.handle, self._ref, lens.data_ptr(), n, strides, 1 if align_right else 0, K_out.data_ptr(),
                         V_out.data_ptr(), self._where(stream))
+        if rc:
+            self._fail(rc, "criticalkv_cache_load")
+        return K_out, V_out
+
+    def _load_new(self, lens, n, align_right, stream):
+        key = ("new", n, lens.dtype, lens.shape, lens.stride(), lens.get_device())
+        like = self._plans.get(key)
+        if like is None:
+            _need(lens, "lens", (self.nseq, self.Hkv), torch.int32, self.device)
+            like = self._keep(key, self._like((self.nseq, self.Hkv, n, self.dh)))
+        raw = self._where(stream)
+        with self._allocating(stream):
+            K_out = torch.empty_like(like, memory_format=torch.contiguous_format)
+            V_out = torch.empty_like(like, memory_format=torch.contiguous_format)
+        rc = self._load(self.handle, self._ref, lens.data_ptr(), n, None, (1 if align_right else 0) + B.CKV_LOAD_CLEAR,
+                        K_out.data_ptr(), V_out.data_ptr(), raw)
         if rc:
             self._fail(rc, "criticalkv_cache_load")
         return K_out, V_out
