@@ -83,11 +83,12 @@ __device__ __forceinline__ uint32_t group_scale(float top, float r, bool finite,
   return g;
 }
 
-// Eight elements as e2m1 codes, the first in the lowest half byte.
+// Eight elements as e2m1 codes, the first in the lowest half byte; zeros where the factor is 0 (infinities and NaN, and the
+// sign of zeros, included).
 __device__ __forceinline__ uint32_t encode8_e2m1(const float* x, float factor) {
   float y[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = factor == 0.f ? 0.f : __fmul_rn(x[j], factor);   // no codes of infinities and NaN
+  for (int j = 0; j < 8; ++j) y[j] = __fmul_rn(x[j], factor);
   uint32_t code;
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
@@ -95,7 +96,7 @@ __device__ __forceinline__ uint32_t encode8_e2m1(const float* x, float factor) {
       "mov.b32 %0, {a, b, c, d};\n\t}"
       : "=r"(code)
       : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
-  return code;
+  return factor == 0.f ? 0u : code;
 }
 
 }  // namespace ckv
