@@ -221,12 +221,12 @@ struct LoadArgs {
   long long ds[3];             // destination byte strides: sequence, head, row
   int n;
   int align_right;
-  int clear;                   // rows of the destination that get none are zeroed
   int chunks;
   int* status;
 };
 
-template <typename T, int FMT, int DH>
+// CLEAR: rows of the destination that get none are zeroed.
+template <typename T, int FMT, int DH, bool CLEAR>
 __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
   wait_for_previous_kernel();
   constexpr int V = Piece<T>::V, LANES = DH / V, RPP = kThreads / LANES;
@@ -241,15 +241,15 @@ __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
   const int at = p.align_right ? p.n - rows : 0;         // and where it goes
   const int32_t* pages = p.c.table + (long long)item * p.c.max_pages;
   const int step = RPP * kRows;
-  const int before = p.clear ? at : 0;                   // rows of the destination in front of the first, where they are cleared
-  const int last = p.clear ? p.n - at : rows;            // row behind the last, counted from the first
+  const int before = CLEAR ? at : 0;                     // rows of the destination in front of the first, where they are cleared
+  const int last = CLEAR ? p.n - at : rows;              // row behind the last, counted from the first
   for (long long base = (long long)chunk * step - before; base < last; base += (long long)p.chunks * step) {
     long long slot[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const long long r = base + u * RPP + sub;
       slot[u] = -1;
-      if (r >= 0 && r < rows) {
+      if ((!CLEAR || r >= 0) && r < rows) {
         const int row = from + (int)r;
         const int page = pages[row >> p.c.page_shift];
         if (page >= 0 && page < p.c.num_pages)
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(LoadArgs p) {
         bad = bad || slot[u] < 0;
       }
     }
-    if (p.clear) {
+    if constexpr (CLEAR) {
 #pragma unroll
       for (int u = 0; u < kRows; ++u)
 #pragma unroll
@@ -408,13 +408,15 @@ cudaError_t launch_cache_load(const CacheDims& d, const int32_t* lens, int n, co
   p.lens = lens;
   p.dst[0] = (char*)K_out; p.dst[1] = (char*)V_out;
   for (int i = 0; i < 3; ++i) p.ds[i] = stride[i] * es;
-  p.n = n; p.align_right = align_right; p.clear = clear != 0;
+  p.n = n; p.align_right = align_right;
   p.status = d.debug_checks ? status_word : nullptr;
   const int step = kThreads / (d.dh * es / 16) * kRows;
   p.chunks = chunks_for(n, step, items);
   cudaError_t e = cudaSuccess;
   by_type(d, [&](auto t, auto fmt, auto dh) {
-    e = launch_early<LoadArgs>(load_kernel<decltype(t), decltype(fmt)::value, decltype(dh)::value>,
+    using T = decltype(t);
+    constexpr int FMT = decltype(fmt)::value, DH = decltype(dh)::value;
+    e = launch_early<LoadArgs>(clear ? load_kernel<T, FMT, DH, true> : load_kernel<T, FMT, DH, false>,
                                dim3((unsigned)(items * p.chunks)), kThreads, 0, st, p);
   });
   *launches += 1;
