@@ -374,3 +374,83 @@ def test_refusals():
             cache.attend(q, lens, table=table)
     out, lse = cache.attend_selected(q, lens, summary, 2)                     # empty heads
     assert not bool(out.any()) and bool((lse == -math.inf).all())
+
+
+def test_wild_lengths_absent_pages_and_no_sequences():
+    """Lengths outside the table are clipped, pages outside the pool score last and are treated as absent by attention."""
+    lens = torch.tensor([[160, 160, 0]], dtype=torch.int32)
+    cache = make("e2m1", nseq=1, Hq=6, Hkv=3, dh=64, dtype="bf16", page=16, cols=10, flags=B.CKV_FLAG_DEBUG_CHECKS).fill(lens, 3)
+    summary = cache.c.summarise(cache.c.new_summary(), lens.cuda())
+    q = torch.randn(1, 6, 64, generator=gen(2)).bfloat16()
+    assert cache.c.device_status() == 0
+    want, table, rows = check_choice(cache, q, lens, summary, 4, 1, 1)
+    given = torch.tensor([[2 ** 31 - 1, 161, -2 ** 31]], dtype=torch.int32)
+    got = cache.c.select_pages(q.cuda(), given.cuda(), summary, 4)
+    assert cache.c.device_status() == B.CKV_EBOUNDS
+    assert torch.equal(got[0], table) and torch.equal(got[1], rows)
+    cache.table_dev[0, 0, 3:9] = torch.tensor([-1, cache.k.shape[0], 2 ** 31 - 1, -2 ** 31, -7, 10 ** 9], dtype=torch.int32, device="cuda")
+    want, table, rows = check_choice(cache, q, lens, summary, 4, 1, 1)
+    assert want[0, 0] == [0, 1, 2, 9] and cache.c.device_status() == B.CKV_EBOUNDS
+    out, lse = cache.c.attend_selected(q.cuda(), lens.cuda(), summary, 7)              # three absent pages among the chosen
+    want, table, rows = check_choice(cache, q, lens, summary, 7, 1, 1)
+    there = [j for j in want[0, 0] if 0 <= int(cache.table_dev[0, 0, j]) < cache.k.shape[0]]
+    only = {(0, 0): there, (0, 1): want[0, 1], (0, 2): []}
+    check_attention(cache, q, only, lens, (out, lse), torch.tensor([[16 * len(there), 16 * 7, 0]], dtype=torch.int32))
+    none = PagedCache(Hq=6, dtype="bf16", format="e2m1", k_pages=cache.k, v_pages=cache.v, k_scale=cache.ks, v_scale=cache.vs,
+                      k_group_scale=cache.kg, v_group_scale=cache.vg, page_table=cache.table_dev[:0])
+    empty = none.new_lengths()
+    x = torch.zeros(0, 6, 64, dtype=torch.bfloat16, device="cuda")
+    none.summarise(summary, empty)
+    assert none.attend_selected(x, empty, summary, 4)[0].shape == (0, 6, 64)
+    rotary = Rotary(dh=64, frequencies=rope_frequencies(64), device="cuda:0")
+    assert none.append(x[:, :, None], x[:, :3, None], x[:, :3, None], torch.zeros(0, 1, dtype=torch.int32, device="cuda"), rotary,
+                       empty)[0].shape == (0, 6, 1, 64)
+
+
+def test_two_streams_at_once():
+    """The same cache chooses and attends on two streams that run side by side, with other queries on each."""
+    lens = LENS["ragged"](4, 4)
+    cache = make("e2m1", nseq=4, Hq=16, Hkv=4, dh=128, dtype="bf16", page=32, cols=-(-int(lens.max()) // 32)).fill(lens, 2)
+    qs = [torch.randn(4, 16, 128, generator=gen(i)).bfloat16().cuda() for i in range(2)]
+    dev = lens.cuda()
+    summary = cache.c.summarise(cache.c.new_summary(), dev)
+    want = [[x.clone() for x in cache.c.attend_selected(q, dev, summary, pages)] for q, pages in zip(qs, (5, 5))]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(30):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(cache.c.attend_selected(qs[i], dev, summary, 5))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out, lse in got[i]:
+            assert torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1])
+
+
+def test_pages_behind_two_gigabytes():
+    """A pool whose last pages lie more than 2^31 bytes behind its first: rows in, out, summarised, chosen and attended to."""
+    n, page, dh, Hkv, Hq, rows = 2_200_000, 16, 128, 2, 8, 330
+    k, v = (torch.empty((n, page, dh // 2), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.empty((n, page), device="cuda") for _ in range(2))
+    kg, vg = (torch.empty((n, page, dh // 16), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2))
+    cols = -(-(rows + 1) // page)
+    table = (n - 1 - torch.arange(Hkv * cols, dtype=torch.int32)).view(1, Hkv, cols).cuda()
+    far = PagedCache(Hq=Hq, dtype="bf16", format="e2m1", k_pages=k, v_pages=v, k_scale=ks, v_scale=vs, k_group_scale=kg,
+                     v_group_scale=vg, page_table=table)
+    near = PagedCache.allocate(nseq=1, Hq=Hq, Hkv=Hkv, dh=dh, dtype="bf16", rows=rows + 1, format="e2m1", page_size=page)
+    g = gen(8)
+    K, V = (torch.randn(1, Hkv, rows, dh, generator=g).bfloat16().cuda() for _ in range(2))
+    q, k1, v1 = (torch.randn(1, h, 1, dh, generator=g).bfloat16().cuda() for h in (Hq, Hkv, Hkv))
+    rotary = Rotary(dh=dh, frequencies=rope_frequencies(dh), device="cuda:0")
+    pos = torch.full((1, 1), 9, dtype=torch.int32, device="cuda")
+    results = []
+    for c in (far, near):
+        lens = c.store(K, V, c.new_lengths())
+        summary = PageSummary(torch.empty((c.num_pages, 2, dh), dtype=torch.int8, device="cuda"), torch.empty(c.num_pages, device="cuda"))
+        qr, lens = c.append(q, k1, v1, pos, rotary, lens)
+        c.summarise(summary, lens)
+        ids = c.page_table.long()
+        results.append((qr, lens, *c.load(lens, rows + 1), summary.codes[ids], summary.scale[ids], *c.attend(qr[:, :, 0], lens),
+                        *c.attend_selected(qr[:, :, 0], lens, summary, 6)))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
