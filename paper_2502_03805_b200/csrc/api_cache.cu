@@ -252,7 +252,7 @@ int criticalkv_select_pages(criticalkv_handle h, const criticalkv_cache* c, cons
     if (a.q_stride[i] % vec) return CKV_EALIGN;
   }
   const long long heads = (long long)d.nseq * d.Hkv;
-  if (d.Hq / d.Hkv > 128 || d.max_pages > 32768 || heads > (1LL << 26)) return CKV_ENOTSUP;
+  if (d.Hq / d.Hkv > ckv::kSelectMostGroup || d.max_pages > ckv::kSelectMostPages || heads > (1LL << 26)) return CKV_ENOTSUP;
   // rows are numbered in 32 bits in the chosen table too
   if ((long long)count << d.page_shift > 0x7fffffffLL - 256) return CKV_ENOTSUP;
   if (d.nseq == 0) return CKV_OK;

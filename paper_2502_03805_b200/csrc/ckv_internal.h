@@ -164,6 +164,8 @@ struct AppendCall {
   void* q_out;
   int32_t* lens_out;
 };
+// What a choice of pages takes: query heads a KV head, and pages a head, whose scores fit in shared memory.
+constexpr int kSelectMostGroup = 128, kSelectMostPages = 32768;
 struct SelectPagesCall {
   const void* q;
   long long q_stride[2];                    // elements: sequence, head
@@ -187,7 +189,6 @@ cudaError_t launch_append(const CacheDims& d, const AppendCall& call, int sm_cou
                           int* launches);
 cudaError_t launch_summarise(const CacheDims& d, const int32_t* start, const int32_t* lens, int8_t* codes, float* scales,
                              int sm_count, int* status_word, cudaStream_t st, int* launches);
-size_t select_pages_smem(const CacheDims& d);      // dynamic shared memory of a CTA
 cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call, int sm_count, int* status_word,
                                 cudaStream_t st, int* launches);
 size_t decode_workspace_bytes(const CacheDims& d);

@@ -595,9 +595,8 @@ cudaError_t launch_summarise(const CacheDims& d, const int32_t* start, const int
   return e;
 }
 
-size_t select_pages_smem(const CacheDims& d) {
-  const size_t heads8 = (size_t)(d.Hq / d.Hkv + 7) / 8 * 8;
-  return heads8 * (2 * (d.dh + 64) + 4) + 4 * (size_t)d.max_pages;
+constexpr size_t select_pages_smem(int group, int dh, int max_pages) {
+  return (size_t)(group + 7) / 8 * 8 * (2 * (dh + 64) + 4) + 4 * (size_t)max_pages;
 }
 
 cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call, int sm_count, int* status_word, cudaStream_t st,
@@ -613,7 +612,7 @@ cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call,
   p.count = call.count; p.first = call.first; p.last = call.last;
   p.table_out = call.table_out; p.lens_out = call.lens_out; p.chosen = call.chosen;
   p.status = d.debug_checks ? status_word : nullptr;
-  const int smem = (int)select_pages_smem(d);
+  const int smem = (int)select_pages_smem(d.Hq / d.Hkv, d.dh, d.max_pages);
   // a cluster as large as its pages keep busy and as leaves every head one at the same time
   const int tiles = (d.max_pages + 15) / 16;
   p.cluster = 1;
@@ -621,7 +620,9 @@ cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call,
   const auto kernel = d.dtype == CKV_F32 ? (d.dh == 64 ? select_pages_kernel<float, 64> : select_pages_kernel<float, 128>)
                                          : (d.dh == 64 ? select_pages_kernel<__nv_bfloat16, 64> : select_pages_kernel<__nv_bfloat16, 128>);
   if (smem > 48 * 1024 - (int)sizeof(Search)) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    // the same number for every call: host threads with handles of their own set it for one another
+    constexpr int most = (int)select_pages_smem(kSelectMostGroup, 128, kSelectMostPages);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (e != cudaSuccess) return e;
   }
   *launches += 1;

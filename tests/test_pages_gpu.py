@@ -1,6 +1,7 @@
 """Summaries of pages, the choice of pages and attention over them: whole numbers equal to the plain form's, attention against
 64 bits over the rows of the chosen pages."""
 import math
+from concurrent.futures import ThreadPoolExecutor
 
 import numpy as np
 import pytest
@@ -454,3 +455,27 @@ def test_pages_behind_two_gigabytes():
         results.append((qr, lens, *c.load(lens, rows + 1), summary.codes[ids], summary.scale[ids], *c.attend(qr[:, :, 0], lens),
                         *c.attend_selected(qr[:, :, 0], lens, summary, 6)))
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_two_threads_with_tables_of_other_lengths():
+    """Caches of two host threads, each with a handle of its own, whose choices take different amounts of shared memory."""
+    work = []
+    for cols, pages in ((32768, 40), (12500, 17)):
+        lens = torch.tensor([[16 * 100 + 3]], dtype=torch.int32)
+        cache = make("plain", nseq=1, Hq=4, Hkv=1, dh=64, dtype="bf16", page=16, cols=101).fill(lens, cols)
+        table = torch.full((1, 1, cols), -1, dtype=torch.int32, device="cuda")
+        table[:, :, :101] = cache.table_dev
+        wide = PagedCache(Hq=4, dtype="bf16", k_pages=cache.k, v_pages=cache.v, page_table=table)
+        q, dev = torch.randn(1, 4, 64, generator=gen(cols)).bfloat16().cuda(), lens.cuda()
+        summary = wide.summarise(wide.new_summary(), dev)
+        want, rows = cache.c.select_pages(q, dev, summary, pages)
+        work.append((wide, q, dev, summary, pages, want, rows))
+    torch.cuda.synchronize()
+
+    def choose(cache, q, dev, summary, pages, want, rows):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            got = [cache.select_pages(q, dev, summary, pages) for _ in range(2000)]
+            return all(torch.equal(t, want) and torch.equal(n, rows) for t, n in got[::100])
+
+    with ThreadPoolExecutor(2) as pool:
+        assert all(f.result() for f in [pool.submit(choose, *w) for w in work])
