@@ -23,7 +23,7 @@
 // Measured: 32 x 6553 rows a head, 32 query heads on 8 of 128, 66 us, 3.9 TB/s (0.60 of the copy bandwidth; as 4-bit pages in
 // paged_decode_mma.cu 88.8, with bulk copies and masks as selections 76 to 82): instructions, 348 for 16 rows (codes and
 // products 165, copies 48), 2.4 a cycle in the loop on 12 warps an SM; 16 warps, with up to 270 bytes spilled, take 69 us, a ring
-// of three steps 68.  float32 queries 74 us.  1 x 819 rows: 8.4 us, a chain of latencies.
+// of three steps 68.  float32 queries 75 us.  1 x 819 rows: 8.4 us, a chain of latencies.
 #include <stddef.h>
 
 #include "paged_decode.cuh"
@@ -61,6 +61,14 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
       : "=l"(reinterpret_cast<unsigned long long&>(d))
       : "l"(reinterpret_cast<const unsigned long long&>(a)), "l"(reinterpret_cast<const unsigned long long&>(b)));
   return d;
+}
+__device__ __forceinline__ void add4(float (&a)[4], const float (&b)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    const float2 x = add2(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]));
+    a[i] = x.x;
+    a[i + 1] = x.y;
+  }
 }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
@@ -343,6 +351,10 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[n][u][e] = 0.f;
+          // The matrix instructions cut their sums off instead of rounding them.  For float32 queries two of them at a time
+          // begin anew, and the products of the second halves have a sum of their own: outputs of 1 to 5 queries a head over
+          // 1101 to 11297 rows were 5e-7 to 3e-6 off in one chain, 3e-7 to 6e-7 so (32 x 6553 rows 74.2 -> 75 us)
+          float small[4] = {0.f, 0.f, 0.f, 0.f};
           uint32_t x[2][R::kWords];
           __half2 g[2][DH / 64];
 #pragma unroll
@@ -370,14 +382,23 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
 #pragma unroll
               for (int i = 0; i < 4; ++i) a[h][i] = bits(__hmul2(halves(a[h][i]), g[h][w / 2]));
             }
+            if constexpr (kParts == 2) {
+              float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 4; i += 2)
+              for (int i = 0; i < 4; i += 2) {
+                mma_f16(d, a[0][i], a[1][i], a[0][i + 1], a[1][i + 1], q[0][0][4 * w + i], q[0][0][4 * w + i + 1]);
+                mma_f16(small, a[0][i], a[1][i], a[0][i + 1], a[1][i + 1], q[0][kParts - 1][4 * w + i], q[0][kParts - 1][4 * w + i + 1]);
+              }
+              add4(s[0][u], d);
+            } else {
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
+              for (int i = 0; i < 4; i += 2)
 #pragma unroll
-                for (int part = 0; part < kParts; ++part)
-                  mma_f16(s[n][u], a[0][i], a[1][i], a[0][i + 1], a[1][i + 1], q[n][part][4 * w + i], q[n][part][4 * w + i + 1]);
+                for (int n = 0; n < NT; ++n)
+                  mma_f16(s[n][u], a[0][i], a[1][i], a[0][i + 1], a[1][i + 1], q[n][0][4 * w + i], q[n][0][4 * w + i + 1]);
+            }
           }
+          if (kParts == 2) add4(s[0][u], small);
         }
         // ---- weights.  Pair h of unit u: row `row` of the warp's, query columns 2cc and 2cc + 1
         float2 z[NT][kUnits][2];
