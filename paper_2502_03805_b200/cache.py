@@ -12,6 +12,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import math
+import operator
 
 import torch
 
@@ -491,6 +492,7 @@ class PagedCache(_Owner):
         ones among them.  Returns (table int32 [nseq, Hkv, pages], -1 behind the last chosen page; rows int32 [nseq, Hkv],
         how many rows those pages hold): attend(q, rows, table=table) looks at them.  chosen int32 [nseq, Hkv, pages], when
         given, receives which pages of a head they are."""
+        pages = operator.index(pages)
         if table is None or rows is None:
             with self._allocating(stream):
                 shape = (self.nseq, self.Hkv)
@@ -520,6 +522,7 @@ class PagedCache(_Owner):
 
     def attend_selected(self, q, lens, summary, pages, out=None, lse=None, *, first=1, last=1, ws=None, stream=None):
         """attend over the `pages` pages that select_pages chooses: (out, lse) of one new token per sequence."""
+        pages = operator.index(pages)
         key = ("selected", pages, q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(),
                lens.get_device(), _sig(summary.codes), _sig(summary.scale), _sig(out), _sig(lse), _sig(ws))
         strides, size = self._plans.get(key) or self._keep(key, self._describe_selected(q, lens, summary, pages, out, lse, ws))
@@ -564,6 +567,8 @@ class PagedCache(_Owner):
         """Rows 0..min(lens, n)-1 of every head as K_out, V_out [nseq, Hkv, n, dh] (zeros where there is no row, when
         allocated here; left as they were in a caller's tensor).  align_right puts the last rows of a head at the end,
         as the compression step's valid_from = n - lens wants it."""
+        if n is not None:
+            n = operator.index(n)            # plans are kept by it, and a tensor may change its value
         if K_out is None or V_out is None:
             if n is None or K_out is not None or V_out is not None:
                 raise ValueError("give n, or both K_out and V_out")
