@@ -564,10 +564,17 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-              for (int n = 0; n < NT; ++n)
+              for (int n = 0; n < NT; ++n) {
+                // Cut-off sums again: a chain over all rows of a warp ends up to half a step a tile low.  For float32 queries
+                // each tile begins anew and is added with a rounding (448 heads of 100000 rows with values of one sign:
+                // 8.5e-5 off on the average in one chain)
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int b = 0; b < kB; ++b)
-                  mma_f16(o[n][4 * y + i], even[0][i], odd[0][i], even[1][i], odd[1][i], weight[n][u][b][0], weight[n][u][b][1]);
+                  mma_f16(kParts == 2 ? d : o[n][4 * y + i], even[0][i], odd[0][i], even[1][i], odd[1][i], weight[n][u][b][0],
+                          weight[n][u][b][1]);
+                if (kParts == 2) add4(o[n][4 * y + i], d);
+              }
           }
         }
       }
