@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import four_bit as F
 from paper_2502_03805_b200 import PagedCache
 from paper_2502_03805_b200 import binding as B
 from test_cache_gpu import gen
@@ -40,3 +41,30 @@ def test_long_heads_with_values_of_one_sign(dh, G, rows):
     assert bool(((out.double() - mean).abs() <= tol * mean).all())
     # the sum of the weights is exact; its logarithm, the product and the product's factor
     assert bool(((lse.double() - math.log(rows)).abs() <= 2 * STEP * math.log(rows)).all())
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("G", [1, 5])
+@pytest.mark.parametrize("place", [0, 17, 63])
+def test_logits_of_one_large_and_many_small_products(dh, G, place):
+    """One product of 1 and dh - 1 of d each, sixteen of which (a matrix instruction's) are 0.9 steps of 1: a chain of cut-off
+    sums loses all of them, 127 d or 63 d.
+
+    The sum begins anew with every two instructions, so the 31 d beside the large product may be lost, and up to three
+    additions of such sums are rounded (the second halves of these queries are zero).  The logit's factor, scale * log2(e), is 1
+    to within 2^-28, the sum of the weights 1; the logarithm's factor 0.693 is off by 2^-28 of it and the result by a rounding."""
+    cache = F.FourBit(nseq=1, Hq=G, Hkv=1, dh=dh, dtype="f32", page=16, cols=1, scale=math.log(2.0))
+    page = int(cache.table[0, 0, 0])
+    for code, group, scale in cache.parts():
+        code[page, 0], group.view(torch.uint8)[page, 0], scale[page, 0] = 0x22, 0x38, 1.0          # a row of ones
+    assert bool((cache.values()[0][page, 0] == 1).all())
+    d = round(0.9 * 2048) / 2048 * 2.0 ** -27
+    q = torch.full((1, G, dh), d)
+    q[0, :, place] = 1.0
+    out, lse = cache.c.attend(q.cuda(), torch.ones(1, 1, dtype=torch.int32, device="cuda"))
+    ln2 = float(torch.tensor(math.log(2.0), dtype=torch.float32))
+    want = ln2 * (1 + (dh - 1) * d)
+    tol = ln2 * (31 * d + (dh // 32 - 1) * STEP / 2 + 2 * 2.0 ** -28) + 2.0 ** -25
+    assert tol < 0.8 * ln2 * (dh - 1) * d                          # what the chain loses is far outside
+    assert bool(((lse.double().cpu() - want).abs() <= tol).all())
+    assert bool((out.cpu() == 1).all())
