@@ -6,6 +6,8 @@ number is computed by the kernels of libcriticalkv.  Work goes to torch's curren
 a stream is given.  The tensors of a call must be ready on that stream; what an object keeps for itself (pages, tables,
 frequencies, workspaces) may be dropped while calls are in flight on torch's own streams.  On a stream that torch did not
 make (an address, torch.cuda.ExternalStream) the caller keeps the object until the calls are done.
+
+Host threads that call one object at once do so on streams of their own: workspaces are kept per stream.
 """
 from __future__ import annotations
 
@@ -13,6 +15,7 @@ import contextlib
 import ctypes as C
 import math
 import operator
+import threading
 
 import torch
 
@@ -329,6 +332,7 @@ class PagedCache(_Owner):
         self._append, self._select = self._lib.criticalkv_cache_append, self._lib.criticalkv_select_pages
         self._parts = {}                 # descriptions of the cache with chosen pages, by their number
         self._chosen = {}                # tables of chosen pages, by stream and number
+        self._lock = threading.Lock()    # held from when a shared description or table is set until it has been used
 
     @classmethod
     def allocate(cls, *, nseq, Hq, Hkv, dh, dtype, rows, format="plain", page_size=64, device=0, **kw):
@@ -534,14 +538,14 @@ class PagedCache(_Owner):
             lse = torch.empty_like(self._lse_like) if lse is None else lse
             ws = self._workspace(raw, captured) if ws is None else ws
         at, rows_at = table.data_ptr(), rows.data_ptr()
-        rc = self._select(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), summary.codes.data_ptr(),
-                          summary.scale.data_ptr(), pages, first, last, at, rows_at, None, raw)
+        with self._lock:                         # the choice is read before another thread's is written over it
+            rc, where = self._select(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), summary.codes.data_ptr(),
+                                     summary.scale.data_ptr(), pages, first, last, at, rows_at, None, raw), "criticalkv_select_pages"
+            if not rc:
+                rc, where = self._decode(self.handle, self._part(pages, at), q.data_ptr(), strides, rows_at, out.data_ptr(),
+                                         lse.data_ptr(), ws.data_ptr(), size, raw), "criticalkv_decode"
         if rc:
-            self._fail(rc, "criticalkv_select_pages")
-        rc = self._decode(self.handle, self._part(pages, at), q.data_ptr(), strides, rows_at, out.data_ptr(), lse.data_ptr(),
-                          ws.data_ptr(), size, raw)
-        if rc:
-            self._fail(rc, "criticalkv_decode")
+            self._fail(rc, where)
         return out, lse
 
     def _describe_selected(self, q, lens, summary, pages, out, lse, ws):
@@ -646,7 +650,6 @@ class PagedCache(_Owner):
         key = (q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(), lens.get_device(),
                _sig(out), _sig(lse), _sig(ws), _sig(table))
         strides, size = self._plans.get(key) or self._keep(key, self._describe_attend(q, lens, out, lse, ws, table))
-        ref = self._ref if table is None else self._part(table.shape[2], table.data_ptr())
         raw = self._where(stream)
         if stream is None:
             out = torch.empty_like(self._out_like) if out is None else out
@@ -657,14 +660,20 @@ class PagedCache(_Owner):
                 out = torch.empty_like(self._out_like) if out is None else out
                 lse = torch.empty_like(self._lse_like) if lse is None else lse
                 ws = self._workspace(raw) if ws is None else ws
-        rc = self._decode(self.handle, ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                          ws.data_ptr(), size, raw)
+        if table is None:
+            rc = self._decode(self.handle, self._ref, q.data_ptr(), strides, lens.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                              ws.data_ptr(), size, raw)
+        else:
+            with self._lock:
+                rc = self._decode(self.handle, self._part(table.shape[2], table.data_ptr()), q.data_ptr(), strides,
+                                  lens.data_ptr(), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, raw)
         if rc:
             self._fail(rc, "criticalkv_decode")
         return out, lse
 
     def _part(self, columns, at):
-        """The cache's description with another page table (used at once: descriptions are shared by their columns)."""
+        """The cache's description with another page table.  One for all tables of as many columns, so it is used at once, under
+        the lock."""
         part = self._parts.get(columns)
         if part is None:
             desc = type(self.desc).from_buffer_copy(self.desc)
