@@ -493,7 +493,7 @@ class PagedCache(_Owner):
 
     def select_pages(self, q, lens, summary, pages, *, first=1, last=1, table=None, rows=None, chosen=None, stream=None):
         """The `pages` pages of every head that score best against q [nseq, Hq, dh], the first `first` and the last `last`
-        ones among them.  Returns (table int32 [nseq, Hkv, pages], -1 behind the last chosen page; rows int32 [nseq, Hkv],
+        ones among them (so `pages` is first + last at least: 2, unless one of them is set to 0).  Returns (table int32 [nseq, Hkv, pages], -1 behind the last chosen page; rows int32 [nseq, Hkv],
         how many rows those pages hold): attend(q, rows, table=table) looks at them.  chosen int32 [nseq, Hkv, pages], when
         given, receives which pages of a head they are."""
         pages = operator.index(pages)
@@ -510,8 +510,13 @@ class PagedCache(_Owner):
                           summary.scale.data_ptr(), pages, first, last, table.data_ptr(), rows.data_ptr(),
                           None if chosen is None else chosen.data_ptr(), self._where(stream))
         if rc:
-            self._fail(rc, "criticalkv_select_pages")
+            self._fail_choice(rc, "criticalkv_select_pages", pages, first, last)
         return table, rows
+
+    def _fail_choice(self, rc, where, pages, first, last):
+        if first < 0 or last < 0 or first + last > pages:
+            raise B.CriticalKVError(rc, where, f"pages={pages} must hold the first={first} and the last={last} pages")
+        self._fail(rc, where)
 
     def _describe_select(self, q, lens, summary, pages, table, rows, chosen):
         dev, shape = self.device, (self.nseq, self.Hkv)
@@ -525,7 +530,8 @@ class PagedCache(_Owner):
         return (B._strides(_row_strides(q, "q")),)
 
     def attend_selected(self, q, lens, summary, pages, out=None, lse=None, *, first=1, last=1, ws=None, stream=None):
-        """attend over the `pages` pages that select_pages chooses: (out, lse) of one new token per sequence."""
+        """attend over the `pages` pages that select_pages chooses (first + last at least): (out, lse) of one new token per
+        sequence."""
         pages = operator.index(pages)
         key = ("selected", pages, q.dtype, q.shape, q.stride(), q.get_device(), lens.dtype, lens.shape, lens.stride(),
                lens.get_device(), _sig(summary.codes), _sig(summary.scale), _sig(out), _sig(lse), _sig(ws))
@@ -545,7 +551,7 @@ class PagedCache(_Owner):
                 rc, where = self._decode(self.handle, self._part(pages, at), q.data_ptr(), strides, rows_at, out.data_ptr(),
                                          lse.data_ptr(), ws.data_ptr(), size, raw), "criticalkv_decode"
         if rc:
-            self._fail(rc, where)
+            self._fail_choice(rc, where, pages, first, last)
         return out, lse
 
     def _describe_selected(self, q, lens, summary, pages, out, lse, ws):
