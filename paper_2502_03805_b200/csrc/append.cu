@@ -1,8 +1,8 @@
 // New tokens on their way into the paged cache, in one launch: queries and keys rotated, keys and values written (quantised
 // where the pages are) behind the rows that their heads hold.
 //
-// The rotation is that of rope.cu (angles reduced in float64; cosine and sine in float32), the rounding of a rotated row to
-// the model's type and the scales and codes are those of rope and store one behind the other: the pages get the same bits,
+// The rotation is that of rope.cu (angles reduced in float64; cosine and sine in float32; rotate.cuh), the rounding of a rotated row
+// to the model's type and the scales and codes are those of rope and store one behind the other: the pages get the same bits,
 // but the keys do not travel through memory in between.  A thread owns 16 elements of a row: eight of a half-layout pair's
 // first elements and the eight second ones, or 16 neighbours, so that rotation needs no other lane; it keeps their angles in
 // registers and walks over the rows of its token, two at a time: two query rows, or the key and the value row of a head.
@@ -11,6 +11,7 @@
 // 109; ALU 41 % and latency on 22 warps an SM).  One token: 2.7 us, a chain of latencies.
 #include "launch_early.cuh"
 #include "paged_codes.cuh"
+#include "rotate.cuh"
 
 namespace ckv {
 namespace {
@@ -86,14 +87,6 @@ __device__ __forceinline__ int tokens_of(const AppendArgs& p, int s, bool& bad) 
   const int n = p.counts[s];
   bad = bad || n < 0 || n > p.T;
   return min(max(n, 0), p.T);
-}
-
-// A pair turned: a cos - b sin, b cos + a sin, with the roundings that rope.cu is compiled to (of one product, and of the
-// sum), so that what is appended equals what is rotated and stored in two calls.  The second's rounded product is that of
-// a in rope's kernels for bf16 vectors, that of b in its others.
-__device__ __forceinline__ float turned_first(float a, float b, float c, float s) { return __fmaf_rn(a, c, -__fmul_rn(b, s)); }
-__device__ __forceinline__ float turned_second(float a, float b, float c, float s, bool vectors) {
-  return vectors ? __fmaf_rn(b, c, __fmul_rn(a, s)) : __fmaf_rn(a, s, __fmul_rn(b, c));
 }
 
 // Pair of the turned element e.

@@ -13,6 +13,7 @@
 
 #include "ckv_internal.h"
 #include "launch_early.cuh"
+#include "rotate.cuh"
 
 namespace ckv {
 namespace {
@@ -123,8 +124,8 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs p) {
               T& ta = (VEC && !HALF) ? a[k].e[(2 * i) % (16 / (int)sizeof(T))] : a[k].e[i];
               T& tb = (VEC && !HALF) ? a[k].e[(2 * i + 1) % (16 / (int)sizeof(T))] : b[k].e[i];
               const float va = to_f32<T>(ta), vb = to_f32<T>(tb);
-              ta = from_f32<T>(va * cs[i] - vb * sn[i]);
-              tb = from_f32<T>(vb * cs[i] + va * sn[i]);
+              ta = from_f32<T>(turned_first(va, vb, cs[i], sn[i]));
+              tb = from_f32<T>(turned_second(va, vb, cs[i], sn[i], VEC && sizeof(T) == 2));
             }
           }
           if (VEC) {
