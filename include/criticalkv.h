@@ -406,7 +406,7 @@ CKV_API int criticalkv_cache_load(criticalkv_handle h, const criticalkv_cache* c
  * enters its product with the values rounded to 16 bits (plain pages) or, times the row's scale, to 22 bits and no finer than
  * 2^-40 of the head's largest such product (8-bit pages; 2^-36 on 4-bit pages, whose code times group scale enters exactly).
  * float32 queries, and CKV_FLAG_FORCE_SIMT, run on CUDA cores, in float32 throughout; on 4-bit pages float32 queries run on
- * tensor cores too, an element as the sum of two halves (its error 2^-24 of it, or 2^-39 of the query's largest element where
+ * tensor cores too, an element as the sum of two halves (its error 2^-23 of it, or 2^-39 of the query's largest element where
  * that is more).  CKV_ENOTSUP when nseq * Hkv * ceil(Hq/Hkv / 8) exceeds 2^26 or, times ceil(max_pages *
  * page_size / 64), 2^31 - 1.  ws: criticalkv_decode_workspace_bytes, 256-byte aligned,
  * needs no initialisation; calls that may overlap on the GPU need workspaces of their own.

@@ -9,7 +9,7 @@
 //              rows of an element in a register, so the half bytes of two rows are mixed first, two instructions for four
 //              registers.
 //   queries    halves after a scaling by a power of two that puts the largest element at 2^14, as for 8-bit pages; a float32
-//              query is the sum of two halves (an error of 2^-24 of an element, or 2^-39 of the largest), two products each.
+//              query is the sum of two halves (an error of 2^-23 of an element, or 2^-39 of the largest), two products each.
 //   softmax    a warp's logits are taken relative to a maximum that is moved only when one is 2^10 times above it, and its
 //              weights (times the row scales) relative to a largest one that is moved only when one is 16 times above it: sums
 //              are rescaled a few times a head instead of in most steps.  A weight enters the second product as two halves
