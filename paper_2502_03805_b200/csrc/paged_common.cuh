@@ -39,7 +39,9 @@ __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
   return h;
 }
 
-// Eight e2m1 codes (lowest half byte first) as pairs of halves: exact.
+// Eight e2m1 codes (lowest half byte first) as pairs of halves: exact.  For words that are loaded as 32 bits or more, and for what
+// is masked and mixed from such.  nvcc 12.9 keeps two 16-bit loads in one register and then converts bytes of the wrong half (a prmt
+// in front, which makes a register of the word, prevents that at 4 % of a decode call).
 __device__ __forceinline__ void e2m1x8_to_half2(uint32_t eight, uint32_t (&h)[4]) {
   asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
       "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
@@ -47,8 +49,8 @@ __device__ __forceinline__ void e2m1x8_to_half2(uint32_t eight, uint32_t (&h)[4]
       : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
       : "r"(eight));
 }
-// Four of them by shifts, which place a code's exponent and fraction bits in a half that is 2^-14 times its value: exact.
-// (The conversions above give wrong halves where nvcc 12.9 sees their bytes come from a 16-bit load or a shift.)
+// Four of them, which a 16-bit load may give, by shifts that place a code's exponent and fraction bits in a half that is 2^-14 times
+// its value: exact.
 __device__ __forceinline__ void e2m1x4_to_half2(uint32_t four, uint32_t (&h)[2]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
