@@ -7,7 +7,7 @@
 // numbers, so the matrix instructions' order of additions does not matter and equal inputs choose equal pages anywhere.
 //
 // summarise reads every key once and is bound by HBM.  select reads 2 dh + 4 bytes a page: a (sequence, KV head) is a
-// cluster's of 1 to 16 CTAs whose warps score 16 pages at a time (pages on the 16-row side of mma.sync, 8 queries on the
+// cluster's of 1 to 8 CTAs whose warps score 16 pages at a time (pages on the 16-row side of mma.sync, 8 queries on the
 // other) and leave the scores in the shared memory of the cluster's first CTA, which looks for the smallest chosen one in a
 // histogram and writes the chosen pages in order: one launch, and the table that it writes is one that decode reads.
 //
@@ -246,6 +246,10 @@ constexpr int kSelectThreads = 512, kSelectWarps = kSelectThreads / 32;
 constexpr int kBins = 1024, kShort = 1024;       // of the histogram of keys; pages that share the last bin and are ranked one by one
 constexpr uint32_t kForced = 0xffffffffu;        // key of a page that is always chosen
 
+// Bytes from query to query in shared memory, half of what the banks span more than a multiple of it: the eight lanes of a read, four
+// on each of two queries, are on different banks.
+constexpr int query_bytes(int dh) { return dh % 128 == 64 ? dh : dh + 64; }
+
 struct SelectArgs {
   Pages c;
   const char* q;
@@ -389,7 +393,8 @@ __device__ __forceinline__ void find_least(const uint32_t* keys, int n, uint32_t
 
 template <typename T, int DH> __global__ void __launch_bounds__(kSelectThreads, 2) select_pages_kernel(SelectArgs p) {
   wait_for_previous_kernel();
-  constexpr int Q = DH + 64;                     // bytes from query to query: the eight lanes of a read on different banks
+  constexpr int Q = query_bytes(DH);
+  static_assert(Q % 128 == 64, "two queries a turn of the banks");
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ Search found;
   const int heads8 = (p.G + 7) / 8 * 8;
@@ -596,7 +601,7 @@ cudaError_t launch_summarise(const CacheDims& d, const int32_t* start, const int
 }
 
 constexpr size_t select_pages_smem(int group, int dh, int max_pages) {
-  return (size_t)(group + 7) / 8 * 8 * (2 * (dh + 64) + 4) + 4 * (size_t)max_pages;
+  return (size_t)(group + 7) / 8 * 8 * (2 * query_bytes(dh) + 4) + 4 * (size_t)max_pages;
 }
 
 cudaError_t launch_select_pages(const CacheDims& d, const SelectPagesCall& call, int sm_count, int* status_word, cudaStream_t st,
