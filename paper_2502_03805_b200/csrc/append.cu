@@ -7,8 +7,12 @@
 // first elements and the eight second ones, or 16 neighbours, so that rotation needs no other lane; it keeps their angles in
 // registers and walks over the rows of its token, two at a time: two query rows, or the key and the value row of a head.
 // Bound by HBM: every row is read and written once.  32768 tokens of 32 + 8 heads of 128 bf16 into plain pages: 130 us, 6.2 TB/s
-// (rope and store one behind the other: 107 + 45 us); into 4-bit pages 143 us (floor
-// 109; ALU 41 % and latency on 22 warps an SM).  One token: 2.7 us, a chain of latencies.
+// (rope and store one behind the other: 107 + 45 us); into 4-bit pages 143 us (floor 109; no unit is full: ALU 41 %, 22 warps an
+// SM on 80 registers).  One token: 2.7 us, a chain of latencies.
+// Turned parts that are no multiple of 16 take a kernel of 16 angles a thread that reads a pair's other element by itself, with
+// up to 344 bytes spilled: slower than rope and store, whose kernels move whole vectors for some of these (32768 tokens, plain bf16,
+// 20 elements turned 510 to 520 us, rope and store 374; 24 interleaved 500 and 150, into 4-bit pages 525 and 141; float32, 24 in
+// the half layout 642 and 289; one token 6.2 and 3.7, 36 in the half layout 6.9 and 3.6).
 #include "launch_early.cuh"
 #include "paged_codes.cuh"
 #include "rotate.cuh"

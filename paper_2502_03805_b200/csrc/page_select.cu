@@ -12,7 +12,7 @@
 // histogram and writes the chosen pages in order: one launch, and the table that it writes is one that decode reads.
 //
 // Measured, 8 KV heads of 128: summaries of 131072 bf16 rows 44.6 us, 6.1 TB/s (0.94 of the copy bandwidth; with conversions to
-// float32 66.9), of e4m3 rows 43 (conversions: ALU 62 %); the choice of 64 of 2048 pages for 4 queries a head 8.0 us, a chain of
+// float32 66.9), of e4m3 rows 43 (no unit full: ALU 62 %, DRAM 38 %; what holds it was not found); the choice of 64 of 2048 pages for 4 queries a head 8.0 us, a chain of
 // latencies (length, page, summary, two cluster barriers, histogram; 11.9 with a bisection of the keys), 32 sequences of 512
 // pages 13.4 us.
 #include "launch_early.cuh"

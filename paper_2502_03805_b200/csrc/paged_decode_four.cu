@@ -1,8 +1,8 @@
 // Decode attention over pages in 4 bits a value, on tensor cores.
 //
 // The products are those of paged_decode_mma.cu: the cache rows on the 16-row side of mma.sync, 8 queries on the other,
-// S^T = K Q^T, then O^T = V^T P^T.  A row of 128 elements is 76 bytes, so the kernel is bound by the instructions that turn
-// codes into halves, and everything else is kept short.
+// S^T = K Q^T, then O^T = V^T P^T.  A row of 128 elements is 76 bytes, for which the instructions that turn codes into halves are
+// many, so everything else is kept short.
 //
 //   codes      cvt takes two codes of a byte to two halves; code times group scale is exact in a half (2 and 4 significant
 //              bits), one instruction for two elements.  K: a byte is two elements of a row.  V: the matrix instruction wants two
@@ -20,10 +20,13 @@
 //              (Bulk copies take their operands from uniform registers, which made each of six to nine a step some fifteen
 //              instructions.)
 //
-// Measured: 32 x 6553 rows a head, 32 query heads on 8 of 128, 66 us, 3.9 TB/s (0.60 of the copy bandwidth; as 4-bit pages in
-// paged_decode_mma.cu 88.8, with bulk copies and masks as selections 76 to 82): instructions, 348 for 16 rows (codes and
-// products 165, copies 48), 2.4 a cycle in the loop on 12 warps an SM; 16 warps, with up to 270 bytes spilled, take 69 us, a ring
-// of three steps 68.  float32 queries 75 us.  1 x 819 rows: 8.4 us, a chain of latencies.
+// Measured: 32 x 6553 rows a head, 32 query heads on 8 of 128, 66 to 67 us (73 on another B200), 3.9 TB/s (0.60 of the copy
+// bandwidth; as 4-bit pages in paged_decode_mma.cu 88.8, with bulk copies and masks as selections 76 to 82).  348 instructions for
+// 16 rows (codes and products 165, copies 48), which at four a cycle and SM would be 31 us.  No unit is full: 2.0 a cycle, 2.4 in the
+// loop, ALU 42 %, tensor pipe 19 %, DRAM 40 %.  What holds it are the 12 warps an SM that 163 registers leave, whose most frequent
+// stall is the fixed latency of the instruction before, and CTAs that end 49 to 66 us after the start with equal shares; 16 warps,
+// with up to 270 bytes spilled, take 69 us, a ring of three steps 68.  float32 queries 75.5 us, with 8 query heads a KV head 90.5 (in
+// one chain of cut-off sums 85.8).  1 x 819 rows: 8.4 us, a chain of latencies.
 #include <stddef.h>
 
 #include "paged_decode.cuh"
