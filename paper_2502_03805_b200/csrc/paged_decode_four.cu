@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kDecodeThreads, CTAS) decode_four_kernel(const
           q[n][kParts - 1][i] = bits(__floats2half2_rn(a - back.x, b - back.y));
         }
       }
-      float up[2];
+      float up[2];                                 // (the scale as one float: 2^-24 of a logit, as its other roundings)
 #pragma unroll
       for (int y = 0; y < 2; ++y)
         up[y] = p.scale_log2 * __int_as_float((127 + __shfl_sync(0xffffffffu, e, 8 * cc + 4 * y)) << 23);   // of query 8n + 2cc + y
