@@ -379,7 +379,7 @@ CKV_API int criticalkv_cache_store(criticalkv_handle h, const criticalkv_cache* 
  * those of the cache, k_out_stride 0); v [nseq, Hkv, T, dh] has strides of its own (v_stride[3], NULL or 0 entries = dense).
  * Tokens 0..counts[s]-1 of a sequence (device int32 [nseq]; NULL: all T) go behind row start[s, g] of every head; the others
  * are ignored, their rows of q_out keep their contents.  q_out may be q (same strides); start and lens_out as for
- * criticalkv_cache_store.  Where rot is no multiple of 16 the two calls take less time on the device (a prompt down to 0.27 of it, a token 0.52).
+ * criticalkv_cache_store.  Where rot is no multiple of 16 the two calls take less time on the device (a prompt down to 0.28 of it, a token 0.53).
  */
 CKV_API int criticalkv_cache_append(criticalkv_handle h, const criticalkv_cache* c, const criticalkv_rope_desc* r,
                                     const void* q, const void* k, const void* v, const int64_t* v_stride, const int32_t* pos,

@@ -413,7 +413,7 @@ class PagedCache(_Owner):
         parts of one projection, each with strides of its own; q_out may be q.  With counts only the first counts[s] tokens
         of a sequence are taken (the other rows of q_out keep their contents, whatever a new q_out holds there).  Returns (q_out,
         lens_out); lens_out may be `start`, both are allocated when None.  Where the turned part is no multiple of 16 elements,
-        rotate and store take less time on the device (a prompt down to 0.27 of it, a token 0.52)."""
+        rotate and store take less time on the device (a prompt down to 0.28 of it, a token 0.53)."""
         key = (rotary._kind, q.dtype, q.shape, q.stride(), q.get_device(), k.dtype, k.shape, k.stride(), k.get_device(), v.dtype,
                v.shape, v.stride(), v.get_device(), positions.dtype, positions.shape, positions.stride(), positions.get_device(),
                start.dtype, start.shape, start.stride(), start.get_device(), _sig(lens_out), _sig(q_out), _sig(counts))

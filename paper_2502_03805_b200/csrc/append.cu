@@ -11,8 +11,8 @@
 // SM on 80 registers).  One token: 2.7 us, a chain of latencies.
 // Turned parts that are no multiple of 16 take a kernel of 16 angles a thread that reads a pair's other element by itself, with
 // up to 344 bytes spilled: slower than rope and store, whose kernels move whole vectors for some of these (32768 tokens, plain bf16,
-// 20 elements turned 510 to 520 us, rope and store 374; 24 interleaved 500 and 150, into 4-bit pages 525 and 141; float32, 24 in
-// the half layout 642 and 289; one token 6.2 and 3.7, 36 in the half layout 6.9 and 3.6).
+// 20 elements turned 455 us, rope and store 374; 24 interleaved 447 and 150, into 4-bit pages 503 and 141; float32, 24 in the half
+// layout 644 and 289; one token 5.9 and 3.6, 36 in the half layout 6.8 and 3.6).
 #include "launch_early.cuh"
 #include "paged_codes.cuh"
 #include "rotate.cuh"
@@ -73,6 +73,15 @@ template <typename T> struct Eight {
 #pragma unroll
       for (int j = 0; j < Piece<T>::V; ++j) y[j] = x[Piece<T>::V * i + j];
       raw[i] = Piece<T>::put(y);
+    }
+  }
+  // The elements from the even number `turned` on as they were in `was`: through a float and back a NaN of a bf16 becomes another.
+  __device__ __forceinline__ void keep(const Eight& was, int turned) {
+    if constexpr (sizeof(T) == 2) {
+      if (turned <= 0) raw[0].x = was.raw[0].x;
+      if (turned <= 2) raw[0].y = was.raw[0].y;
+      if (turned <= 4) raw[0].z = was.raw[0].z;
+      if (turned <= 6) raw[0].w = was.raw[0].w;
     }
   }
 };
@@ -195,8 +204,13 @@ __global__ void __launch_bounds__(kThreads, 3) append_kernel(AppendArgs p) {
           xb = turned_second(va, vb, cs[i], sn[i], sizeof(T) == 2);
         }
       }
+      const Eight<T> was[2] = {a[w], b[w]};
       a[w].put(x[w]);                                          // rounded to the model's type
       b[w].put(x[w] + 8);
+      if (MODE == kAnyPair) {                                  // the last thread that turns has elements that are copied
+        a[w].keep(was[0], p.rot - kOwn * u);
+        b[w].keep(was[1], p.rot - kOwn * u - 8);
+      }
     }
     if (MODE == kAnyPair) __syncwarp(mask);                    // the outputs may be the rows that others read pairs from
     if (is_q) {
